@@ -171,7 +171,7 @@ def prepare(case, seed):
         rows, C = case["rows"], case["C"]
         st["x"] = mk.i32(20000.0, rows, C) if case["x32"] else mk.i8(32.0, rows, C)
         if case["res"]:
-            target = 1000.0 if case["h32"] else 10.0     # size of a branch in the units of the stream
+            target = 500.0 if case["h32"] else 10.0      # size of a branch in the units of the stream (ratios stay below 1)
             st["x_scale"] = mk.channel_scale(C, target / (20000.0 if case["x32"] else 1100.0))
             st["res"] = mk.i32(3000.0, rows, C) if case["h32"] else mk.i8(20.0, rows, C)
             st["res_scale"] = _dyadic(0.96875)
