@@ -175,7 +175,7 @@ def prepare(case, seed):
             st["x_scale"] = mk.channel_scale(C, target / (20000.0 if case["x32"] else 1100.0))
             st["res"] = mk.i32(3000.0, rows, C) if case["h32"] else mk.i8(20.0, rows, C)
             st["res_scale"] = _dyadic(0.96875)
-            st["sum"] = torch.zeros_like(st["res"])
+            st["sum"] = torch.zeros_like(st["res"]) if case["h32"] else mk.i8(0.0, rows, C)
         st["gamma"] = mk.channel_scale(C, 0.45 if case["dynamic"] else 32.0 * math.sqrt(C) / 2.0 ** M_LN)
         st["out"] = mk.i8(0.0, rows, C)
         st["row_max"] = torch.zeros(rows, dtype=torch.int32, device=mk.dev) if case["dynamic"] else None
