@@ -22,8 +22,9 @@
  *    its events on first use.
  *  - Work is enqueued on the CUDA stream held by the context; the entry
  *    points do not synchronise (ivit_ctx_profile_stop and ivit_ctx_destroy
- *    do).  Device-side failures (a bounded wait that ran out) are
- *    reported by ivit_ctx_poll_status after the stream has been synchronised.
+ *    do).  Device-side failures (a bounded wait that ran out, an index on the
+ *    device that points nowhere) are reported by ivit_ctx_poll_status after the
+ *    stream has been synchronised.
  *  - Calls on one context take effect in the order in which they are made: any
  *    operand or parameter array of a call may be written by work that was
  *    enqueued on the stream before it, an earlier library call included.
@@ -411,6 +412,84 @@ int ivit_probe_int8_mma(ivit_ctx* ctx, int32_t iters, float* ms, double* ops);
  * of an int8 row of 1536 channels).  The kernels take it from a cubic in 32-bit integers, corrected by its square,
  * instead of running Eq. (iterative); a test compares this routine with the iteration over the whole range. */
 int ivit_isqrt_range(ivit_ctx* ctx, uint32_t n0, uint32_t count, uint16_t* out);
+
+/* ---- decoder operators: root-mean-square norm, a key/value cache held in 4 bits ----
+ * The paper describes encoders; these are the operators that a decoder needs beside ivit_linear, in the same integer arithmetic. */
+
+/* Root-mean-square norm over each row, with the residual's addition in front:
+ *   h   = res ? sat( rq(x; x_scale[c]) + rq(res; res_scale) ) : clip(x)        (sum = h)
+ *   V   = sum_c h^2;  sd = floor(sqrt(V));  e = bit length of sd;  F = sd ? floor(2^(M_ln+e) / sd) : 0
+ *   y   = floor((h F + 2^(e-1)) / 2^e)          (M_ln + 1 significant bits of F whatever the size of the row; |y| <= 2^M_ln)
+ *   z   = rq(y; gamma_scale[c])
+ *   row_max == NULL:  out = sat8(z)                                            (one static scale)
+ *   row_max != NULL:  A = max_c |z|, a = bit length of A, R = floor(127 2^(23+a) / A) (0 when A = 0),
+ *                     out = floor((z R + 2^(22+a)) / 2^(23+a)),  row_max[r] = A:  the row stands for out A / 127
+ * x int8 or int32 (the output, or the accumulators, of a Dense layer); res (the stream) int8, saturated like int8, or int32,
+ * saturated to [-2^20, 2^20]; without res x is clipped to [-2^20, 2^20], x_scale and res_scale are not used and sum must be NULL.
+ * sum has the type of res, may be res itself, or NULL (not wanted).  x_scale and gamma_scale per-channel or per-tensor, res_scale
+ * per-tensor.  8 <= M_ln <= 22, C % 4 == 0, C <= 16384; pointers 16-byte aligned, leading dimensions multiples of 16 bytes (row_max and
+ * the scales' arrays of their own size).  out may not overlap the other tensors. */
+int ivit_rmsnorm(ivit_ctx* ctx, const void* x, int32_t x_dtype, int64_t ldx, ivit_scale x_scale,
+                 const void* res, int32_t res_dtype, int64_t ldres, ivit_scale res_scale,
+                 ivit_scale gamma_scale, int32_t M_ln, void* sum, int64_t ldsum,
+                 int8_t* out, int64_t ldout, int32_t* row_max, int64_t rows, int64_t C);
+
+/* A pool of pages that holds keys and values in 4 bits.  A page takes `page` tokens; its part for one head is a block of
+ * page (d + d/32 + 1) bytes, at data + (page_index heads + head) times that:
+ *   K codes [page][d/2] | K steps [page][d/32] | V codes [page][d/2] | V steps [page]
+ * A value is code step / 8, code in [-7, 7] (held as code + 8 in 4 bits), step in [0, 147]: keys have a step for each 32 channels (some
+ * channels of keys are far larger than others), values one for each token and head.  Byte 4 (d/32 t + g) + i of a K row holds the
+ * channels 32 g + 4 t + i (low half) and 32 g + 16 + 4 t + i (t, i < 4); byte p of a V row holds channels p and p + d/2.
+ * d 64 or 128; page 32, 64, 128 or 256; data 16-byte aligned; a sequence's pages are named by a table of page indices. */
+typedef struct {
+  uint8_t* data;
+  int64_t pages, heads, d, page;
+} ivit_kv4_cache;
+
+#define IVIT_KV4_MAX_LEN 196608   /* keys of a sequence that ivit_kv4_attention takes */
+
+/* Bytes of the whole pool; 0 when the description is not one that the library takes (data is not looked at). */
+size_t ivit_kv4_cache_bytes(const ivit_kv4_cache* cache);
+
+/* Writes tokens into the cache: token t goes to row slots[t] % page of page slots[t] / page.  A negative slot leaves its token out
+ * (padding); one past the pool too, and is reported by ivit_ctx_poll_status (IVIT_ERR_RANGE).  No two tokens of a call may have the same slot.
+ *   keys:   step_g = ceil(8 max |x| / 7) over the 32 channels of group g;  code = floor((16 x + step) / (2 step)), 0 when step is 0
+ *   values: the same with one step over the d channels
+ * K, V int8 [tokens, heads d] (for instance column ranges of a QKV tensor), 16-byte aligned, leading dimensions multiples of 16. */
+int ivit_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
+                    const int64_t* slots, int64_t tokens);
+
+/* Attention of query rows over the cache.  Sequence b has rows q_start[b] .. q_start[b+1]-1 of Q and O and lens[b] keys: key j is
+ * row j % page of page table[b, j / page].  Its last keys are its query tokens' own: query t of n sees the keys j <= lens[b] - n + t.
+ * Query head h reads key/value head h / (q_heads / heads).  For one query row of one head, over the keys j that it sees:
+ *   a_j  = sum_g kstep[j,g] sum_{c in g} q_c kcode[j,c]       (eighths: the 1/8, 1 / sqrt(d) and both scales live in qk_scale)
+ *   s_j  = sat8(rq(a_j; qk_scale));  e_j = ShiftExp(s_j - max s)      (Algorithm 1; top = I0 2^N, 2^14 <= top < 2^24, M = 45, k_out not used)
+ *   u_j  = floor((e_j vstep_j + 2^(z-1)) / 2^z), z = bit length of top - 8     (weights in 16 bits)
+ *   num_c = sum_j u_j vcode[j,c];  den = sum_j e_j;  t_c = floor(num_c 2^(z+5) / den)        (1/256 of a value's unit)
+ *   O_c  = sat8(rq(t_c; pv_scale))
+ * The division comes behind the product, in one piece: probabilities of 8 bits would turn nearly every key of a long row into zero.  A
+ * row that sees no key gets zeros.  weights (NULL: not wanted) int64 [seqs, heads, ldw]:
+ *   weights[b, h, j] += sum over the rows that see j, of all query heads that read h, of floor(e_j 2^24 / den)
+ * Q, O int8 [tokens, q_heads d], not overlapping, 16-byte aligned; rows of no sequence are left as they are.  max_q and max_len: no sequence has more query
+ * tokens or keys (the launch is sized by them; ldtable >= ceil(max_len / page), ldw >= max_len); max_len <= IVIT_KV4_MAX_LEN.  A sequence
+ * that breaks them, a q_start outside 0 .. tokens, or a page outside the pool is reported by ivit_ctx_poll_status (IVIT_ERR_RANGE) and read only as
+ * far as it is valid: keys of such a page are not seen, query rows past max_q or tokens are not written, keys past max_len do not exist. */
+int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
+                       const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable,
+                       ivit_scale qk_scale, ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo,
+                       int64_t* weights, int64_t ldw, int64_t seqs, int64_t max_q, int64_t max_len);
+
+/* Eviction by accumulated weight.  Of every sequence and head with lens[b] > keep keys, keeps the first `sinks`, the last `recent`, and
+ * of the others those of largest weight (of equal ones the lower index) until `keep` are left, in their order; new_lens[b] = min(lens[b], keep).
+ *   kept[b, h, i]   = index of the i-th key that stays, -1 from new_lens[b] on             (int32 [seqs, heads, keep])
+ *   row i of dst_table's pages = that key's codes and steps;  weights_out[b, h, i] = its weight, 0 from new_lens[b] to ldw_out
+ * In place: dst_table == table and weights_out == weights (with the same leading dimensions).  Else the pages of dst_table hold no
+ * source row, and weights_out does not overlap weights.  new_lens may be lens.  sinks + recent <= keep; ldw >= max_len, ldw_out >= keep, ldtable >=
+ * ceil(max_len / page), ld_dst >= ceil(min(keep, max_len) / page); max_len < 2^31.  lens above max_len and pages outside the pool are reported as above (such rows are not moved). */
+int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens,
+                   const int32_t* table, int64_t ldtable, const int32_t* dst_table, int64_t ld_dst,
+                   int64_t* weights_out, int64_t ldw_out, int32_t* kept, int32_t* new_lens,
+                   int64_t seqs, int64_t max_len, int64_t keep, int64_t sinks, int64_t recent);
 
 /* ---- data movement helpers (not in the paper; needed by the full models) ---- */
 

@@ -26,6 +26,7 @@ EXPORTS = [
     "ivit_layernorm", "ivit_block_workspace_bytes", "ivit_block_forward", "ivit_block_forward_static", "ivit_attention",
     "ivit_vit_workspace_bytes", "ivit_vit_forward", "ivit_vit_host_workspace_bytes", "ivit_vit_forward_host",
     "ivit_ctx_profile_start", "ivit_ctx_profile_stop", "ivit_ctx_profile_get", "ivit_kernel_kind_name", "ivit_patchify", "ivit_gather_rows", "ivit_fill_rows",
+    "ivit_rmsnorm", "ivit_kv4_cache_bytes", "ivit_kv4_append", "ivit_kv4_attention", "ivit_kv4_evict",
     "ivit_token_mean", "ivit_dyadic_from_double", "ivit_validate_exp_params", "ivit_validate_scale",
 ]
 
@@ -36,6 +37,10 @@ class CScale(C.Structure):
 
 class CExp(C.Structure):
     _fields_ = [("I0", C.c_int32), ("N", C.c_int32), ("M", C.c_int32), ("k_out", C.c_int32)]
+
+
+class CKv4(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("pages", C.c_int64), ("heads", C.c_int64), ("d", C.c_int64), ("page", C.c_int64)]
 
 
 class CBlock(C.Structure):
@@ -151,6 +156,13 @@ def load_library():
     L.ivit_isqrt_range.argtypes = [vp, C.c_uint32, C.c_uint32, vp]
     L.ivit_kernel_kind_name.argtypes = [i32]
     L.ivit_kernel_kind_name.restype = C.c_char_p
+    L.ivit_rmsnorm.argtypes = [vp, vp, i32, i64, CScale, vp, i32, i64, CScale, CScale, i32, vp, i64, vp, i64, vp, i64, i64]
+    L.ivit_kv4_cache_bytes.argtypes = [C.POINTER(CKv4)]
+    L.ivit_kv4_cache_bytes.restype = C.c_size_t
+    L.ivit_kv4_append.argtypes = [vp, C.POINTER(CKv4), vp, i64, vp, i64, vp, i64]
+    L.ivit_kv4_attention.argtypes = [vp, C.POINTER(CKv4), vp, i64, i64, i64, vp, vp, vp, i64, CScale, CExp, CScale, vp, i64, vp, i64,
+                                     i64, i64, i64]
+    L.ivit_kv4_evict.argtypes = [vp, C.POINTER(CKv4), vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64]
     L.ivit_patchify.argtypes = [vp, vp, i64, i64, i64, i64, i64, i64, vp, i64]
     L.ivit_gather_rows.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64]
     L.ivit_fill_rows.argtypes = [vp, vp, i64, vp, i64, i64]
@@ -182,6 +194,11 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(-2) if t.dim() >= 2 else t.shape[-1]
 
 
+def _row_ld(t: torch.Tensor) -> int:
+    """Leading dimension of a 2-d tensor; one row (or none) has no use for it, and its stride may be anything."""
+    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+
+
 class DevScale:
     """Device-side copy of a Scale: per-channel arrays live in device memory."""
 
@@ -197,7 +214,40 @@ class DevScale:
             self.c = CScale(None, None, int(scale.mult), int(scale.shift))
 
 
+    @classmethod
+    def of(cls, mult, shift) -> "DevScale":
+        """From what is on the device already (int32 multipliers and uint8 shifts, one per channel), or from one pair of numbers."""
+        self = cls(None, None)
+        if torch.is_tensor(mult):
+            if mult.dtype != torch.int32 or shift.dtype != torch.uint8 or mult.shape != shift.shape or not (mult.is_contiguous() and shift.is_contiguous()):
+                raise ValueError("a per-channel scale is a contiguous int32 tensor and a uint8 tensor of the same length")
+            self.mult_t, self.shift_t = mult, shift
+            self.c = CScale(mult.data_ptr(), shift.data_ptr(), 0, 0)
+        else:
+            self.c = CScale(None, None, int(mult), int(shift))
+        return self
+
+
+class Kv4Cache:
+    """A pool of pages that holds keys and values in 4 bits (ivit_kv4_cache): a uint8 tensor [pages, heads, page (d + d/32 + 1)]."""
+
+    def __init__(self, pool: torch.Tensor, d: int, page: int):
+        if pool.dtype != torch.uint8 or pool.dim() != 3 or not pool.is_contiguous() or pool.shape[2] != page * (d + d // 32 + 1):
+            raise ValueError("a pool is a contiguous uint8 tensor [pages, heads, page (d + d/32 + 1)]")
+        self.pool, self.d, self.page, self.heads, self.pages = pool, d, page, pool.shape[1], pool.shape[0]
+        self.c = CKv4(pool.data_ptr(), pool.shape[0], pool.shape[1], d, page)
+        if pool.numel() != load_library().ivit_kv4_cache_bytes(C.byref(self.c)):
+            raise ValueError("ivit_kv4_cache_bytes rejected the cache: d is 64 or 128, page 32, 64, 128 or 256")
+        self.ref = C.byref(self.c)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, d: int, page: int, device) -> "Kv4Cache":
+        return cls(torch.zeros((pages, heads, page * (d + d // 32 + 1)), dtype=torch.uint8, device=device), d, page)
+
+
 def _cexp(p) -> CExp:
+    if isinstance(p, CExp):
+        return p
     return CExp(int(p.I0), int(p.N), int(p.M), int(p.k_out))
 
 
@@ -373,6 +423,107 @@ class Context:
                                      _ld(x) if ldin is None else ldin, gamma_scale.c, _ptr(beta), M_ln,
                                      out.data_ptr(), _ld(out), rows, Cc), "ivit_layernorm")
         return out
+
+    def _want(self, what: str, dtype, dim: int, t: torch.Tensor):
+        """Refuses a tensor that the C side would read as something else."""
+        if t.dtype != dtype or t.dim() != dim or t.device != self.device or (t.shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{what}: want a {dim}-d {dtype} tensor on {self.device} with contiguous rows, got {tuple(t.shape)} "
+                             f"{t.dtype} on {t.device}, strides {t.stride()}")
+
+    def rmsnorm(self, x, gamma_scale: DevScale, x_scale: DevScale = None, res=None, res_scale: DevScale = None, M_ln=20, sum_out=None,
+                out=None, row_max=None):
+        """ivit_rmsnorm: x (int8 or int32) [rows, C], with res added first (its sum goes to sum_out, which may be res); returns int8 rows.
+        row_max (int32 [rows]): every row gets a scale of its own, written there."""
+        rows, Cc = x.shape
+        if out is None:
+            out = torch.empty((rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
+        self._want("x", torch.int8 if x.dtype == torch.int8 else torch.int32, 2, x)
+        self._want("out", torch.int8, 2, out)
+        if out.shape != x.shape or (res is None) != (res_scale is None):
+            raise ValueError("out has the shape of x, and res comes with res_scale")
+        for t, n in ((res, "res"), (sum_out, "sum_out")):
+            if t is not None:
+                self._want(n, torch.int8 if res is not None and res.dtype == torch.int8 else torch.int32, 2, t)
+                if t.shape != x.shape:
+                    raise ValueError(f"{n} has the shape of x")
+        if row_max is not None:
+            self._want("row_max", torch.int32, 1, row_max)
+            if row_max.shape[0] != rows:
+                raise ValueError("row_max has an entry for each row")
+        for s in (gamma_scale, x_scale):
+            if s is not None and s.mult_t is not None and s.mult_t.numel() != Cc:
+                raise ValueError("a per-channel scale has an entry for each channel")
+        one = CScale(None, None, 2 ** 31 - 1, 31)
+        _chk(self.lib.ivit_rmsnorm(self.h, x.data_ptr(), I8 if x.dtype == torch.int8 else I32, _row_ld(x),
+                                   x_scale.c if x_scale is not None else one, _ptr(res),
+                                   I8 if res is not None and res.dtype == torch.int8 else I32, _row_ld(res) if res is not None else 0,
+                                   res_scale.c if res_scale is not None else one, gamma_scale.c, M_ln, _ptr(sum_out),
+                                   _row_ld(sum_out) if sum_out is not None else 0, out.data_ptr(), _row_ld(out), _ptr(row_max), rows, Cc),
+             "ivit_rmsnorm")
+        return out
+
+    # ---- cache in 4 bits ----
+
+    def kv4_append(self, cache: Kv4Cache, k, v, slots):
+        """ivit_kv4_append: int8 rows [tokens, heads d] into the rows of the pool that slots (int64) names; negative: left out."""
+        self._want("k", torch.int8, 2, k)
+        self._want("v", torch.int8, 2, v)
+        self._want("slots", torch.int64, 1, slots)
+        if k.shape != v.shape or k.shape != (slots.shape[0], cache.heads * cache.d) or cache.pool.device != self.device:
+            raise ValueError("k and v are [tokens, heads d], slots [tokens], the pool is on the context's device")
+        _chk(self.lib.ivit_kv4_append(self.h, cache.ref, k.data_ptr(), _row_ld(k), v.data_ptr(), _row_ld(v), slots.data_ptr(),
+                                      slots.shape[0]), "ivit_kv4_append")
+
+    def kv4_attention(self, cache: Kv4Cache, q, q_start, lens, table, qk_scale: DevScale, smax, pv_scale: DevScale, max_q: int, max_len: int,
+                      out=None, weights=None):
+        """ivit_kv4_attention: query rows [tokens, query heads d] of len(lens) sequences over the cache; returns int8 rows of the same
+        shape (a new one starts as zeros, rows of no sequence keep what out held).  weights (int64 [seqs, heads, >= max_len]) is added to."""
+        if out is None:
+            out = torch.zeros_like(q, memory_format=torch.contiguous_format)
+        self._want("q", torch.int8, 2, q)
+        self._want("out", torch.int8, 2, out)
+        self._want("lens", torch.int32, 1, lens)
+        self._want("q_start", torch.int32, 1, q_start)
+        self._want("table", torch.int32, 2, table)
+        seqs = lens.shape[0]
+        if q.shape != out.shape or q.shape[1] % cache.d or q_start.shape[0] != seqs + 1 or table.shape[0] != seqs or cache.pool.device != self.device:
+            raise ValueError("q and out are [tokens, query heads d], q_start [seqs + 1], table [seqs, pages], the pool is on the context's device")
+        if table.shape[1] * cache.page < max_len:
+            raise ValueError("table names pages for max_len keys of each sequence")
+        ldw = 0
+        if weights is not None:
+            self._want("weights", torch.int64, 3, weights)
+            ldw = weights.shape[2]
+            if weights.shape[:2] != (seqs, cache.heads) or not weights.is_contiguous():
+                raise ValueError("weights is a contiguous [seqs, heads, keys]")
+        _chk(self.lib.ivit_kv4_attention(self.h, cache.ref, q.data_ptr(), _row_ld(q), q.shape[1] // cache.d, q.shape[0], q_start.data_ptr(),
+                                         lens.data_ptr(), table.data_ptr(), _row_ld(table), qk_scale.c, _cexp(smax), pv_scale.c,
+                                         out.data_ptr(), _row_ld(out), _ptr(weights), ldw, seqs, max_q, max_len), "ivit_kv4_attention")
+        return out
+
+    def kv4_evict(self, cache: Kv4Cache, weights, lens, table, keep: int, sinks: int, recent: int, max_len: int, dst_table=None,
+                  weights_out=None, kept=None, new_lens=None):
+        """ivit_kv4_evict: at most `keep` keys of each sequence and head stay; in place unless dst_table and weights_out are given.
+        Returns (kept [seqs, heads, keep], new_lens [seqs])."""
+        seqs = lens.shape[0]
+        dst_table = table if dst_table is None else dst_table
+        weights_out = weights if weights_out is None else weights_out
+        kept = torch.empty((seqs, cache.heads, keep), dtype=torch.int32, device=self.device) if kept is None else kept
+        new_lens = torch.empty_like(lens) if new_lens is None else new_lens
+        for n, t, dt, dim in (("weights", weights, torch.int64, 3), ("weights_out", weights_out, torch.int64, 3), ("lens", lens, torch.int32, 1),
+                              ("new_lens", new_lens, torch.int32, 1), ("table", table, torch.int32, 2), ("dst_table", dst_table, torch.int32, 2),
+                              ("kept", kept, torch.int32, 3)):
+            self._want(n, dt, dim, t)
+            if t.shape[0] != seqs or (dim == 3 and (t.shape[1] != cache.heads or not t.is_contiguous())):
+                raise ValueError(f"{n} has an entry for each of the {seqs} sequences (and {cache.heads} heads), contiguous")
+        if kept.shape[2] != keep or cache.pool.device != self.device:
+            raise ValueError("kept is [seqs, heads, keep], the pool is on the context's device")
+        if table.shape[1] * cache.page < max_len or dst_table.shape[1] * cache.page < min(keep, max_len):
+            raise ValueError("the tables name pages for max_len and keep keys of each sequence")
+        _chk(self.lib.ivit_kv4_evict(self.h, cache.ref, weights.data_ptr(), weights.shape[2], lens.data_ptr(), table.data_ptr(), _row_ld(table),
+                                     dst_table.data_ptr(), _row_ld(dst_table), weights_out.data_ptr(), weights_out.shape[2], kept.data_ptr(),
+                                     new_lens.data_ptr(), seqs, max_len, keep, sinks, recent), "ivit_kv4_evict")
+        return kept, new_lens
 
     def patchify(self, img, P, window=0):
         B, Cc, Hi, Wi = img.shape

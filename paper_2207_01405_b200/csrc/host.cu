@@ -11,6 +11,20 @@ using namespace ivit;
 
 namespace {
 
+// The context's device while a call runs, whatever device the caller has current.
+struct DeviceGuard {
+  int before = -1;
+  bool ok;
+  explicit DeviceGuard(const ivit_ctx* ctx) {
+    ok = cudaGetDevice(&before) == cudaSuccess;
+    if (ok && before == ctx->device) before = -1;
+    else ok = ok && cudaSetDevice(ctx->device) == cudaSuccess;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
 
@@ -448,7 +462,8 @@ int ivit_ctx_create(ivit_ctx** out, int device, void* cuda_stream) {
       qres != cudaDriverEntryPointSuccess)
     fn = nullptr;
   c->tmap_encode = fn;
-  if (gemm_tc_prepare_device() != IVIT_OK || gemm_small_prepare_device() != IVIT_OK || attention_prepare_device() != IVIT_OK) {
+  if (gemm_tc_prepare_device() != IVIT_OK || gemm_small_prepare_device() != IVIT_OK || attention_prepare_device() != IVIT_OK ||
+      kv4_prepare_device() != IVIT_OK) {
     cudaGetLastError();
     cudaFree(c->gelu_tables);
     cudaFreeHost(c->status_host);
@@ -1069,6 +1084,99 @@ const char* ivit_kernel_kind_name(int32_t kind) {
     case KIND_MOVE: return "data_movement";
     default: return "unknown";
   }
+}
+
+int ivit_rmsnorm(ivit_ctx* ctx, const void* x, int32_t x_dtype, int64_t ldx, ivit_scale x_scale, const void* res, int32_t res_dtype,
+                 int64_t ldres, ivit_scale res_scale, ivit_scale gamma_scale, int32_t M_ln, void* sum, int64_t ldsum, int8_t* out,
+                 int64_t ldout, int32_t* row_max, int64_t rows, int64_t C) {
+  if (!ctx || rows < 0 || C < 1 || (rows > 0 && (!x || !out)) || (sum && !res)) return IVIT_ERR_INVALID_ARG;
+  if (x_dtype != IVIT_I8 && x_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
+  if (res && res_dtype != IVIT_I8 && res_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
+  if (C % 4 || C > 16384 || rows > (1ll << 40)) return IVIT_ERR_UNSUPPORTED;
+  if (M_ln < 8 || M_ln > 22) return IVIT_ERR_RANGE;
+  if (ldx < C || ldout < C || (res && ldres < C) || (sum && ldsum < C)) return IVIT_ERR_INVALID_ARG;
+  auto misaligned = [](const void* p, int64_t ld, int dtype) { return !aligned16(p) || ld % (dtype == IVIT_I8 ? 16 : 4); };
+  if (misaligned(x, ldx, x_dtype) || misaligned(out, ldout, IVIT_I8) || !aligned4(row_max)) return IVIT_ERR_ALIGNMENT;
+  if ((res && misaligned(res, ldres, res_dtype)) || (sum && misaligned(sum, ldsum, res_dtype))) return IVIT_ERR_ALIGNMENT;
+  if (!scale_ok(gamma_scale) || (res && (!scale_ok(x_scale) || !scale_ok(res_scale) || res_scale.mult_c))) return IVIT_ERR_RANGE;
+  if (!aligned4(gamma_scale.mult_c) || (res && !aligned4(x_scale.mult_c))) return IVIT_ERR_ALIGNMENT;
+  DeviceGuard guard(ctx);
+  if (!guard.ok) return IVIT_ERR_CUDA;
+  return launch_rmsnorm(ctx, x, x_dtype, ldx, to_dev(x_scale), res, res_dtype, ldres, to_dev(res_scale), to_dev(gamma_scale), M_ln, sum, ldsum,
+                        out, ldout, row_max, rows, C);
+}
+
+static int check_kv4(const ivit_kv4_cache* c, bool data) {
+  if (!c || (data && !c->data) || c->pages < 1 || c->heads < 1) return IVIT_ERR_INVALID_ARG;
+  if ((c->d != 64 && c->d != 128) || (c->page != 32 && c->page != 64 && c->page != 128 && c->page != 256)) return IVIT_ERR_UNSUPPORTED;
+  if (c->pages > 0x7fffffffll || c->heads > 65535) return IVIT_ERR_UNSUPPORTED;
+  return data && !aligned16(c->data) ? IVIT_ERR_ALIGNMENT : IVIT_OK;
+}
+
+size_t ivit_kv4_cache_bytes(const ivit_kv4_cache* c) {
+  if (check_kv4(c, false) != IVIT_OK) return 0;
+  return (size_t)c->pages * (size_t)c->heads * (size_t)(c->page * (c->d + c->d / 32 + 1));
+}
+
+int ivit_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
+                    const int64_t* slots, int64_t tokens) {
+  if (!ctx || tokens < 0 || (tokens > 0 && (!K || !V || !slots))) return IVIT_ERR_INVALID_ARG;
+  int rc = check_kv4(cache, true);
+  if (rc) return rc;
+  if (ldk < cache->heads * cache->d || ldv < cache->heads * cache->d) return IVIT_ERR_INVALID_ARG;
+  if (tokens > (1ll << 40)) return IVIT_ERR_UNSUPPORTED;
+  if (!aligned16(K) || !aligned16(V) || ldk % 16 || ldv % 16 || (reinterpret_cast<uintptr_t>(slots) & 7)) return IVIT_ERR_ALIGNMENT;
+  DeviceGuard guard(ctx);
+  if (!guard.ok) return IVIT_ERR_CUDA;
+  return launch_kv4_append(ctx, cache, K, ldk, V, ldv, slots, tokens);
+}
+
+int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
+                       const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable, ivit_scale qk_scale,
+                       ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo, int64_t* weights, int64_t ldw, int64_t seqs,
+                       int64_t max_q, int64_t max_len) {
+  if (!ctx || tokens < 0 || seqs < 0 || max_q < 0 || max_len < 0) return IVIT_ERR_INVALID_ARG;
+  const bool any = tokens > 0 && seqs > 0 && max_q > 0;   // (nothing to do: pointers may be null)
+  if (any && (!Q || !O || Q == O || !q_start || !lens || (!table && max_len > 0))) return IVIT_ERR_INVALID_ARG;
+  int rc = check_kv4(cache, true);
+  if (rc) return rc;
+  if (q_heads < cache->heads || q_heads % cache->heads) return IVIT_ERR_INVALID_ARG;
+  if (ldq < q_heads * cache->d || ldo < q_heads * cache->d || ldtable < (max_len + cache->page - 1) / cache->page || (weights && ldw < max_len))
+    return IVIT_ERR_INVALID_ARG;
+  if (max_len > IVIT_KV4_MAX_LEN || seqs > 65535 || q_heads > 65535 || max_q > 0xffffff || tokens > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  if (!aligned16(Q) || !aligned16(O) || ldq % 16 || ldo % 16 || !aligned4(q_start) || !aligned4(lens) || !aligned4(table) ||
+      (reinterpret_cast<uintptr_t>(weights) & 7))
+    return IVIT_ERR_ALIGNMENT;
+  if (!scale_ok(qk_scale) || !scale_ok(pv_scale) || qk_scale.mult_c || pv_scale.mult_c) return IVIT_ERR_RANGE;
+  if (smax.I0 < 1 || smax.I0 > (1 << 15) || smax.N < 0 || smax.N > 24 || smax.M != 45) return IVIT_ERR_RANGE;
+  const int64_t top = (int64_t)smax.I0 << smax.N;
+  if (top < (1 << 14) || top >= (1 << 24)) return IVIT_ERR_RANGE;
+  if (!any) return IVIT_OK;
+  DeviceGuard guard(ctx);
+  if (!guard.ok) return IVIT_ERR_CUDA;
+  return launch_kv4_attention(ctx, cache, Q, ldq, q_heads, tokens, q_start, lens, table, ldtable, qk_scale, smax, pv_scale, O, ldo, weights, ldw,
+                              seqs, max_q, max_len);
+}
+
+int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens, const int32_t* table,
+                   int64_t ldtable, const int32_t* dst_table, int64_t ld_dst, int64_t* weights_out, int64_t ldw_out, int32_t* kept,
+                   int32_t* new_lens, int64_t seqs, int64_t max_len, int64_t keep, int64_t sinks, int64_t recent) {
+  if (!ctx || seqs < 0 || max_len < 0) return IVIT_ERR_INVALID_ARG;
+  if (seqs > 0 && (!weights || !lens || !table || !dst_table || !weights_out || !kept || !new_lens)) return IVIT_ERR_INVALID_ARG;
+  int rc = check_kv4(cache, true);
+  if (rc) return rc;
+  if (keep < 1 || sinks < 0 || recent < 0 || sinks > keep || recent > keep - sinks) return IVIT_ERR_INVALID_ARG;
+  if (seqs > 65535 || max_len > 0x7fffffffll || keep > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  const int64_t rows = keep < max_len ? keep : max_len;
+  if (ldw < max_len || ldw_out < keep || ldtable < (max_len + cache->page - 1) / cache->page || ld_dst < (rows + cache->page - 1) / cache->page)
+    return IVIT_ERR_INVALID_ARG;
+  if ((dst_table == table && ld_dst != ldtable) || (weights_out == weights && ldw_out != ldw)) return IVIT_ERR_INVALID_ARG;
+  const uintptr_t al8 = reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out);
+  if ((al8 & 7) || !aligned4(lens) || !aligned4(table) || !aligned4(dst_table) || !aligned4(kept) || !aligned4(new_lens)) return IVIT_ERR_ALIGNMENT;
+  DeviceGuard guard(ctx);
+  if (!guard.ok) return IVIT_ERR_CUDA;
+  return launch_kv4_evict(ctx, cache, weights, ldw, lens, table, ldtable, dst_table, ld_dst, weights_out, ldw_out, kept, new_lens, seqs, max_len,
+                          keep, sinks, recent);
 }
 
 int ivit_patchify(ivit_ctx* ctx, const int8_t* img, int64_t B, int64_t C, int64_t Hi, int64_t Wi,

@@ -1,0 +1,247 @@
+"""CPU side of the decoder operators: the reference pinned against floating point and closed forms, the scalars that host and device
+share, and every refusal of the entry points (arguments are checked before anything of the context or the device is touched)."""
+import ctypes as C
+import math
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from ivit_inputs.gen import dyadic
+from oracle import api as O
+from oracle import decoder as D
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+# ---- the reference ----
+
+def test_reference_uses_the_library_s_exponential_and_rounding():
+    rng = np.random.default_rng(0)
+    for I0, N in ((17, 15), (1, 14), (32767, 9), (255, 0)):
+        for n in list(range(256)):
+            assert int(D.shiftexp(n, I0, N)) == O.shiftexp(-n, I0, N)
+    for a, m, s in zip(rng.integers(-2 ** 31, 2 ** 31, 500), rng.integers(1, 2 ** 31, 500), rng.integers(31, 63, 500)):
+        assert int(D.rq(int(a), int(m), int(s))) == O.rq(int(a), int(m), int(s))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [32, 256])
+def test_cache_bytes_round_trip(d, page):
+    rng = np.random.default_rng(d + page)
+    raw = rng.integers(0, 256, (3, 2, page * (d + d // 32 + 1))).astype(np.uint8)
+    assert np.array_equal(D.Cache.of_bytes(raw, d, page).to_bytes(), raw)
+
+
+def test_quantisation_error_is_half_a_step():
+    """code step / 8 is off by at most half a step (exactly: 16 |8 x - code step| <= 8 step 2), and a code never passes 7."""
+    rng = np.random.default_rng(1)
+    for std in (0.5, 3, 30, 200):
+        x = np.clip(np.rint(rng.standard_normal((4000, 32)) * std), -128, 127).astype(np.int64)
+        code, step = D._quantise(x)
+        assert np.abs(code).max() <= 7 and step.max() <= 147 and step.min() >= 0
+        assert (2 * np.abs(8 * x - code * step) <= step).all()
+
+
+def test_attention_reference_against_floating_point():
+    """Against exp and an exact division on the cache's own values.  ShiftExp's weights are p_j (1 + x_j) before they are normalised, |x_j| <= x
+    (read off the table of all differences of scores), which moves an average by at most x / (1 - x) sum p_j |v_j - average|; u_j is off by half
+    a unit of 2^z, which moves it by at most 7 2^(z-1) / 8 for each key over den; the floor of t by 1/256; the last rounding by 1/2."""
+    rng = np.random.default_rng(2)
+    d, page, L, I0, N = 64, 32, 500, 64, 15
+    ref = D.Cache(16, 1, d, page)
+    k = np.clip(np.rint(rng.standard_normal((L, d)) * 32), -128, 127).astype(np.int8)
+    v = np.clip(np.rint(rng.standard_normal((L, d)) * 32), -128, 127).astype(np.int8)
+    ref.append(k, v, np.arange(L))
+    q = np.clip(np.rint(rng.standard_normal((1, d)) * 32), -128, 127).astype(np.int8)
+    ratio, gain = 20.0 / (8 * math.sqrt(d) * 32 * 32), 127 / 128
+    out, w = D.attention(ref, q, 1, [0, 1], [L], np.arange(16)[None], dyadic(ratio), I0, N, dyadic(gain / 256), np.zeros((1, d)),
+                         np.zeros((1, 1, L), np.int64))
+    K = (ref.kc.reshape(-1, d) * np.repeat(ref.ks.reshape(-1, d // 32), 32, -1))[:L] / 8
+    V = (ref.vc.reshape(-1, d) * ref.vs.reshape(-1, 1))[:L] / 8
+    s = np.clip(np.floor(K @ q[0] * 8 * ratio + 0.5), -128, 127)
+    n = np.arange(int(s.max() - s.min()) + 1)
+    x = np.abs(D.shiftexp(n, I0, N) / (I0 << N) / np.exp(-n / I0) - 1).max()
+    p = np.exp((s - s.max()) / I0)
+    den = p.sum() * (1 - x) * (I0 << N)
+    p /= p.sum()
+    z = (I0 << N).bit_length() - 8
+    avg = p @ V
+    tol = 0.5 + gain * (x / (1 - x) * (p[:, None] * np.abs(V - avg)).sum(0) + 7 * 2 ** (z - 1) / 8 * L / den + 1 / 256) + 1e-6
+    assert (np.abs(out[0] - avg * gain) <= tol).all()
+    assert (np.abs(w[0, 0] / 2 ** 24 - p) <= 2 * x / (1 - x) * p + 2.0 ** -24).all()
+    assert 2 ** 24 - L <= w.sum() <= 2 ** 24
+
+
+def test_rmsnorm_reference_against_floating_point():
+    rng = np.random.default_rng(3)
+    C_, M = 777 // 4 * 4, 20
+    for std, wide in ((20, False), (3000, True), (200000, True)):
+        h = np.rint(rng.standard_normal((6, C_)) * std).astype(np.int64)
+        ratio = 30 * math.sqrt(C_) / 2 ** M
+        out, _, _ = D.rmsnorm(h, dyadic(ratio), M)
+        hc = np.clip(h, -2 ** 20, 2 ** 20)
+        want = 30 * hc / np.sqrt((hc.astype(float) ** 2).mean(-1, keepdims=True))
+        # half a unit of rounding, and the floor of the root: at most one part in sd, |value| <= 128
+        assert np.abs(out - np.clip(want, -128, 127)).max() <= 0.5 + 129 / (std * math.sqrt(C_) * 0.9) + 0.01
+        out, top, _ = D.rmsnorm(h, dyadic(0.5), M, dynamic=True)
+        z = out * top[:, None] / 127
+        assert np.abs(out).max(-1).tolist() == [127] * 6 and np.abs(z - want / 30 * 2 ** M / math.sqrt(C_) / 2).max() <= top.max() / 254 + 0.002 * top.max()
+
+
+# ---- scalars of a row, compiled for the host ----
+
+def test_row_scalars_on_the_host(tmp_path):
+    src = tmp_path / "t.cpp"
+    src.write_text('#include "rms_scalars.cuh"\n'
+                   'extern "C" unsigned root(unsigned long long n) { return ivit::isqrt56(n); }\n'
+                   'extern "C" void row(unsigned long long V, int M, int* F, int* e) { auto k = ivit::rms_row(V, M); *F = k.F; *e = k.e; }\n'
+                   'extern "C" void scale(int A, int* R, int* sh) { ivit::rms_row_scale(A, *R, *sh); }\n')
+    so = tmp_path / "t.so"
+    subprocess.run(["g++", "-O2", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2207_01405_b200", "csrc"), "-o", str(so), str(src)], check=True)
+    L = C.CDLL(str(so))
+    L.root.argtypes, L.root.restype = [C.c_ulonglong], C.c_uint
+    L.row.argtypes = [C.c_ulonglong, C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int)]
+    L.scale.argtypes = [C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int)]
+    rng = np.random.default_rng(4)
+    ns = [n for b in range(56) for n in ((1 << b) - 1, 1 << b, (1 << b) + 1)] + [2 ** 56 - 1]
+    ns += [r * r + o for r in rng.integers(2 ** 12, 2 ** 28 - 1, 20000).tolist() for o in (-1, 0, 1)]
+    ns += [int(2 ** x) for x in rng.uniform(0, 56, 50000)]
+    for n in ns:
+        if 0 <= n < 2 ** 56:
+            assert L.root(n) == math.isqrt(n), n
+    a, b = C.c_int(), C.c_int()
+    for n in ns[:2000]:
+        for M in (8, 20, 22):
+            L.row(n, M, C.byref(a), C.byref(b))
+            sd = math.isqrt(n)
+            assert (a.value, b.value) == (((1 << (M + sd.bit_length())) // sd, sd.bit_length()) if sd else (0, 0))
+    for A in list(range(1, 3000)) + rng.integers(1, 2 ** 23, 3000).tolist() + [2 ** 22, 2 ** 22 + 1]:
+        L.scale(A, C.byref(a), C.byref(b))
+        assert b.value == 23 + A.bit_length() and a.value == (127 << b.value) // A and a.value < 2 ** 31
+    L.scale(0, C.byref(a), C.byref(b))
+    assert a.value == 0
+
+
+# ---- refusals ----
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2207_01405_b200 import binding, build
+    build.build()
+    return binding
+
+
+CTX = C.create_string_buffer(8192)          # never looked at: every call here is refused, or has nothing to do
+AT = 1 << 20                                # an aligned address that is never read
+
+
+def rms(b, **k):
+    v = dict(ctx=C.addressof(CTX), x=AT, xd=0, ldx=64, xs=b.CScale(None, None, 2 ** 30, 33), res=None, rd=0, ldr=0, rs=b.CScale(None, None, 2 ** 30, 31),
+             gs=b.CScale(None, None, 2 ** 30, 35), M=20, sum=None, lds=0, out=AT, ldo=64, rm=None, rows=1, C=64)
+    v.update(k)
+    return b.load_library().ivit_rmsnorm(v["ctx"], v["x"], v["xd"], v["ldx"], v["xs"], v["res"], v["rd"], v["ldr"], v["rs"], v["gs"], v["M"], v["sum"],
+                                         v["lds"], v["out"], v["ldo"], v["rm"], v["rows"], v["C"])
+
+
+def test_rmsnorm_refusals(lib):
+    b = lib
+    bad = b.CScale(None, None, 0, 33)
+    chan = b.CScale(AT, AT, 0, 0)
+    for code, k in ((-1, dict(ctx=None)), (-1, dict(x=None)), (-1, dict(out=None)), (-1, dict(rows=-1)), (-1, dict(C=0)), (-1, dict(xd=2)),
+                    (-1, dict(sum=AT, lds=64)), (-1, dict(res=AT, rd=5, ldr=64)), (-4, dict(C=66)), (-4, dict(C=16388, ldx=16400, ldo=16400)),
+                    (-3, dict(M=7)), (-3, dict(M=23)), (-1, dict(ldx=48)), (-1, dict(ldo=48)), (-1, dict(res=AT, ldr=48)),
+                    (-1, dict(res=AT, ldr=64, sum=AT, lds=32)), (-2, dict(x=AT + 4)), (-2, dict(ldx=68)), (-2, dict(out=AT + 1)), (-2, dict(ldo=72)),
+                    (-2, dict(xd=1, ldx=66)), (-2, dict(res=AT, ldr=65)), (-2, dict(res=AT, ldr=64, sum=AT, lds=66)), (-2, dict(rm=AT + 2)),
+                    (-3, dict(gs=bad)), (-3, dict(res=AT, ldr=64, xs=bad)), (-3, dict(res=AT, ldr=64, rs=bad)), (-3, dict(res=AT, ldr=64, rs=chan)),
+                    (-3, dict(gs=b.CScale(AT, None, 0, 0))), (-3, dict(gs=b.CScale(None, None, 5, 63))), (-3, dict(gs=b.CScale(None, None, 5, 30))),
+                    (-2, dict(gs=b.CScale(AT + 2, AT, 0, 0)))):
+        assert rms(b, **k) == code, k
+
+
+def cache(b, **k):
+    v = dict(data=AT, pages=4, heads=2, d=64, page=32)
+    v.update(k)
+    return b.CKv4(v["data"], v["pages"], v["heads"], v["d"], v["page"])
+
+
+BAD_CACHES = [(-1, dict(data=None)), (-1, dict(pages=0)), (-1, dict(heads=0)), (-4, dict(d=32)), (-4, dict(d=96)), (-4, dict(page=48)),
+              (-4, dict(page=16)), (-4, dict(page=512)), (-4, dict(pages=1 << 31)), (-4, dict(heads=65536)), (-2, dict(data=AT + 8))]
+
+
+def test_cache_bytes(lib):
+    L = lib.load_library()
+    for d in (64, 128):
+        for page in (32, 64, 128, 256):
+            assert L.ivit_kv4_cache_bytes(C.byref(cache(lib, d=d, page=page, pages=5, heads=3))) == 15 * page * (d + d // 32 + 1)
+    assert L.ivit_kv4_cache_bytes(C.byref(cache(lib, data=None, pages=1 << 30, heads=65535, d=128, page=256))) == (65535 << 30) * 256 * 133
+    assert L.ivit_kv4_cache_bytes(None) == 0
+    for code, k in BAD_CACHES:
+        if code != -2 and "data" not in k:
+            assert L.ivit_kv4_cache_bytes(C.byref(cache(lib, **k))) == 0
+
+
+def append(b, c=None, **k):
+    v = dict(ctx=C.addressof(CTX), K=AT, ldk=128, V=AT, ldv=128, slots=AT, tokens=1)
+    v.update(k)
+    return b.load_library().ivit_kv4_append(v["ctx"], C.byref(c or cache(b)), v["K"], v["ldk"], v["V"], v["ldv"], v["slots"], v["tokens"])
+
+
+def test_append_refusals(lib):
+    for code, k in BAD_CACHES:
+        assert append(lib, cache(lib, **k)) == code, k
+    for code, k in ((-1, dict(ctx=None)), (-1, dict(K=None)), (-1, dict(V=None)), (-1, dict(slots=None)), (-1, dict(tokens=-1)), (-1, dict(ldk=112)),
+                    (-1, dict(ldv=112)), (-2, dict(K=AT + 4)), (-2, dict(V=AT + 8)), (-2, dict(ldk=136)), (-2, dict(ldv=129)), (-2, dict(slots=AT + 4)),
+                    (-4, dict(tokens=(1 << 40) + 1))):
+        assert append(lib, **k) == code, k
+
+
+def attend(b, c=None, **k):
+    one = b.CScale(None, None, 2 ** 30, 40)
+    v = dict(ctx=C.addressof(CTX), Q=AT, ldq=256, qh=4, tokens=3, qs=AT, lens=AT, table=AT, ldt=4, qk=one, p=b.CExp(17, 15, 45, 8), pv=one, O=2 * AT,
+             ldo=256, w=None, ldw=0, seqs=2, mq=2, ml=100)
+    v.update(k)
+    return b.load_library().ivit_kv4_attention(v["ctx"], C.byref(c or cache(b)), v["Q"], v["ldq"], v["qh"], v["tokens"], v["qs"], v["lens"], v["table"],
+                                               v["ldt"], v["qk"], v["p"], v["pv"], v["O"], v["ldo"], v["w"], v["ldw"], v["seqs"], v["mq"], v["ml"])
+
+
+def test_attention_refusals(lib):
+    b = lib
+    chan, bad = b.CScale(AT, AT, 0, 0), b.CScale(None, None, -4, 40)
+    for code, k in BAD_CACHES:
+        assert attend(b, cache(b, **k)) == code, k
+    for code, k in ((-1, dict(ctx=None)), (-1, dict(Q=None)), (-1, dict(O=None)), (-1, dict(O=AT)), (-1, dict(qs=None)), (-1, dict(lens=None)),
+                    (-1, dict(table=None)), (-1, dict(tokens=-1)), (-1, dict(seqs=-1)), (-1, dict(mq=-1)), (-1, dict(ml=-1)), (-1, dict(qh=3)),
+                    (-1, dict(qh=0)), (-1, dict(qh=1)), (-1, dict(ldq=240)), (-1, dict(ldo=240)), (-1, dict(ldt=3)), (-1, dict(w=AT, ldw=99)),
+                    (-4, dict(ml=196609, ldt=10000)), (-4, dict(seqs=65536)), (-4, dict(mq=1 << 24)), (-4, dict(tokens=1 << 31)),
+                    (-4, dict(qh=65536, ldq=65536 * 64, ldo=65536 * 64)), (-2, dict(Q=AT + 8)), (-2, dict(O=2 * AT + 1)), (-2, dict(ldq=264)),
+                    (-2, dict(ldo=257)), (-2, dict(qs=AT + 2)), (-2, dict(lens=AT + 1)), (-2, dict(table=AT + 3)), (-2, dict(w=AT + 4, ldw=100)),
+                    (-3, dict(qk=chan)), (-3, dict(pv=chan)), (-3, dict(qk=bad)), (-3, dict(pv=bad)), (-3, dict(p=b.CExp(0, 15, 45, 8))),
+                    (-3, dict(p=b.CExp(17, 25, 45, 8))), (-3, dict(p=b.CExp(17, -1, 45, 8))), (-3, dict(p=b.CExp(17, 15, 44, 8))),
+                    (-3, dict(p=b.CExp(1, 13, 45, 8))), (-3, dict(p=b.CExp(1, 24, 45, 8))), (-3, dict(p=b.CExp(32768, 9, 45, 8))),
+                    (-3, dict(p=b.CExp(32769, 1, 45, 8)))):
+        assert attend(b, **k) == code, k
+    for k in (dict(tokens=0, Q=None, O=None), dict(seqs=0, lens=None, table=None, qs=None), dict(mq=0)):
+        assert attend(b, **k) == 0, k
+
+
+def evict(b, c=None, **k):
+    v = dict(ctx=C.addressof(CTX), w=AT, ldw=100, lens=AT, table=AT, ldt=4, dst=2 * AT, ldd=2, wo=2 * AT, ldwo=64, kept=AT, new=AT, seqs=1, ml=100,
+             keep=50, sinks=4, recent=20)
+    v.update(k)
+    return b.load_library().ivit_kv4_evict(v["ctx"], C.byref(c or cache(b)), v["w"], v["ldw"], v["lens"], v["table"], v["ldt"], v["dst"], v["ldd"],
+                                           v["wo"], v["ldwo"], v["kept"], v["new"], v["seqs"], v["ml"], v["keep"], v["sinks"], v["recent"])
+
+
+def test_evict_refusals(lib):
+    b = lib
+    for code, k in BAD_CACHES:
+        assert evict(b, cache(b, **k)) == code, k
+    for code, k in ((-1, dict(ctx=None)), *((-1, {n: None}) for n in ("w", "lens", "table", "dst", "wo", "kept", "new")), (-1, dict(seqs=-1)),
+                    (-1, dict(ml=-1)), (-1, dict(keep=0)), (-1, dict(sinks=-1)), (-1, dict(recent=-1)), (-1, dict(sinks=31)), (-1, dict(sinks=51, recent=0)),
+                    (-1, dict(recent=47)), (-1, dict(recent=2 ** 63 - 1)), (-1, dict(ldw=99)), (-1, dict(ldwo=49)), (-1, dict(ldt=3)), (-1, dict(ldd=1)),
+                    (-1, dict(dst=AT)), (-1, dict(wo=AT)), (-4, dict(seqs=65536)), (-4, dict(ml=1 << 31, ldw=1 << 31, ldt=1 << 30)),
+                    (-2, dict(w=AT + 4)), (-2, dict(wo=AT + 4)), (-2, dict(lens=AT + 2)), (-2, dict(table=AT + 2)), (-2, dict(dst=AT + 2)),
+                    (-2, dict(kept=AT + 2)), (-2, dict(new=AT + 2))):
+        assert evict(b, **k) == code, k

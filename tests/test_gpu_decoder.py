@@ -1,0 +1,520 @@
+"""GPU parity of the decoder operators (root-mean-square norm, cache in 4 bits, attention over it, eviction) with their definitions
+in 64-bit integers, bit for bit: everything is integer arithmetic, so no difference is allowed anywhere."""
+import numpy as np
+import pytest
+import torch
+
+from ivit_inputs import ExpParams, Scale
+from ivit_inputs.gen import dyadic, scale_channels
+from oracle import api as O
+from oracle import decoder as D
+
+pytestmark = pytest.mark.gpu
+
+
+def _g():
+    import gpu_util
+    return gpu_util
+
+
+def rand_i8(rng, shape, std=32):
+    return np.clip(np.rint(rng.standard_normal(shape) * std), -128, 127).astype(np.int8)
+
+
+def cuda(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# ---- root-mean-square norm ----
+
+def norm_case(rng, rows, C, x32, h32, kind):
+    """x, res, x ratio: ordinary, zeros in some rows, or the extremes of the types."""
+    x = rng.standard_normal((rows, C)) * (20000 if x32 else 32)
+    res = rng.standard_normal((rows, C)) * (3000 if h32 else 20)
+    x, res = np.rint(x), np.rint(res)
+    if kind == "extreme":
+        x = rng.choice([-2.0 ** 31, 2.0 ** 31 - 1, 0, 1, -1] if x32 else [-128, 127, 0, -1], (rows, C))
+        res = rng.choice([-2.0 ** 31, 2.0 ** 31 - 1, 2.0 ** 20, -2.0 ** 20, 0] if h32 else [-128, 127, 0], (rows, C))
+    elif kind == "sparse":
+        keep = rng.random((rows, C)) < 1.5 / C
+        x, res = np.where(keep, x, 0), np.where(keep, res, 0)
+        x[0], res[0] = 0, 0
+    x = x.astype(np.int32) if x32 else np.clip(x, -128, 127).astype(np.int8)
+    return x, res.astype(np.int32) if h32 else np.clip(res, -128, 127).astype(np.int8)
+
+
+@pytest.mark.parametrize("kind", ["ordinary", "sparse", "extreme"])
+@pytest.mark.parametrize("x32,h32", [(0, None), (1, None), (0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("rows,C", [(1, 4), (1, 768), (3, 772), (130, 64), (197, 192), (700, 132), (40, 1000), (64, 4096), (2000, 2048), (9, 16384),
+                                    (400, 5000)])
+def test_rmsnorm_parity(rows, C, x32, h32, kind):
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(rows * 31 + C + 7 * x32 + 3 * (h32 or 0) + len(kind))
+    x, res = norm_case(rng, rows, C, x32, h32 or 0, kind)
+    xs = scale_channels(rng.uniform(0.5, 1.5, C) * ((500.0 if h32 else 10.0) / (20000.0 if x32 else 1100.0)))
+    rs = Scale(*dyadic(0.96875))
+    for dynamic, M_ln, ratio in ((False, 20, 32.0 * np.sqrt(C) / 2 ** 20), (True, 22, 0.4), (True, 8, 0.9)):
+        gs = scale_channels(rng.uniform(0.8, 1.1, C) * min(ratio, 0.9))
+        want, top, total = D.rmsnorm(x, (gs.mult, gs.shift), M_ln, (xs.mult, xs.shift), None if h32 is None else res, (rs.mult, rs.shift), h32 == 1,
+                                     dynamic)
+        dx, dr = g.dev(x), None if h32 is None else g.dev(res)
+        sums = None if h32 is None else g.dev(np.zeros_like(res))
+        rm = torch.zeros(rows, dtype=torch.int32, device="cuda") if dynamic else None
+        got = c.rmsnorm(dx, g.binding.DevScale(gs, "cuda"), x_scale=g.binding.DevScale(xs, "cuda"), res=dr,
+                        res_scale=None if h32 is None else g.binding.DevScale(rs, "cuda"), M_ln=M_ln, sum_out=sums, row_max=rm)
+        what = f"M_ln {M_ln} dynamic {dynamic}"
+        g.assert_equal(g.host(got), want.astype(np.int8), what)
+        if dynamic:
+            g.assert_equal(g.host(rm), top.astype(np.int32), what + " row_max")
+        if h32 is not None:
+            g.assert_equal(g.host(sums), total.astype(sums.cpu().numpy().dtype), what + " sum")
+            # the stream in place, without and with the sum wanted
+            got = c.rmsnorm(dx, g.binding.DevScale(gs, "cuda"), x_scale=g.binding.DevScale(xs, "cuda"), res=dr,
+                            res_scale=g.binding.DevScale(rs, "cuda"), M_ln=M_ln, row_max=rm)
+            g.assert_equal(g.host(got), want.astype(np.int8), what + " no sum")
+            c.rmsnorm(dx, g.binding.DevScale(gs, "cuda"), x_scale=g.binding.DevScale(xs, "cuda"), res=dr,
+                      res_scale=g.binding.DevScale(rs, "cuda"), M_ln=M_ln, sum_out=dr, row_max=rm, out=got)
+            g.assert_equal(g.host(got), want.astype(np.int8), what + " in place")
+            g.assert_equal(g.host(dr), total.astype(res.dtype), what + " stream in place")
+    assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("shift", [31, 32, 33, 39, 40, 41, 54, 55, 61, 62])
+@pytest.mark.parametrize("x32,h32", [(0, 0), (1, 1)])
+def test_rmsnorm_every_shift(shift, x32, h32):
+    """Per-tensor scales, and per-channel ones, over the whole range of shifts, at both ends of the multipliers."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(shift)
+    rows, C = 37, 516
+    x, res = norm_case(rng, rows, C, x32, h32, "extreme")
+    for mult in (1, 2 ** 31 - 1):
+        s = Scale(mult, shift)
+        sc = Scale(np.full(C, mult, np.int32), np.full(C, shift, np.uint8))
+        want, top, total = D.rmsnorm(x, (mult, shift), 21, (mult, shift), res, (mult, shift), h32 == 1, True)
+        for per in (s, sc):
+            sums, rm = g.dev(np.zeros_like(res)), torch.zeros(rows, dtype=torch.int32, device="cuda")
+            got = c.rmsnorm(g.dev(x), g.binding.DevScale(per, "cuda"), x_scale=g.binding.DevScale(per, "cuda"), res=g.dev(res),
+                            res_scale=g.binding.DevScale(s, "cuda"), M_ln=21, sum_out=sums, row_max=rm)
+            g.assert_equal(g.host(got), want.astype(np.int8), f"mult {mult}")
+            g.assert_equal(g.host(rm), top.astype(np.int32), f"mult {mult} row_max")
+            g.assert_equal(g.host(sums), total.astype(res.dtype), f"mult {mult} sum")
+
+
+def test_rmsnorm_leaves_the_rest_alone():
+    """Columns past C of every tensor, and rows past the last, keep what they held."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(3)
+    for rows, C, ld in ((5, 100, 112), (2, 772, 1024), (1, 4, 16), (300, 36, 48)):
+        x, res = norm_case(rng, rows, C, 0, 0, "ordinary")
+        bx = torch.full((rows + 1, ld), 77, dtype=torch.int8, device="cuda")
+        br, bo = bx.clone(), bx.clone()
+        bx[:rows, :C], br[:rows, :C] = cuda(x), cuda(res)
+        s = g.binding.DevScale(Scale(*dyadic(0.01)), "cuda")
+        c.rmsnorm(bx[:rows, :C], s, x_scale=s, res=br[:rows, :C], res_scale=s, sum_out=br[:rows, :C], out=bo[:rows, :C])
+        for t in (bx, br, bo):
+            assert (t[rows:] == 77).all() and (t[:, C:] == 77).all()
+
+
+# ---- cache in 4 bits: append ----
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [32, 64, 128, 256])
+@pytest.mark.parametrize("heads,tokens", [(1, 1), (3, 29), (8, 200), (5, 1500)])
+def test_append_parity(d, page, heads, tokens):
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(d + page + heads + tokens)
+    pages = -(-tokens // page) + 2
+    k, v = rand_i8(rng, (tokens, heads * d)), rand_i8(rng, (tokens, heads * d), 50)
+    k[rng.random(k.shape) < 0.01] = -128
+    k[0, :32], v[-1, :d] = 0, 0                                   # groups of zeros
+    v[0, :d] = np.where(np.arange(d) == 5, 1, 0)
+    qkv = np.concatenate([np.full((tokens, 32), 99, np.int8), k, v], 1)
+    slots = rng.permutation(pages * page)[:tokens].astype(np.int64)
+    if tokens > 10:
+        slots[[3, 7]] = -1, -2 ** 40
+    ref = D.Cache(pages, heads, d, page)
+    before = rng.integers(0, 256, (pages, heads, page * (d + d // 32 + 1))).astype(np.uint8)
+    ref = D.Cache.of_bytes(before, d, page)
+    ref.append(k, v, slots)
+    cache = g.binding.Kv4Cache(cuda(before), d, page)
+    dq = g.dev(qkv)
+    c.kv4_append(cache, dq[:, 32:32 + heads * d], dq[:, 32 + heads * d:32 + 2 * heads * d], cuda(slots))
+    g.assert_equal(g.host(cache.pool), ref.to_bytes(), "pool")
+    assert c.poll_status() == 0
+    # a slot past the pool is left out and reported; a call without tokens does nothing
+    slots[0] = pages * page
+    c.kv4_append(cache, dq[:1, 32:32 + heads * d], dq[:1, 32 + heads * d:32 + 2 * heads * d], cuda(slots[:1]))
+    torch.cuda.synchronize()
+    assert c.poll_status() == -3 and c.poll_status() == 0
+    g.assert_equal(g.host(cache.pool), ref.to_bytes(), "pool after a bad slot")
+    c.kv4_append(cache, dq[:0, 32:32 + heads * d], dq[:0, 32 + heads * d:32 + 2 * heads * d], cuda(slots[:0]))
+
+
+def test_append_every_value():
+    """Every int8 value against every step a group can have."""
+    g, c = _g(), _g().ctx()
+    top = np.repeat(np.arange(129), 256)                          # largest magnitude of the group
+    x = np.tile(np.arange(-128, 128), 129)
+    use = np.abs(x) <= top
+    top, x = top[use], x[use]
+    tokens, d = len(x), 64
+    k, v = np.zeros((tokens, d), np.int64), np.zeros((tokens, d), np.int64)
+    k[:, 0], k[:, 17] = x, -top
+    k[:, 40], k[:, 33] = x, -top
+    v[:, 1], v[:, 63] = x, -top
+    k, v = k.astype(np.int8), v.astype(np.int8)
+    pages = -(-tokens // 256)
+    ref = D.Cache(pages, 1, d, 256)
+    slots = np.arange(tokens, dtype=np.int64)
+    ref.append(k, v, slots)
+    cache = g.binding.Kv4Cache.empty(pages, 1, d, 256, "cuda")
+    cache.pool.fill_(0x88)
+    cache.pool.view(pages, -1)[:, :] = cuda(D.Cache(pages, 1, d, 256).to_bytes()).view(pages, -1)
+    c.kv4_append(cache, cuda(k), cuda(v), cuda(slots))
+    g.assert_equal(g.host(cache.pool), ref.to_bytes(), "pool")
+
+
+# ---- attention over it ----
+
+def filled(rng, pages, heads, d, page, std=24):
+    ref = D.Cache(pages, heads, d, page)
+    ref.ks = rng.integers(0, 148, ref.ks.shape) // rng.integers(1, 9, ref.ks.shape)
+    ref.vs = rng.integers(0, 148, ref.vs.shape) // rng.integers(1, 9, ref.vs.shape)
+    ref.kc, ref.vc = rng.integers(-7, 8, ref.kc.shape), rng.integers(-7, 8, ref.vc.shape)
+    return ref
+
+
+def attend(c, g, ref, q, heads_q, tq, lens, table, max_q=None, max_len=None, qk=None, pv=None, I0=17, N=15, weights=False, ldw=None, out=None):
+    d, page, hk = ref.d, ref.page, ref.kc.shape[1]
+    cache = g.binding.Kv4Cache(cuda(ref.to_bytes()), d, page)
+    qs = np.concatenate([[0], np.cumsum(tq)]).astype(np.int32)
+    qk = qk or dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40))
+    pv = pv or dyadic(1 / 128)
+    max_q = max(list(tq) + [0]) if max_q is None else max_q
+    max_len = max(list(lens) + [0]) if max_len is None else max_len
+    w0 = np.arange(len(lens) * hk * (ldw or table.shape[1] * page), dtype=np.int64).reshape(len(lens), hk, -1) if weights else None
+    if out is None:
+        out = np.full(q.shape, 55, np.int8)
+    dout, dw = cuda(out), None if w0 is None else cuda(w0)
+    c.kv4_attention(cache, cuda(q), cuda(qs), cuda(np.asarray(lens, np.int32)), cuda(np.asarray(table, np.int32)), g.binding.DevScale.of(*qk),
+                    ExpParams(I0, N), g.binding.DevScale.of(*pv), max_q, max_len, out=dout, weights=dw)
+    want, ww = D.attention(ref, q, heads_q, qs, lens, table, qk, I0, N, pv, out, w0)
+    g.assert_equal(g.host(dout), want.astype(np.int8), "out")
+    if weights:
+        g.assert_equal(g.host(dw), ww, "weights")
+    return g.host(dout)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [32, 64, 256])
+@pytest.mark.parametrize("hq,hk", [(1, 1), (6, 6), (8, 4), (9, 3), (4, 1), (14, 2), (16, 2), (17, 1), (40, 2)])
+def test_attention_decode(d, page, hq, hk):
+    """One query token for each of sequences of 0, 1, ... keys; rows of no sequence stay; with and without weights."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(d + page + 17 * hq + hk)
+    lens = [0, 1, 2, 31, 32, 33, 63, 64, 65, page - 1, page, page + 1, 300, 511, 700]
+    B, np_ = len(lens), -(-max(lens) // page)
+    ref = filled(rng, B * np_ + 3, hk, d, page)
+    table = rng.permutation(B * np_ + 3)[:B * np_].reshape(B, np_)
+    q = rand_i8(rng, (B + 3, hq * d))                              # three rows behind the last sequence
+    for w in (False, True):
+        got = attend(c, g, ref, q, hq, [1] * B, lens, table, weights=w)
+        assert (got[B:] == 55).all()
+    assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("d,page,hq,hk", [(64, 32, 4, 4), (128, 64, 8, 2), (128, 32, 7, 1), (64, 128, 16, 1), (128, 256, 3, 3)])
+def test_attention_query_rows(d, page, hq, hk):
+    """Several query tokens per sequence: causal; fewer keys than queries, so that the first rows see nothing; no queries at all."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(d + page + hq)
+    tq = [5, 0, 1, 33, 70, 9, 2, 17]
+    lens = [5, 40, 1, 20, 70, 333, 0, 160]
+    np_ = -(-max(lens) // page)
+    ref = filled(rng, len(lens) * np_, hk, d, page)
+    table = rng.permutation(len(lens) * np_).reshape(len(lens), np_)
+    q = rand_i8(rng, (sum(tq), hq * d))
+    attend(c, g, ref, q, hq, tq, lens, table)
+    attend(c, g, ref, q, hq, tq, lens, table, weights=True)
+    # the same launch sized for more than there is
+    attend(c, g, ref, q, hq, tq, lens, table, max_q=90, max_len=np_ * page, weights=True, ldw=np_ * page + 5)
+    assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("I0,N", [(17, 15), (1, 14), (1, 23), (255, 15), (16384, 0), (32767, 9), (3, 22), (100, 8)])
+def test_attention_exponentials(I0, N):
+    """The corners of ShiftExp's constants, scores that saturate, equal scores, steps of zero."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(I0 + N)
+    d, page, hk, hq = 128, 32, 2, 4
+    lens = [257, 90, 1]
+    ref = filled(rng, 3 * 9, hk, d, page)
+    ref.ks[::5], ref.vs[::7] = 147, 147
+    ref.kc[::3], ref.vc[::5] = 7, -7
+    table = np.arange(27).reshape(3, 9)
+    q = rng.choice([-128, 127, 0, 3], (3, hq * d)).astype(np.int8)
+    for ratio in (2.0 ** -30, 2e-5, 1e-3, 0.99):
+        attend(c, g, ref, q, hq, [1, 1, 1], lens, table, qk=dyadic(ratio), pv=dyadic(0.9), I0=I0, N=N, weights=True)
+    ref.vs[:], ref.ks[:] = 0, 0
+    attend(c, g, ref, q, hq, [1, 1, 1], lens, table, I0=I0, N=N, weights=True)
+
+
+@pytest.mark.parametrize("d,page,hq,hk,L", [(64, 32, 1, 1, 3000), (128, 64, 4, 1, 9001), (128, 256, 16, 1, 20000), (64, 128, 8, 1, 40001), (128, 128, 17, 1, 5003)])
+def test_attention_long_rows(d, page, hq, hk, L):
+    """Rows long enough to be split, every key of equal weight at the end of the range of a code: the largest sums."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(L)
+    np_ = -(-L // page)
+    ref = filled(rng, np_, hk, d, page)
+    table = rng.permutation(np_)[None]
+    q = rand_i8(rng, (2, hq * d))
+    attend(c, g, ref, q, hq, [2], [L], table, weights=True)
+    ref.vc[:], ref.vs[:], ref.ks[:] = 7, 147, 0
+    attend(c, g, ref, q, hq, [2], [L], table, weights=True, pv=dyadic(1 / 400))
+
+
+def test_attention_longest():
+    """The longest sequence that the entry point takes."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(11)
+    L, page = 196608, 256
+    ref = filled(rng, L // page, 1, 64, page)
+    ref.vc[:], ref.vs[:] = 7, 147
+    attend(c, g, ref, rand_i8(rng, (1, 64 * 5)), 5, [1], [L], np.arange(L // page)[None], weights=True)
+    assert c.poll_status() == 0
+
+
+def test_attention_far_pages():
+    """Pages more than 2^32 bytes into the pool."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(12)
+    d, page, hk = 128, 256, 4
+    block = page * (d + d // 32 + 1)
+    pages = (5 << 30) // (hk * block)
+    small = filled(rng, 6, hk, d, page)
+    pool = torch.zeros((pages, hk, block), dtype=torch.uint8, device="cuda")
+    at = [pages - 1, 0, pages - 3, pages // 2, pages - 2, pages // 2 + 7]
+    pool[at] = cuda(small.to_bytes())
+    cache = g.binding.Kv4Cache(pool, d, page)
+    q = rand_i8(rng, (2, 8 * d))
+    table, lens, qs = np.arange(6).reshape(2, 3), [700, 768], np.array([0, 1, 2])
+    out = torch.zeros((2, 8 * d), dtype=torch.int8, device="cuda")
+    qk, pv = dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40)), dyadic(1 / 128)
+    far = cuda(np.array(at, np.int32)[table])
+    c.kv4_attention(cache, cuda(q), cuda(qs.astype(np.int32)), cuda(np.array(lens, np.int32)), far, g.binding.DevScale.of(*qk), ExpParams(17, 15),
+                    g.binding.DevScale.of(*pv), 1, 768, out=out)
+    want, _ = D.attention(small, q, 8, qs, lens, table, qk, 17, 15, pv, np.zeros_like(q))
+    g.assert_equal(g.host(out), want.astype(np.int8), "out")
+    # a row appended there, and eviction that moves rows there
+    k, v = rand_i8(rng, (1, hk * d)), rand_i8(rng, (1, hk * d))
+    small.append(k, v, [2 * page + 200])
+    c.kv4_append(cache, cuda(k), cuda(v), cuda(np.array([at[2] * page + 200])))
+    w = rng.integers(0, 1 << 40, (2, hk, 768))
+    kept, new = c.kv4_evict(cache, cuda(w), cuda(np.array(lens, np.int32)), far, 300, 4, 32, 768, weights_out=torch.empty((2, hk, 300), dtype=torch.int64, device="cuda"))
+    wk, wn, _, bytes_ = D.evict(small, w, lens, table, table, 300, 300, 4, 32)
+    g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+    g.assert_equal(g.host(pool[at]), bytes_, "pool")
+
+
+def test_attention_indices_that_point_nowhere():
+    """Pages outside the pool are not read: their keys are not seen, and the call says so.  The same for lengths past max_len,
+    more queries than max_q, and rows past the end of Q."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(5)
+    d, page, hk, hq = 64, 32, 2, 4
+    lens, tq = [100, 64, 70], [1, 3, 1]
+    ref = filled(rng, 12, hk, d, page)
+    table = np.arange(12).reshape(3, 4)
+    table[0, 1], table[1, 0], table[1, 1], table[2, 3] = 12, -1, 2 ** 31 - 1, -7        # (the last one holds no key)
+    q = rand_i8(rng, (5, hq * d))
+    attend(c, g, ref, q, hq, tq, lens, table, weights=True)
+    torch.cuda.synchronize()
+    assert c.poll_status() == -3 and c.poll_status() == 0
+    table = np.arange(12).reshape(3, 4)
+    cache = g.binding.Kv4Cache(cuda(ref.to_bytes()), d, page)
+
+    def call(qs, lens, max_q, max_len):
+        out = torch.full((5, hq * d), 55, dtype=torch.int8, device="cuda")
+        c.kv4_attention(cache, cuda(q), cuda(np.array(qs, np.int32)), cuda(np.array(lens, np.int32)), cuda(table.astype(np.int32)),
+                        g.binding.DevScale.of(*dyadic(1e-4)), ExpParams(17, 15), g.binding.DevScale.of(*dyadic(1 / 128)), max_q, max_len, out=out)
+        torch.cuda.synchronize()
+        return g.host(out)
+
+    good = call([0, 1, 4, 5], [100, 64, 70], 3, 128)
+    assert c.poll_status() == 0
+    for qs, lens, max_q, max_len, same in (([0, 1, 4, 5], [100, 64, 2 ** 31 - 1], 3, 128, slice(0, 4)), ([0, 1, 4, 5], [-3, 64, 70], 3, 128, slice(1, 5)),
+                                           ([0, 1, 4, 5], [100, 64, 70], 2, 128, slice(0, 1)), ([0, 1, 4, 2 ** 30], [100, 64, 70], 3, 128, slice(0, 4)),
+                                           ([-5, 1, 4, 5], [100, 64, 70], 3, 128, slice(1, 5)), ([0, 1, 4, -2 ** 31], [100, 64, 70], 3, 128, slice(0, 4))):
+        got = call(qs, lens, max_q, max_len)
+        assert c.poll_status() == -3, (qs, lens)
+        assert np.array_equal(got[same], good[same]), (qs, lens)
+
+
+# ---- eviction ----
+
+@pytest.mark.parametrize("d,page,hk", [(64, 32, 1), (128, 64, 3), (64, 256, 5), (128, 128, 2)])
+@pytest.mark.parametrize("keep,sinks,recent", [(1, 0, 0), (1, 1, 0), (40, 4, 16), (100, 0, 100), (33, 33, 0), (255, 1, 3), (600, 4, 64)])
+def test_evict_parity(d, page, hk, keep, sinks, recent):
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(d + page + keep)
+    lens = [0, 1, keep - 1, keep, keep + 1, 300, 1029, 2500]
+    B, ps, pd = len(lens), -(-2500 // page), -(-keep // page)
+    w = rng.integers(0, 50, (B, hk, 2500)) << rng.integers(0, 45, (B, hk, 2500))
+    w[5], w[6, :, ::2] = 7, 2 ** 62                                 # all equal; half of them equal at the top
+    for in_place in (False, True):
+        ref = filled(rng, B * (ps + pd), hk, d, page)
+        order = rng.permutation(B * (ps + pd))
+        table, dst = order[:B * ps].reshape(B, ps).astype(np.int32), order[B * ps:].reshape(B, pd).astype(np.int32)
+        cache = g.binding.Kv4Cache(cuda(ref.to_bytes()), d, page)
+        dw, dl, dt = cuda(w), cuda(np.array(lens, np.int32)), cuda(table)
+        if in_place:
+            kept, new = c.kv4_evict(cache, dw, dl, dt, keep, sinks, recent, 2500, new_lens=dl)
+            wo = dw
+        else:
+            wo = torch.full((B, hk, pd * page + 3), -5, dtype=torch.int64, device="cuda")
+            kept, new = c.kv4_evict(cache, dw, dl, dt, keep, sinks, recent, 2500, dst_table=cuda(dst), weights_out=wo)
+        wk, wn, ww, pool = D.evict(ref, w, lens, table, table if in_place else dst, wo.shape[2], keep, sinks, recent)
+        g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+        g.assert_equal(g.host(new), wn.astype(np.int32), "new lens")
+        g.assert_equal(g.host(wo), ww, "weights")
+        g.assert_equal(g.host(cache.pool), pool, "pool")
+        assert c.poll_status() == 0
+
+
+def test_evict_any_weights():
+    """Negative weights and the ends of int64 order like any others."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(8)
+    L, keep = 1500, 700
+    w = rng.choice([-2 ** 63, 2 ** 63 - 1, -1, 0, 1, 255, 256, -256, 2 ** 40], (2, 2, L))
+    ref = filled(rng, 2 * 12, 2, 64, 128)
+    table = np.arange(24).reshape(2, 12).astype(np.int32)
+    cache, dw = g.binding.Kv4Cache(cuda(ref.to_bytes()), 64, 128), cuda(w)
+    kept, _ = c.kv4_evict(cache, dw, cuda(np.array([L, L - 1], np.int32)), cuda(table), keep, 2, 9, L)
+    wk, _, ww, pool = D.evict(ref, w, [L, L - 1], table, table, L, keep, 2, 9)
+    g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+    g.assert_equal(g.host(dw), ww, "weights")
+    g.assert_equal(g.host(cache.pool), pool, "pool")
+
+
+def test_evict_long():
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(9)
+    L, keep, page = 70001, 30011, 256
+    np_ = -(-L // page)
+    w = (rng.standard_exponential((1, 2, L)) ** 4 * 1e6).astype(np.int64)
+    for in_place in (True, False):
+        ref = filled(rng, 2 * np_, 2, 64, page)
+        table, dst = np.arange(np_, dtype=np.int32)[None], np.arange(np_, 2 * np_, dtype=np.int32)[None]
+        cache, dw = g.binding.Kv4Cache(cuda(ref.to_bytes()), 64, page), cuda(w)
+        wo = dw if in_place else torch.empty_like(dw)
+        to = table if in_place else dst
+        kept, _ = c.kv4_evict(cache, dw, cuda(np.array([L], np.int32)), cuda(table), keep, 4, 500, L, dst_table=None if in_place else cuda(dst), weights_out=wo)
+        wk, _, ww, pool = D.evict(ref, w, [L], table, to, L, keep, 4, 500)
+        g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+        g.assert_equal(g.host(wo), ww, "weights")
+        g.assert_equal(g.host(cache.pool), pool, "pool")
+
+
+def test_evict_reports_lengths_and_pages():
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(10)
+    ref = filled(rng, 8, 2, 64, 32)
+    w = rng.integers(0, 1000, (2, 2, 128))
+    table = np.arange(8).reshape(2, 4).astype(np.int32)
+    bad = table.copy()
+    bad[1, 2] = 8
+    for lens, t in (([200, 100], table), ([100, -4], table), ([100, 128], bad)):
+        cache = g.binding.Kv4Cache(cuda(ref.to_bytes()), 64, 32)
+        kept, new = c.kv4_evict(cache, cuda(w), cuda(np.array(lens, np.int32)), cuda(t), 50, 1, 1, 128)
+        torch.cuda.synchronize()
+        assert c.poll_status() == -3
+        assert g.host(new).tolist() == [min(50, max(0, min(n, 128))) for n in lens]
+
+
+# ---- as they are used ----
+
+def test_a_decoder_step_and_a_graph_of_it():
+    """Prompt, then tokens one by one: norm, QKV Dense, append, attention, output Dense, norm; then eviction and one more token.
+    Each operator's reference takes the same bytes as its kernel; the token step is then captured and replayed with the same result."""
+    g = _g()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = g.binding.Context(0, stream)
+        rng = np.random.default_rng(21)
+        d, hq, hk, page, pages, steps, prompt = 64, 6, 2, 32, 8, 6, 70
+        Dm = hq * d
+        wqkv, wo = rand_i8(rng, ((hq + 2 * hk) * d, Dm), 33), rand_i8(rng, (Dm, Dm), 33)
+        acc = np.sqrt(Dm) * 32 * 33
+        s_qkv, s_o = scale_channels(rng.uniform(25, 35, len(wqkv)) / acc), scale_channels(rng.uniform(8, 12, Dm) / acc)
+        gamma = scale_channels(rng.uniform(28, 36, Dm) * np.sqrt(Dm) / 2 ** 20)
+        unit, rs = Scale(*dyadic(0.5)), Scale(*dyadic(0.9))
+        qk, pv = dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40)), dyadic(1 / 128)
+        B = g.binding
+        D_ = {n: B.DevScale(s, "cuda") for n, s in dict(qkv=s_qkv, o=s_o, gamma=gamma, unit=unit, rs=rs).items()}
+        dqk, dpv, dwqkv, dwo = B.DevScale.of(*qk), B.DevScale.of(*pv), cuda(wqkv), cuda(wo)
+        cache = B.Kv4Cache.empty(pages, hk, d, page, "cuda")
+        cache.pool.copy_(cuda(D.Cache(pages, hk, d, page).to_bytes()))
+        ref = D.Cache(pages, hk, d, page)
+        table = np.array([[3, 0, 7, 2, 5]])
+        dtable = cuda(table.astype(np.int32))
+        weights = torch.zeros((1, hk, 160), dtype=torch.int64, device="cuda")
+        w_ref = np.zeros((1, hk, 160), np.int64)
+
+        def gpu(x, stream_in, slots, qs, lens):
+            a = c.rmsnorm(x, D_["gamma"], x_scale=D_["unit"], res=stream_in, res_scale=D_["rs"], sum_out=stream_in)
+            qkv = c.linear(a, dwqkv, None, D_["qkv"])
+            c.kv4_append(cache, qkv[:, Dm:Dm + hk * d], qkv[:, Dm + hk * d:], slots)
+            o = c.kv4_attention(cache, qkv[:, :Dm], qs, lens, dtable, dqk, ExpParams(17, 15), dpv, x.shape[0], 160, weights=weights)
+            return c.linear(o, dwo, None, D_["o"], res=stream_in, res_scale=D_["rs"])
+
+        def cpu(x, stream_in, slots, n, length):
+            a, _, h = D.rmsnorm(x, (gamma.mult, gamma.shift), 20, (unit.mult, unit.shift), stream_in, (rs.mult, rs.shift))
+            qkv = O.linear(a.astype(np.int8), wqkv, None, s_qkv)
+            ref.append(qkv[:, Dm:Dm + hk * d], qkv[:, Dm + hk * d:], slots)
+            nonlocal w_ref
+            o, w_ref = D.attention(ref, qkv[:, :Dm], hq, [0, n], [length], table, qk, 17, 15, pv, np.zeros((n, Dm)), w_ref)
+            return O.linear(o.astype(np.int8), wo, None, s_o, res=h.astype(np.int8), res_scale=rs), h
+
+        def slots_of(j):
+            return table[0][j // page] * page + j % page
+
+        length = 0
+        for step in range(steps):
+            n = prompt if step == 0 else 1
+            x, h = rand_i8(rng, (n, Dm)), rand_i8(rng, (n, Dm), 20)
+            slots = slots_of(np.arange(length, length + n)).astype(np.int64)
+            length += n
+            dh = cuda(h)
+            got = gpu(cuda(x), dh, cuda(slots), cuda(np.array([0, n], np.int32)), cuda(np.array([length], np.int32)))
+            want, hh = cpu(x, h, slots, n, length)
+            stream.synchronize()
+            g.assert_equal(g.host(dh), hh.astype(np.int8), f"stream, step {step}")
+            g.assert_equal(g.host(cache.pool), ref.to_bytes(), f"pool, step {step}")
+            g.assert_equal(g.host(got), want, f"step {step}")
+            g.assert_equal(g.host(weights), w_ref, f"weights, step {step}")
+        kept, new = c.kv4_evict(cache, weights, cuda(np.array([length], np.int32)), dtable, 40, 4, 16, 160)
+        wk, wn, w_ref, _ = D.evict(ref, w_ref, [length], table, table, 160, 40, 4, 16)
+        g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+        g.assert_equal(g.host(cache.pool), ref.to_bytes(), "pool behind eviction")
+        length = int(g.host(new)[0])
+        # one more token, twice: launched, and as a graph that is replayed on new inputs
+        bx, bh, bs = cuda(rand_i8(rng, (1, Dm))), cuda(rand_i8(rng, (1, Dm), 20)), cuda(slots_of(np.array([length])).astype(np.int64))
+        bq, bl = cuda(np.array([0, 1], np.int32)), cuda(np.array([length + 1], np.int32))
+        graph = torch.cuda.CUDAGraph()
+        stream.synchronize()
+        with torch.cuda.graph(graph, stream=stream):
+            out = gpu(bx, bh, bs, bq, bl)
+        for i in range(3):
+            x, h = rand_i8(rng, (1, Dm)), rand_i8(rng, (1, Dm), 20)
+            slots = slots_of(np.array([length])).astype(np.int64)
+            length += 1
+            for t, a in ((bx, x), (bh, h), (bs, slots), (bl, np.array([length], np.int32))):
+                t.copy_(cuda(a))
+            graph.replay()
+            stream.synchronize()
+            want, _ = cpu(x, h, slots, 1, length)
+            g.assert_equal(g.host(out), want, f"replay {i}")
+            g.assert_equal(g.host(weights), w_ref, f"weights, replay {i}")
+        assert c.poll_status() == 0
+        c.close()
