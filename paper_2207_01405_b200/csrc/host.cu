@@ -1143,7 +1143,7 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t*
   if (q_heads < cache->heads || q_heads % cache->heads) return IVIT_ERR_INVALID_ARG;
   if (ldq < q_heads * cache->d || ldo < q_heads * cache->d || ldtable < (max_len + cache->page - 1) / cache->page || (weights && ldw < max_len))
     return IVIT_ERR_INVALID_ARG;
-  if (max_len > IVIT_KV4_MAX_LEN || seqs > 65535 || q_heads > 65535 || max_q > 0xffffff || tokens > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  if (max_len > IVIT_KV4_MAX_LEN || seqs > 65535 || q_heads > 65535 || max_q > 0xffffff || max_q * (q_heads / cache->heads) > 0x7fffff00ll || tokens > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
   if (!aligned16(Q) || !aligned16(O) || ldq % 16 || ldo % 16 || !aligned4(q_start) || !aligned4(lens) || !aligned4(table) ||
       (reinterpret_cast<uintptr_t>(weights) & 7))
     return IVIT_ERR_ALIGNMENT;

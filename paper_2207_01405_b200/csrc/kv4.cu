@@ -1,4 +1,4 @@
-// A key/value cache held in 4 bits: append, attention over it, eviction from it (sm_100a).  Layout: ivit_kv4_cache in ivit.h.
+// A key/value cache held in 4 bits: append to it, eviction from it (sm_100a).  Layout: ivit_kv4_cache in ivit.h.
 #include "common.cuh"
 
 namespace ivit {
@@ -82,130 +82,6 @@ int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* 
   const int64_t ctas = (tokens * cache->heads + 7) / 8;
   launch_k(kv4_append_kernel, (int)(ctas < 8 * ctx->sm_count ? ctas : 8 * ctx->sm_count), 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv,
            slots, tokens, ctx->status_dev);
-  return ls.done();
-}
-
-// ---------------------------------------------------------------- attention
-
-struct AttendArgs {
-  Cache c;
-  const int8_t* Q; int64_t ldq;
-  int group;                       // query heads per key/value head
-  int64_t tokens;
-  const int32_t *q_start, *lens, *table;
-  int64_t ldtable;
-  int qk_mult, qk_shift, pv_mult, pv_shift, I0, N, z;
-  int8_t* O; int64_t ldo;
-  int64_t* weights; int64_t ldw;
-  int max_q, max_len;
-  int* status;
-};
-
-// One CTA per query row of one head; the row's scores wait in shared memory between the passes.
-__global__ void __launch_bounds__(256) kv4_attention_kernel(AttendArgs a) {
-  extern __shared__ int8_t score[];
-  __shared__ int8_t q[128];
-  __shared__ int top_s[8];
-  __shared__ unsigned long long den_s[8];
-  __shared__ long long num_s[256];
-  pdl_wait();
-  pdl_trigger();
-  const int t = blockIdx.x, hq = blockIdx.y, b = blockIdx.z, h = hq / a.group, d = a.c.d;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int64_t q0 = a.q_start[b], q1 = a.q_start[b + 1];
-  int len = a.lens[b];
-  if (tid == 0 && t == 0 && hq == 0 && (q0 < 0 || q1 < q0 || q1 > a.tokens || q1 - q0 > a.max_q || len < 0 || len > a.max_len)) report(a.status, IVIT_ERR_RANGE);
-  const int64_t row = q0 + t;
-  if (row >= q1 || row < 0 || row >= a.tokens) return;
-  const int n = (int)(q1 - q0);
-  int seen = len - n + t + 1;
-  seen = max(0, min(seen, a.max_len));
-  if (tid < d) q[tid] = a.Q[row * a.ldq + (int64_t)hq * d + tid];
-  __syncthreads();
-  auto block = [&](int j) {
-    const int64_t pg = a.table[b * a.ldtable + (j >> a.c.page_log)];
-    if (pg < 0 || pg >= a.c.pages) { report(a.status, IVIT_ERR_RANGE); return Block{nullptr, 0, 0}; }
-    return a.c.block(pg, h);
-  };
-  int top = -1000;
-  for (int j = tid; j < seen; j += 256) {
-    const Block blk = block(j);
-    if (!blk.p) continue;
-    const int o = j & (a.c.page - 1);
-    const uint8_t* kc = blk.kcode(o);
-    int acc = 0;
-    for (int g = 0; g < d / 32; ++g) {
-      int dot = 0;
-      for (int p = 0; p < 16; ++p) {
-        const int byte = kc[4 * (d / 32 * (p >> 2) + g) + (p & 3)];
-        dot += q[32 * g + p] * ((byte & 15) - 8) + q[32 * g + 16 + p] * ((byte >> 4) - 8);
-      }
-      acc += dot * blk.kstep(o)[g];
-    }
-    const int s = sat8(rq(acc, a.qk_mult, a.qk_shift));
-    score[j] = (int8_t)s;
-    top = max(top, s);
-  }
-  top = __reduce_max_sync(~0u, top);
-  if (lane == 0) top_s[warp] = top;
-  __syncthreads();
-  for (int i = 0; i < 8; ++i) top = max(top, top_s[i]);
-  // den; thread = (channel, half of the keys)
-  unsigned long long den = 0;
-  for (int j = tid; j < seen; j += 256)
-    if (block(j).p) den += shiftexp(score[j] - top, a.I0, a.N);
-  for (int o = 16; o; o >>= 1) den += __shfl_xor_sync(~0u, den, o);
-  if (lane == 0) den_s[warp] = den;
-  __syncthreads();
-  den = 0;
-  for (int i = 0; i < 8; ++i) den += den_s[i];
-  const int ch = tid & (d - 1), part = tid / d, parts = 256 / d;
-  long long num = 0;
-  for (int j = part; j < seen; j += parts) {
-    const Block blk = block(j);
-    if (!blk.p) continue;
-    const int o = j & (a.c.page - 1);
-    const unsigned e = shiftexp(score[j] - top, a.I0, a.N);
-    const unsigned u = (e * *blk.vstep(o) + (1u << (a.z - 1))) >> a.z;
-    const int byte = blk.vcode(o)[ch & (d / 2 - 1)];
-    num += (long long)u * ((ch < d / 2 ? byte & 15 : byte >> 4) - 8);
-  }
-  num_s[tid] = num;
-  __syncthreads();
-  if (tid < d) {
-    num = 0;
-    for (int i = 0; i < parts; ++i) num += num_s[i * d + tid];
-    long long tq = 0;
-    if (den) {
-      const long long w = num * (1ll << (a.z + 5)), dd = (long long)den;
-      tq = w / dd;
-      if (w % dd < 0) --tq;
-    }
-    a.O[row * a.ldo + (int64_t)hq * d + tid] = (int8_t)sat8(rq((int)tq, a.pv_mult, a.pv_shift));
-  }
-  if (a.weights && den)
-    for (int j = tid; j < seen; j += 256)
-      if (block(j).p) {
-        const unsigned long long w = ((unsigned long long)shiftexp(score[j] - top, a.I0, a.N) << 24) / den;
-        if (w) atomicAdd(reinterpret_cast<unsigned long long*>(a.weights) + ((int64_t)b * a.c.heads + h) * a.ldw + j, w);
-      }
-}
-
-int kv4_prepare_device() {
-  return cudaFuncSetAttribute(kv4_attention_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) == cudaSuccess ? IVIT_OK : IVIT_ERR_CUDA;
-}
-
-int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
-                         const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable, ivit_scale qk_scale,
-                         ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo, int64_t* weights, int64_t ldw, int64_t seqs,
-                         int64_t max_q, int64_t max_len) {
-  const int64_t top = (int64_t)smax.I0 << smax.N;
-  int bits = 0;
-  while (top >> bits) ++bits;
-  const AttendArgs a{to_dev(cache), Q, ldq, (int)(q_heads / cache->heads), tokens, q_start, lens, table, ldtable, qk_scale.mult, qk_scale.shift,
-                     pv_scale.mult, pv_scale.shift, smax.I0, smax.N, bits - 8, O, ldo, weights, ldw, (int)max_q, (int)max_len, ctx->status_dev};
-  LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * seqs * q_heads * max_q * max_len * cache->d);
-  launch_k(kv4_attention_kernel, dim3((unsigned)max_q, (unsigned)q_heads, (unsigned)seqs), 256, (size_t)max_len, ctx->stream, a);
   return ls.done();
 }
 

@@ -1,0 +1,593 @@
+// Attention of query rows over a key/value cache held in 4 bits (ivit_kv4_attention), sm_100a.
+#include "common.cuh"
+#include "kv4_layout.cuh"
+
+namespace ivit {
+
+struct AttendArgs {
+  const uint8_t* data;
+  int64_t pages, block_bytes;
+  int heads, page, page_log;
+  const int8_t* Q; int64_t ldq;
+  int group;                       // query heads per key/value head
+  int64_t tokens;
+  const int32_t *q_start, *lens, *table;
+  int64_t ldtable;
+  int qk_mult, qk_add, qk_sh;      // s = (hi32(16 a qk_mult) + qk_add) >> qk_sh
+  int pv_mult, pv_shift, I0, N, z;
+  int8_t* O; int64_t ldo;
+  int64_t* weights; int64_t ldw;
+  int max_q, max_len, split, blocks, tiles;
+  int* status;
+};
+
+// ---------------------------------------------------------------- instructions
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_addr(uint32_t a, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ int peer_i32(uint32_t a) {
+  int v;
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ int4 peer_i128(uint32_t a) {
+  int4 v;
+  asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ unsigned long long peer_u64(uint32_t a) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a));
+  return v;
+}
+
+// D += A B on 16 x 32 by 32 x 8 bytes; A signed, B signed or unsigned.
+template <bool kUnsignedB>
+__device__ __forceinline__ void mma8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if (kUnsignedB)
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Sixteen times the codes of the low (high) halves of four bytes, as signed bytes: code + 8 with its top bit flipped is the code in
+// two's complement, and a nibble in the upper half of a byte needs no sign extension.
+__device__ __forceinline__ uint32_t low16(uint32_t w) { return ((w << 4) ^ 0x80808080u) & 0xf0f0f0f0u; }
+__device__ __forceinline__ uint32_t high16(uint32_t w) { return (w ^ 0x80808080u) & 0xf0f0f0f0u; }
+
+// Four 32-bit values saturated to int8 and packed, x0 in the low byte.
+__device__ __forceinline__ uint32_t pack_sat(int x0, int x1, int x2, int x3) {
+  uint32_t t, r;
+  asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(t) : "r"(x3), "r"(x2), "r"(0));
+  asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(x1), "r"(x0), "r"(t));
+  return r;
+}
+
+// y_i = byte i of x0, x1, x2, x3.
+__device__ __forceinline__ void transpose4(const uint32_t (&x)[4], uint32_t (&y)[4]) {
+  const uint32_t a = __byte_perm(x[0], x[1], 0x5140), b = __byte_perm(x[2], x[3], 0x5140);
+  const uint32_t c = __byte_perm(x[0], x[1], 0x7362), d = __byte_perm(x[2], x[3], 0x7362);
+  y[0] = __byte_perm(a, b, 0x5410);
+  y[1] = __byte_perm(a, b, 0x7632);
+  y[2] = __byte_perm(c, d, 0x5410);
+  y[3] = __byte_perm(c, d, 0x7632);
+}
+
+// Entry of the exponentials for the score in one byte of w: `sel` holds -4 kKv4Copies in that byte, t = table + copy + 4 kKv4Copies max.
+__device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t) {
+  unsigned e;
+  asm volatile("{\n\t.reg .u32 a;\n\tdp4a.s32.s32 a, %1, %2, %3;\n\tld.shared.u32 %0, [a];\n\t}" : "=r"(e) : "r"(w), "r"(sel), "r"(t));
+  return e;
+}
+
+// floor(w / den) for |w| < 2^16 den, den > 0: both are cut to a divisor of at most 32 bits, whose quotient is off by at most one (the cut
+// moves it by less than 2^16 2^-31), and multiplied back.  r = floor((2^64 - 1) / (den >> cut)).
+__device__ __forceinline__ int small_quotient(long long w, unsigned long long den, int cut, unsigned long long r) {
+  const unsigned long long a = w < 0 ? 0ull - (unsigned long long)w : (unsigned long long)w;
+  unsigned long long q = __umul64hi(a >> cut, r);
+  long long left = (long long)(a - q * den);
+  while (left < 0) { --q; left += (long long)den; }
+  while (left >= (long long)den) { ++q; left -= (long long)den; }
+  return w < 0 ? -(int)q - (left != 0) : (int)q;
+}
+
+// ---------------------------------------------------------------- the kernel
+//
+// A cluster of `split` CTAs takes up to 8 RN query rows (of one sequence, all of them readers of one key/value head) and shares the
+// keys out in runs of blocks of 32; the eight warps of a CTA take its blocks in turn.  Two passes, because ShiftExp needs the row's
+// maximum before the first weight (its floors do not commute with a change of the maximum, so nothing can be corrected afterwards):
+//   scores:  S^T = K Q^T on m16n8k32 products, keys along M, the query rows along N (a decoder has 1 to 16 of them: none is padding of 16).
+//            One product of 32 channels is one group of a key, whose step multiplies it in 32 bits; the int8 scores stay in shared memory.
+//   values:  O^T = V^T U, channels along M, the weights u (16 bits) as two planes of unsigned bytes.
+// A warp brings its codes in with cp.async, kKv4Stages blocks ahead (the first blocks of V are under way across the exchange of the
+// maxima), and unpacks them in registers: three instructions for eight codes of K, and a transpose of bytes more for V, whose products
+// run along the keys.  Maxima, sums and outputs of the cluster's CTAs meet in distributed shared memory: one launch, no workspace, and
+// integer sums, so that the order changes nothing.
+template <int D, int RN, bool kWeights>
+__global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(const AttendArgs a) {
+  constexpr int kG = D / 32;               // groups of a key
+  constexpr int kLaneWords = D / 32;       // words of a K row that a lane takes
+  constexpr int kVWords = D / 64;          // words of a V row that a lane takes
+  constexpr int kMu = D / 16;              // tiles of 16 channels
+  constexpr int kRows = 8 * RN, kStage = kKv4Block * (D / 2 + D / 32);
+  extern __shared__ __align__(128) uint8_t sm[];
+  pdl_wait();
+  pdl_trigger();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n8 = lane >> 2, t4 = lane & 3;
+  const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split, h = blockIdx.y, b = blockIdx.z;
+  const Kv4Seq seq = kv4_sequence(a.q_start[b], a.q_start[b + 1], a.lens[b], a.tokens, a.max_q, a.max_len);
+  if (seq.bad && tid == 0) *(volatile int*)a.status = IVIT_ERR_RANGE;
+  const int row0 = tile * kRows, nrows = min(kRows, seq.n * a.group - row0);
+  if (nrows <= 0) return;                  // (the whole cluster)
+  const Kv4Smem at = kv4_smem(D, kRows, a.page, a.blocks);
+  int* const pages = reinterpret_cast<int*>(sm + at.pages);
+  int* const small = reinterpret_cast<int*>(sm + at.small);
+  int* const lim = small;                                                            // [16]
+  int* const cta_top = small + 16;                                                   // [16]
+  int* const top = small + 32;                                                       // [16]
+  int* const warp_top = small + 48;                                                  // [8][16]
+  unsigned long long* const cta_den = reinterpret_cast<unsigned long long*>(small + 176);   // [16]
+  unsigned long long* const warp_den = cta_den + 16;                                 // [8][16]
+  const int score_ld = kv4_score_ld(a.blocks);
+  int8_t* const score = reinterpret_cast<int8_t*>(sm + at.score);
+
+  // keys that some row of the tile sees, and this CTA's run of them
+  const int seen_all = kv4_seen(seq, (row0 + nrows - 1) / a.group), seen_min = kv4_seen(seq, row0 / a.group);
+  const int blk0 = rank * a.blocks, nblk = max(0, min(a.blocks, (seen_all + kKv4Block - 1) / kKv4Block - blk0));
+  const int page0 = blk0 * kKv4Block >> a.page_log;
+  for (int i = tid; i < (nblk > 0 ? ((blk0 + nblk) * kKv4Block - 1 >> a.page_log) - page0 + 1 : 0); i += 256) {
+    int pg = a.table[b * a.ldtable + page0 + i];
+    if (pg < 0 || pg >= a.pages) {
+      pg = -1;
+      *(volatile int*)a.status = IVIT_ERR_RANGE;
+    }
+    pages[i] = pg;
+  }
+  if (tid < kRows) lim[tid] = tid < nrows ? kv4_seen(seq, (row0 + tid) / a.group) : 0;
+  {  // the exponentials, shifted so that a weight's 16 bits are the upper half of its product with a step
+    const unsigned e = shiftexp(-tid, a.I0, a.N) << (16 - a.z);
+    uint4* dst = reinterpret_cast<uint4*>(sm + at.table) + tid * (kKv4Copies / 4);
+    static_assert(kKv4Copies % 4 == 0, "whole vectors");
+#pragma unroll
+    for (int i = 0; i < kKv4Copies / 4; ++i) dst[i] = make_uint4(e, e, e, e);
+  }
+  // B operand of the scores: the lane's query row of each tile of eight, bytes 32 g + 4 t.. and 32 g + 16 + 4 t..
+  uint32_t q[RN][kG][2];
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    const int r = row0 + 8 * j + n8;
+    const bool there = 8 * j + n8 < nrows;
+    const int8_t* src = a.Q + (seq.q0 + (there ? r / a.group : 0)) * a.ldq + (int64_t)(h * a.group + (there ? r % a.group : 0)) * D + 4 * t4;
+#pragma unroll
+    for (int g = 0; g < kG; ++g) {
+      q[j][g][0] = there ? *reinterpret_cast<const uint32_t*>(src + 32 * g) : 0;
+      q[j][g][1] = there ? *reinterpret_cast<const uint32_t*>(src + 32 * g + 16) : 0;
+    }
+  }
+  __syncthreads();
+
+  uint8_t* const ring = sm + at.ring + warp * (kKv4Stages * kStage);
+  // Requests a block's codes (at `code`) and steps (at `step` of the block of its page); the chunks of 16 bytes of a row are
+  // exchanged (1 with 3, 0 with 2) in rows 2, 3 modulo 4, which spreads the lanes' reads of V over all banks.
+  auto request = [&](int lb, int stage, int code, int step, int step_bytes) {
+    if (lb < nblk) {
+      const int key = (blk0 + lb) * kKv4Block, pg = pages[(key >> a.page_log) - page0], o = key & (a.page - 1);
+      if (pg >= 0) {
+        const uint8_t* src = a.data + ((int64_t)pg * a.heads + h) * a.block_bytes;
+        const uint32_t dst = smem_u32(ring + stage * kStage);
+#pragma unroll
+        for (int i = 0; i < D / 64 * 2; ++i) {
+          const int c = lane + 32 * i;                       // chunk of the block's codes
+          const int row = c / (D / 32), swap = D == 128 ? (row & 2) : 0;
+          cp16(dst + 16 * (c ^ swap), src + code + o * (D / 2) + 16 * c);
+        }
+        if (lane < step_bytes / 16) cp16(dst + kKv4Block * (D / 2) + 16 * lane, src + step + o * (step_bytes / kKv4Block) + 16 * lane);
+      }
+    }
+    cp_commit();
+  };
+  const int kstep = kv4_kstep(D, a.page, 0), vcode = kv4_vcode(D, a.page, 0), vstep = kv4_vstep(D, a.page, 0);
+  auto request_k = [&](int lb, int stage) { request(lb, stage, 0, kstep, kKv4Block * kG); };
+  auto request_v = [&](int lb, int stage) { request(lb, stage, vcode, vstep, kKv4Block); };
+
+  // ---- scores
+#pragma unroll
+  for (int s = 0; s < kKv4Stages - 1; ++s) request_k(warp + 8 * s, s);
+  int best[RN][2];
+#pragma unroll
+  for (int j = 0; j < RN; ++j) best[j][0] = best[j][1] = -128;
+  int stage = 0;
+  for (int lb = warp; lb < nblk; lb += 8) {
+    cp_wait<kKv4Stages - 2>();
+    __syncwarp();
+    request_k(lb + 8 * (kKv4Stages - 1), (stage + kKv4Stages - 1) % kKv4Stages);
+    const uint8_t* buf = ring + stage * kStage;
+    stage = (stage + 1) % kKv4Stages;
+    const int key0 = (blk0 + lb) * kKv4Block;
+    if (pages[(key0 >> a.page_log) - page0] < 0) continue;
+    int acc[RN][2][4];
+#pragma unroll
+    for (int m = 0; m < 2; ++m) {
+      uint32_t w[2][kLaneWords], st[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int row = 16 * m + 8 * k + n8;
+        if (D == 128) {
+          const uint4 v = *reinterpret_cast<const uint4*>(buf + row * 64 + 16 * (t4 ^ (row & 2)));
+          w[k][0] = v.x; w[k][1] = v.y; w[k][kLaneWords - 2] = v.z; w[k][kLaneWords - 1] = v.w;
+          st[k] = *reinterpret_cast<const uint32_t*>(buf + kKv4Block * 64 + 4 * row);
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(buf + row * 32 + 8 * t4);
+          w[k][0] = v.x; w[k][1] = v.y;
+          st[k] = *reinterpret_cast<const uint16_t*>(buf + kKv4Block * 32 + 2 * row);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < RN; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[j][m][i] = 0;
+#pragma unroll
+      for (int g = 0; g < kG; ++g) {
+        const uint32_t a0 = low16(w[0][g]), a1 = low16(w[1][g]), a2 = high16(w[0][g]), a3 = high16(w[1][g]);
+        const int s0 = (st[0] >> (8 * g)) & 255, s1 = (st[1] >> (8 * g)) & 255;
+#pragma unroll
+        for (int j = 0; j < RN; ++j) {
+          int c[4] = {0, 0, 0, 0};
+          mma8<false>(c, a0, a1, a2, a3, q[j][g][0], q[j][g][1]);
+          acc[j][m][0] += c[0] * s0;
+          acc[j][m][1] += c[1] * s0;
+          acc[j][m][2] += c[2] * s1;
+          acc[j][m][3] += c[3] * s1;
+        }
+      }
+    }
+    const bool whole = key0 + kKv4Block <= seen_min;
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        int v[4];   // keys n8, n8 + 8, n8 + 16, n8 + 24 of row 2 t4 + e
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (__mulhi(acc[j][i >> 1][2 * (i & 1) + e], a.qk_mult) + a.qk_add) >> a.qk_sh;
+        const int row = 8 * j + 2 * t4 + e;
+        if (!whole) {   // what the row does not see: a score that is no larger than any, and whose weight is left out below
+          const int left = lim[row] - key0 - n8;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = 8 * i < left ? v[i] : -128;
+        }
+        best[j][e] = max(max(best[j][e], max(v[0], v[1])), max(v[2], v[3]));
+        *reinterpret_cast<uint32_t*>(score + row * score_ld + lb * kKv4Block + 4 * n8) = pack_sat(v[0], v[1], v[2], v[3]);
+      }
+  }
+  cp_wait<0>();
+  __syncwarp();
+#pragma unroll
+  for (int s = 0; s < kKv4Stages - 1; ++s) request_v(warp + 8 * s, s);
+#pragma unroll
+  for (int j = 0; j < RN; ++j)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      int v = min(best[j][e], 127);
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
+      if (lane < 4) warp_top[warp * 16 + 8 * j + 2 * lane + e] = v;
+    }
+  __syncthreads();
+  if (tid < kRows) {
+    int v = -128;
+#pragma unroll
+    for (int i = 0; i < kKv4Warps; ++i) v = max(v, warp_top[i * 16 + tid]);
+    cta_top[tid] = v;
+    if (a.split == 1) top[tid] = v;
+  }
+  if (a.split > 1) {
+    cluster_sync();
+    if (tid < kRows) {
+      int v = -128;
+      for (int i = 0; i < a.split; ++i) v = max(v, peer_i32(peer_addr(smem_u32(cta_top + tid), i)));
+      top[tid] = v;
+    }
+  }
+  __syncthreads();
+
+  // ---- values
+  int lo[RN][kMu][4], hi[RN][kMu][4];
+  unsigned long long den[RN];
+  uint32_t tab[RN];
+  const uint32_t tab0 = smem_u32(sm + at.table) + 4 * (lane & (kKv4Copies - 1));
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    den[j] = 0;
+    tab[j] = tab0 + (uint32_t)(4 * kKv4Copies * top[8 * j + n8]);
+#pragma unroll
+    for (int m = 0; m < kMu; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lo[j][m][i] = hi[j][m][i] = 0;
+  }
+  constexpr uint32_t kSel = (uint32_t)(-4 * kKv4Copies) & 255u;
+  stage = 0;
+  for (int lb = warp; lb < nblk; lb += 8) {
+    cp_wait<kKv4Stages - 2>();
+    __syncwarp();
+    request_v(lb + 8 * (kKv4Stages - 1), (stage + kKv4Stages - 1) % kKv4Stages);
+    const uint8_t* buf = ring + stage * kStage;
+    stage = (stage + 1) % kKv4Stages;
+    const int key0 = (blk0 + lb) * kKv4Block;
+    if (pages[(key0 >> a.page_log) - page0] < 0) continue;
+    // steps of the lane's keys t, t + 4, ..., t + 28
+    uint32_t vs[8];
+    {
+      const uint4 s0 = *reinterpret_cast<const uint4*>(buf + kKv4Block * (D / 2)), s1 = *reinterpret_cast<const uint4*>(buf + kKv4Block * (D / 2) + 16);
+      const uint32_t w[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vs[i] = __byte_perm(w[i], 0, 0x4440 | t4);
+    }
+    uint32_t bl[RN][2], bh[RN][2];   // B operands: word 0 holds keys t + 8 i, word 1 keys t + 4 + 8 i
+    const bool whole = key0 + kKv4Block <= seen_min;
+#pragma unroll
+    for (int j = 0; j < RN; ++j) {
+      unsigned sum = 0;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t s = *reinterpret_cast<const uint32_t*>(score + (8 * j + n8) * score_ld + lb * kKv4Block + 4 * (t4 + 4 * k));
+        unsigned e[4], p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = exp_of(s, kSel << (8 * i), tab[j]);
+        if (!whole) {
+          const int left = lim[8 * j + n8] - key0 - t4 - 4 * k;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] = 8 * i < left ? e[i] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sum += e[i];
+          p[i] = e[i] * vs[2 * i + k] + 0x8000u;
+        }
+        const uint32_t p01 = __byte_perm(p[0], p[1], 0x7362), p23 = __byte_perm(p[2], p[3], 0x7362);
+        bl[j][k] = __byte_perm(p01, p23, 0x5410);
+        bh[j][k] = __byte_perm(p01, p23, 0x7632);
+      }
+      den[j] += sum;
+    }
+    uint32_t x[kVWords][2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = t4 + 4 * k + 8 * i;
+        if (D == 128) {
+          const uint2 v = *reinterpret_cast<const uint2*>(buf + row * 64 + ((8 * n8) ^ ((row & 2) << 4)));
+          x[0][k][i] = v.x;
+          x[kVWords - 1][k][i] = v.y;
+        } else {
+          x[0][k][i] = *reinterpret_cast<const uint32_t*>(buf + row * 32 + 4 * n8);
+        }
+      }
+#pragma unroll
+    for (int w = 0; w < kVWords; ++w) {
+      uint32_t y[2][4];
+      transpose4(x[w][0], y[0]);
+      transpose4(x[w][1], y[1]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t a0 = low16(y[0][i]), a1 = high16(y[0][i]), a2 = low16(y[1][i]), a3 = high16(y[1][i]);
+#pragma unroll
+        for (int j = 0; j < RN; ++j) {
+          mma8<true>(lo[j][4 * w + i], a0, a1, a2, a3, bl[j][0], bl[j][1]);
+          mma8<true>(hi[j][4 * w + i], a0, a1, a2, a3, bh[j][0], bh[j][1]);
+        }
+      }
+    }
+  }
+  cp_wait<0>();
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    unsigned long long v = den[j];
+    v += __shfl_xor_sync(~0u, v, 1);
+    v += __shfl_xor_sync(~0u, v, 2);
+    if (t4 == 0) warp_den[warp * 16 + 8 * j + n8] = v;
+  }
+
+  // ---- the CTA's sums: warp by warp into slabs [plane][row][channel], added up by the thread that has that row and four channels
+  constexpr int kLd = D + 8;
+  int* const slab = reinterpret_cast<int*>(sm + at.ring);
+  constexpr int kThreads = 8 * D / 4;          // threads that hold sums of a tile of eight rows
+  const int my_row = tid / (D / 4), my_ch = tid % (D / 4) * 4;
+  int4 sl[RN], sh[RN];
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    __syncthreads();
+    int* mine = slab + warp * (2 * 8 * kLd);
+    const int p = kMu * n8;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int m = 0; m < kMu; m += 4) {
+        int* dst = mine + (2 * t4 + (e & 1)) * kLd + p + m + (e >> 1) * (D / 2);
+        *reinterpret_cast<int4*>(dst) = make_int4(lo[j][m][e], lo[j][m + 1][e], lo[j][m + 2][e], lo[j][m + 3][e]);
+        *reinterpret_cast<int4*>(dst + 8 * kLd) = make_int4(hi[j][m][e], hi[j][m + 1][e], hi[j][m + 2][e], hi[j][m + 3][e]);
+      }
+    __syncthreads();
+    sl[j] = sh[j] = make_int4(0, 0, 0, 0);
+    if (tid < kThreads)
+#pragma unroll
+      for (int w = 0; w < kKv4Warps; ++w) {
+        const int4 x = *reinterpret_cast<const int4*>(slab + w * (2 * 8 * kLd) + my_row * kLd + my_ch);
+        const int4 y = *reinterpret_cast<const int4*>(slab + w * (2 * 8 * kLd) + (8 + my_row) * kLd + my_ch);
+        sl[j].x += x.x; sl[j].y += x.y; sl[j].z += x.z; sl[j].w += x.w;
+        sh[j].x += y.x; sh[j].y += y.y; sh[j].z += y.z; sh[j].w += y.w;
+      }
+  }
+  if (tid < kRows) {
+    unsigned long long v = 0;
+#pragma unroll
+    for (int i = 0; i < kKv4Warps; ++i) v += warp_den[i * 16 + tid];
+    cta_den[tid] = v;
+  }
+  __syncthreads();
+  if (a.split > 1) {
+#pragma unroll
+    for (int j = 0; j < RN; ++j)
+      if (tid < kThreads) {
+        *reinterpret_cast<int4*>(slab + (8 * j + my_row) * kLd + my_ch) = sl[j];
+        *reinterpret_cast<int4*>(slab + (kRows + 8 * j + my_row) * kLd + my_ch) = sh[j];
+      }
+    cluster_sync();
+  }
+  auto row_den = [&](int row) {
+    unsigned long long v = 0;
+    if (a.split == 1) v = cta_den[row];
+    else
+      for (int i = 0; i < a.split; ++i) v += peer_u64(peer_addr(smem_u32(cta_den + row), i));
+    return v >> (16 - a.z);
+  };
+
+  // ---- outputs: each CTA of the cluster takes its share of the (row, four channels)
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    const int share = kThreads / a.split;     // (split divides it: 128 or 256 by 1 ... 16)
+    int item = tid;
+    if (a.split > 1) item = tid < share ? rank * share + tid : kThreads;
+    const int row = 8 * j + item / (D / 4), ch = item % (D / 4) * 4;
+    if (item < kThreads && row < nrows) {
+      long long num[4];
+      if (a.split == 1) {
+        num[0] = sl[j].x + 256ll * sh[j].x; num[1] = sl[j].y + 256ll * sh[j].y;
+        num[2] = sl[j].z + 256ll * sh[j].z; num[3] = sl[j].w + 256ll * sh[j].w;
+      } else {
+        num[0] = num[1] = num[2] = num[3] = 0;
+        const uint32_t mine = smem_u32(slab + row * kLd + ch);
+        for (int i = 0; i < a.split; ++i) {
+          const uint32_t src = peer_addr(mine, i);
+          const int4 x = peer_i128(src), y = peer_i128(src + kRows * kLd * 4);
+          num[0] += x.x + 256ll * y.x; num[1] += x.y + 256ll * y.y;
+          num[2] += x.z + 256ll * y.z; num[3] += x.w + 256ll * y.w;
+        }
+      }
+      const unsigned long long dn = row_den(row);
+      int out[4] = {0, 0, 0, 0};
+      if (dn) {
+        const int cut = max(0, 32 - __clzll((long long)dn));
+        const unsigned long long r = ~0ull / (dn >> cut);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)   // (the codes came in sixteenfold: 2^(z+5) / 16)
+          out[i] = rq(small_quotient(num[i] * (1ll << (a.z + 1)), dn, cut, r), a.pv_mult, a.pv_shift);
+      }
+      const int qr = row0 + row;
+      *reinterpret_cast<uint32_t*>(a.O + (seq.q0 + qr / a.group) * a.ldo + (int64_t)(h * a.group + qr % a.group) * D + ch) =
+          pack_sat(out[0], out[1], out[2], out[3]);
+    }
+  }
+
+  // ---- accumulated weights: floor(e 2^24 / den) of every difference of scores, row by row, then the sum over the rows of each key
+  if (kWeights) {
+    unsigned* share = reinterpret_cast<unsigned*>(sm + at.ring + 2 * kRows * kLd * 4);
+    for (int i = tid; i < nrows * 256; i += 256) {
+      const unsigned long long dn = row_den(i >> 8);
+      const unsigned e = *reinterpret_cast<const unsigned*>(sm + at.table + (i & 255) * (4 * kKv4Copies)) >> (16 - a.z);
+      share[i] = dn ? (unsigned)(((unsigned long long)e << 24) / dn) : 0;
+    }
+    __syncthreads();
+    unsigned long long* w = reinterpret_cast<unsigned long long*>(a.weights) + ((int64_t)b * a.heads + h) * a.ldw;
+    for (int i = tid; i < nblk * 8; i += 256) {
+      const int key0 = (blk0 + (i >> 3)) * kKv4Block, n = i & 7;
+      if (pages[(key0 >> a.page_log) - page0] < 0) continue;
+      unsigned long long v[4] = {0, 0, 0, 0};
+      for (int row = 0; row < nrows; ++row) {
+        const uint32_t s = *reinterpret_cast<const uint32_t*>(score + row * score_ld + 4 * i);
+        const int left = lim[row] - key0 - n, base = top[row];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (8 * k < left) v[k] += share[row * 256 + base - (int)(int8_t)(s >> (8 * k))];
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (v[k]) atomicAdd(w + key0 + n + 8 * k, v[k]);
+    }
+  }
+  if (a.split > 1) cluster_sync();   // a CTA's sums stay until its peers have read them
+}
+
+template <class F>
+static int each_kernel(F f) {
+  int rc;
+  if ((rc = f(kv4_attention_kernel<64, 1, false>, 64, 1, false)) || (rc = f(kv4_attention_kernel<64, 2, false>, 64, 2, false)) ||
+      (rc = f(kv4_attention_kernel<64, 1, true>, 64, 1, true)) || (rc = f(kv4_attention_kernel<64, 2, true>, 64, 2, true)) ||
+      (rc = f(kv4_attention_kernel<128, 1, false>, 128, 1, false)) || (rc = f(kv4_attention_kernel<128, 2, false>, 128, 2, false)) ||
+      (rc = f(kv4_attention_kernel<128, 1, true>, 128, 1, true)) || (rc = f(kv4_attention_kernel<128, 2, true>, 128, 2, true)))
+    return rc;
+  return IVIT_OK;
+}
+
+int kv4_prepare_device() {
+  return each_kernel([](auto k, int, int, bool) {
+    if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kKv4SmemMax) != cudaSuccess ||
+        cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
+      return (int)IVIT_ERR_CUDA;
+    return (int)IVIT_OK;
+  });
+}
+
+int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
+                         const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable, ivit_scale qk_scale,
+                         ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo, int64_t* weights, int64_t ldw, int64_t seqs,
+                         int64_t max_q, int64_t max_len) {
+  const int d = (int)cache->d, page = (int)cache->page;
+  const int64_t group = q_heads / cache->heads;
+  const Kv4Plan p = kv4_plan(d, page, group, cache->heads, seqs, max_q, max_len, ctx->sm_count);
+  if (p.smem > kKv4SmemMax || (int64_t)p.tiles * p.split > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  AttendArgs a{};
+  a.data = cache->data; a.pages = cache->pages; a.block_bytes = kv4_block_bytes(d, page);
+  a.heads = (int)cache->heads; a.page = page;
+  while ((1 << a.page_log) < page) ++a.page_log;
+  a.Q = Q; a.ldq = ldq; a.group = (int)group; a.tokens = tokens;
+  a.q_start = q_start; a.lens = lens; a.table = table; a.ldtable = ldtable;
+  // rq(x; m, s) = rq(16 x; m, s + 4), whose shift is beyond 32: the rounding constant is a whole number in the product's upper word.  Beyond a
+  // shift of 59 every value rounds to zero (|16 x| < 2^30, m < 2^31).
+  const int s16 = qk_scale.shift + 4;
+  a.qk_mult = s16 <= 63 ? qk_scale.mult : 0;
+  a.qk_add = s16 <= 63 ? 1 << (s16 - 33) : 0;
+  a.qk_sh = s16 <= 63 ? s16 - 32 : 0;
+  a.pv_mult = pv_scale.mult; a.pv_shift = pv_scale.shift; a.I0 = smax.I0; a.N = smax.N;
+  const int64_t top = (int64_t)smax.I0 << smax.N;
+  while (top >> (a.z + 8)) ++a.z;
+  a.O = O; a.ldo = ldo; a.weights = weights; a.ldw = ldw;
+  a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.tiles = p.tiles;
+  a.status = ctx->status_dev;
+  LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * seqs * q_heads * max_q * max_len * d);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.tiles * p.split), (unsigned)cache->heads, (unsigned)seqs);
+  cfg.blockDim = 256;
+  cfg.dynamicSmemBytes = (size_t)p.smem;
+  cfg.stream = ctx->stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)p.split;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = p.split > 1 ? 2 : 1;
+  each_kernel([&](auto k, int kd, int rn, bool w) {
+    if (kd == d && rn * 8 == p.rows && w == (weights != nullptr)) cudaLaunchKernelEx(&cfg, k, a);
+    return (int)IVIT_OK;
+  });
+  return ls.done();
+}
+
+}  // namespace ivit

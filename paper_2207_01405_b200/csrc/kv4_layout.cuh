@@ -1,0 +1,103 @@
+// Sizes and index arithmetic of the 4-bit key/value cache and of the attention over it (plain C++, so that the host can run it too).
+#pragma once
+
+#include <stdint.h>
+
+#ifdef __CUDACC__
+#define IVIT_KV4_FN __host__ __device__ __forceinline__
+#else
+#define IVIT_KV4_FN inline
+#endif
+
+namespace ivit {
+
+// One (page, head) block: K codes [page][d/2], K steps [page][d/32], V codes [page][d/2], V steps [page].
+IVIT_KV4_FN int64_t kv4_block_bytes(int d, int page) { return (int64_t)page * (d + d / 32 + 1); }
+IVIT_KV4_FN int kv4_kcode(int d, int, int o) { return o * (d / 2); }
+IVIT_KV4_FN int kv4_kstep(int d, int page, int o) { return page * (d / 2) + o * (d / 32); }
+IVIT_KV4_FN int kv4_vcode(int d, int page, int o) { return page * (d / 2 + d / 32) + o * (d / 2); }
+IVIT_KV4_FN int kv4_vstep(int d, int page, int o) { return page * (d + d / 32) + o; }
+
+// What the lengths on the device allow a launch that was sized for max_q, max_len and `tokens` rows to touch.
+struct Kv4Seq {
+  int64_t q0;   // first row of Q and O
+  int n;        // query tokens that are handled
+  int nq;       // query tokens that the sequence has (saturated): places the last key
+  int len;      // keys
+  bool bad;
+};
+IVIT_KV4_FN Kv4Seq kv4_sequence(int q0, int q1, int len, int64_t tokens, int64_t max_q, int64_t max_len) {
+  Kv4Seq s;
+  s.bad = len < 0 || len > max_len;
+  s.len = len < 0 ? 0 : (len > max_len ? (int)max_len : len);
+  const int64_t nq = (int64_t)q1 - q0;
+  int64_t n = nq < 0 ? 0 : nq;
+  s.nq = (int)(n > 0x3fffffff ? 0x3fffffff : n);
+  if (q0 < 0 || nq < 0 || nq > max_q || q1 > tokens) s.bad = true;
+  if (n > max_q) n = max_q;
+  if (q0 < 0) n = 0;
+  else if (q0 + n > tokens) n = tokens > q0 ? tokens - q0 : 0;
+  s.q0 = q0;
+  s.n = (int)n;
+  return s;
+}
+// Keys that query t sees: those up to its own, which is key len - nq + t.
+IVIT_KV4_FN int kv4_seen(const Kv4Seq& s, int t) {
+  const int v = s.len - s.nq + t + 1;
+  return v < 0 ? 0 : (v > s.len ? s.len : v);
+}
+
+// ---- launch of the attention ----
+
+constexpr int kKv4Block = 32;      // keys that a warp takes at a time
+constexpr int kKv4Warps = 8;
+constexpr int kKv4Stages = 4;      // blocks that a warp has requested ahead
+constexpr int kKv4Copies = 8;      // copies of the exponentials
+constexpr int kKv4SmemMax = 227 * 1024;
+
+// Bytes of a row of scores in shared memory: 16 modulo 128, so that eight rows at the same keys lie in different banks.
+IVIT_KV4_FN int kv4_score_ld(int blocks) { return (blocks * kKv4Block + 127) / 128 * 128 + 16; }
+IVIT_KV4_FN int kv4_stage_bytes(int d) { return kKv4Block * (d / 2 + d / 32); }
+
+struct Kv4Smem {
+  int table, pages, small, ring, score, total;
+};
+// rows: query rows of a CTA (8 or 16); blocks: blocks of keys of a CTA.
+IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int page, int blocks) {
+  Kv4Smem m;
+  m.table = 0;
+  m.small = m.table + 256 * kKv4Copies * 4;
+  m.pages = m.small + 2048;
+  m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 4 + 127) / 128 * 128;
+  // behind the passes the ring holds the warps' partial sums of eight rows (two planes of 32 bits), then a CTA's and the shares of the weights
+  int ring = kKv4Warps * kKv4Stages * kv4_stage_bytes(d);
+  const int slabs = kKv4Warps * 2 * 8 * (d + 8) * 4, behind = 2 * rows * (d + 8) * 4 + rows * 256 * 4;
+  ring = ring > slabs ? ring : slabs;
+  ring = ring > behind ? ring : behind;
+  m.score = m.ring + ring;
+  m.total = m.score + rows * kv4_score_ld(blocks);
+  return m;
+}
+
+struct Kv4Plan {
+  int rows, split, blocks, tiles, smem;   // query rows of a CTA, CTAs of a cluster along the keys, blocks of each, row tiles, bytes
+};
+inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms) {
+  Kv4Plan p;
+  const int64_t all = (max_len + kKv4Block - 1) / kKv4Block, q_rows = max_q * group;
+  for (p.rows = q_rows <= 8 ? 8 : 16;; p.rows = 8) {
+    p.tiles = (int)((q_rows + p.rows - 1) / p.rows);
+    const int64_t ctas = (int64_t)p.tiles * heads * seqs;
+    p.split = 1;
+    while (p.split < 16 && ctas * p.split < 2 * sms && all > (int64_t)p.split * kKv4Warps) p.split *= 2;
+    for (;; p.split *= 2) {
+      p.blocks = (int)((all + p.split - 1) / p.split);
+      if (p.blocks < 1) p.blocks = 1;
+      p.smem = kv4_smem(d, p.rows, page, p.blocks).total;
+      if (p.smem <= kKv4SmemMax || p.split == 16) break;
+    }
+    if (p.smem <= kKv4SmemMax || p.rows == 8) return p;
+  }
+}
+
+}  // namespace ivit

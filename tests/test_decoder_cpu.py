@@ -124,6 +124,91 @@ def test_row_scalars_on_the_host(tmp_path):
     assert a.value == 0
 
 
+# ---- index arithmetic of the attention, compiled for the host ----
+
+@pytest.fixture(scope="module")
+def layout(tmp_path_factory):
+    src = tmp_path_factory.mktemp("layout") / "t.cpp"
+    src.write_text('#include "kv4_layout.cuh"\nusing namespace ivit;\nextern "C" {\n'
+                   'void plan(int d, int page, int64_t g, int64_t h, int64_t s, int64_t q, int64_t l, int sms, int* o) {\n'
+                   '  Kv4Plan p = kv4_plan(d, page, g, h, s, q, l, sms); Kv4Smem m = kv4_smem(d, p.rows, page, p.blocks);\n'
+                   '  int v[] = {p.rows, p.split, p.blocks, p.tiles, p.smem, m.table, m.small, m.pages, m.ring, m.score, kv4_score_ld(p.blocks)};\n'
+                   '  for (int i = 0; i < 11; ++i) o[i] = v[i]; }\n'
+                   'void seq(int q0, int q1, int len, int64_t tok, int64_t mq, int64_t ml, int64_t* o) {\n'
+                   '  Kv4Seq s = kv4_sequence(q0, q1, len, tok, mq, ml); o[0] = s.q0; o[1] = s.n; o[2] = s.nq; o[3] = s.len; o[4] = s.bad; }\n'
+                   'int seen(int q0, int q1, int len, int64_t tok, int64_t mq, int64_t ml, int t) { return kv4_seen(kv4_sequence(q0, q1, len, tok, mq, ml), t); }\n'
+                   'void places(int d, int page, int o, int64_t* v) { v[0] = kv4_kcode(d, page, o); v[1] = kv4_kstep(d, page, o); v[2] = kv4_vcode(d, page, o);\n'
+                   '  v[3] = kv4_vstep(d, page, o); v[4] = kv4_block_bytes(d, page); }\n}\n')
+    so = src.with_suffix(".so")
+    subprocess.run(["g++", "-O2", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2207_01405_b200", "csrc"), "-o", str(so), str(src)], check=True)
+    L = C.CDLL(str(so))
+    i64 = C.c_int64
+    L.plan.argtypes = [C.c_int, C.c_int, i64, i64, i64, i64, i64, C.c_int, C.POINTER(C.c_int)]
+    L.seq.argtypes = [C.c_int, C.c_int, C.c_int, i64, i64, i64, C.POINTER(i64)]
+    L.seen.argtypes = [C.c_int, C.c_int, C.c_int, i64, i64, i64, C.c_int]
+    L.places.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(i64)]
+    return L
+
+
+def test_every_launch_fits(layout):
+    """The plan of a launch covers every key and query row, and the parts of shared memory follow one another inside the limit."""
+    rng = np.random.default_rng(6)
+    o = (C.c_int * 11)()
+    lens = [0, 1, 31, 32, 33, 256, 257, 1000, 4096, 12288, 12289, 24577, 65536, 100003, 131073, 196607, 196608]
+    for d in (64, 128):
+        for page in (32, 256):
+            for L in lens + rng.integers(1, 196609, 30).tolist():
+                for g, h, s, q in ((1, 1, 1, 1), (4, 8, 1, 1), (8, 8, 64, 1), (9, 2, 3, 1), (16, 1, 1, 1), (17, 1, 1, 1), (4, 8, 5, 300), (1, 65535, 65535, 1),
+                                   (7, 3, 2, 1 << 24)):
+                    layout.plan(d, page, g, h, s, q, L, 148, o)
+                    rows, split, blocks, tiles, smem, table, small, pages, ring, score, ld = list(o)
+                    assert rows in (8, 16) and split in (1, 2, 4, 8, 16) and smem <= 227 * 1024
+                    assert tiles * rows >= q * g > (tiles - 1) * rows
+                    assert split * blocks * 32 >= L and blocks >= 1
+                    assert small - table >= 256 * 8 * 4 and pages - small >= 2048 and ring - pages >= 4 * (blocks * 32 // page + 2)
+                    assert score - ring >= max(8 * 4 * 32 * (d // 2 + d // 32), 8 * 2 * 8 * (d + 8) * 4, 2 * rows * (d + 8) * 4 + rows * 1024)
+                    assert ld >= blocks * 32 and ld % 128 == 16 and smem >= score + rows * ld
+                    assert ring % 128 == 0 and score % 16 == 0 and pages % 16 == 0 and small % 16 == 0
+                    # eight rows, four words each, at the same keys: 32 banks
+                    assert len({(r * ld // 4 + t) % 32 for r in range(8) for t in range(4)}) == 32
+                    assert len({(2 * t * ld // 4 + n) % 32 for t in range(4) for n in range(8)}) == 32
+
+
+def test_what_a_sequence_may_touch(layout):
+    o = (C.c_int64 * 5)()
+    ends = [-2 ** 31, -1, 0, 1, 5, 7, 8, 100, 2 ** 30, 2 ** 31 - 1]
+    for q0 in ends:
+        for q1 in ends:
+            for ln in ends:
+                for tok, mq, ml in ((8, 3, 100), (1, 1, 1), (100, 100, 196608)):
+                    layout.seq(q0, q1, ln, tok, mq, ml, o)
+                    s, n, nq, L, bad = list(o)
+                    assert 0 <= n <= mq and 0 <= L <= ml and (n == 0 or (s >= 0 and s + n <= tok))
+                    assert bool(bad) == (not (0 <= q0 <= q1 <= tok and q1 - q0 <= mq and 0 <= ln <= ml))
+                    if not bad:
+                        assert (n, nq, L, s) == (q1 - q0, q1 - q0, ln, q0)
+                    last = -1
+                    for t in range(min(n, 10)):
+                        seen = layout.seen(q0, q1, ln, tok, mq, ml, t)
+                        assert 0 <= seen <= L and seen >= last
+                        last = seen
+                        if not bad:
+                            assert seen == max(0, ln - (q1 - q0) + t + 1)
+
+
+def test_places_in_a_block(layout):
+    v = (C.c_int64 * 5)()
+    for d in (64, 128):
+        for page in (32, 64, 128, 256):
+            used = np.zeros(page * (d + d // 32 + 1), int)
+            for o in range(page):
+                layout.places(d, page, o, v)
+                for at, n in zip(v, (d // 2, d // 32, d // 2, 1)):
+                    used[at:at + n] += 1
+                assert v[4] == len(used) and v[4] % 16 == 0
+            assert (used == 1).all()
+
+
 # ---- refusals ----
 
 @pytest.fixture(scope="module")
