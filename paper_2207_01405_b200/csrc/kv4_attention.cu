@@ -17,7 +17,7 @@ struct AttendArgs {
   int pv_mult, pv_shift, I0, N, z;
   int8_t* O; int64_t ldo;
   int64_t* weights; int64_t ldw;
-  int max_q, max_len, split, blocks, tiles;
+  int max_q, max_len, split, blocks, kept;
   int* status;
 };
 
@@ -30,9 +30,8 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
-}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_addr(uint32_t a, int rank) {
   uint32_t r;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
@@ -43,22 +42,17 @@ __device__ __forceinline__ int peer_i32(uint32_t a) {
   asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a));
   return v;
 }
-__device__ __forceinline__ int4 peer_i128(uint32_t a) {
-  int4 v;
-  asm volatile("ld.shared::cluster.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
 __device__ __forceinline__ unsigned long long peer_u64(uint32_t a) {
   unsigned long long v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a));
   return v;
 }
 
-// D += A B on 16 x 32 by 32 x 8 bytes; A signed, B signed or unsigned.
-template <bool kUnsignedB>
+// D += A B on 16 x 32 by 32 x 8 bytes; both signed or both unsigned.
+template <bool kUnsigned>
 __device__ __forceinline__ void mma8(int (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if (kUnsignedB)
-    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  if (kUnsigned)
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.u8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+r"(c[0]), "+r"(c[1]), "+r"(c[2]), "+r"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   else
     asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -95,15 +89,18 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
   return e;
 }
 
-// floor(w / den) for |w| < 2^16 den, den > 0: both are cut to a divisor of at most 32 bits, whose quotient is off by at most one (the cut
-// moves it by less than 2^16 2^-31), and multiplied back.  r = floor((2^64 - 1) / (den >> cut)).
+__device__ __forceinline__ int cut_of(unsigned long long den) { return max(0, 32 - __clzll((long long)den)); }
+__device__ __forceinline__ unsigned long long recip_of(unsigned long long den) { return den ? ~0ull / (den >> cut_of(den)) : 0; }
+
+// floor(w / den) for |w| <= 2^24 den, den < 2^43 (0 for den = w = 0): both are cut to a divisor of at most 32 bits, whose quotient is off by at most one (the
+// cut moves it by less than 2^24 2^-31), and multiplied back.  cut = cut_of(den), r = recip_of(den).
 __device__ __forceinline__ int small_quotient(long long w, unsigned long long den, int cut, unsigned long long r) {
   const unsigned long long a = w < 0 ? 0ull - (unsigned long long)w : (unsigned long long)w;
-  unsigned long long q = __umul64hi(a >> cut, r);
-  long long left = (long long)(a - q * den);
-  while (left < 0) { --q; left += (long long)den; }
-  while (left >= (long long)den) { ++q; left -= (long long)den; }
-  return w < 0 ? -(int)q - (left != 0) : (int)q;
+  int q = (int)__umul64hi(a >> cut, r);
+  long long left = (long long)(a - (unsigned long long)(unsigned)q * den);
+  if (left < 0) { --q; left += (long long)den; }
+  if (left >= (long long)den && den) { ++q; left -= (long long)den; }
+  return w < 0 ? -q - (left != 0) : q;
 }
 
 // ---------------------------------------------------------------- the kernel
@@ -126,39 +123,31 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   constexpr int kMu = D / 16;              // tiles of 16 channels
   constexpr int kRows = 8 * RN, kStage = kKv4Block * (D / 2 + D / 32);
   extern __shared__ __align__(128) uint8_t sm[];
-  pdl_wait();
-  pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n8 = lane >> 2, t4 = lane & 3;
   const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split, h = blockIdx.y, b = blockIdx.z;
-  const Kv4Seq seq = kv4_sequence(a.q_start[b], a.q_start[b + 1], a.lens[b], a.tokens, a.max_q, a.max_len);
-  if (seq.bad && tid == 0) *(volatile int*)a.status = IVIT_ERR_RANGE;
-  const int row0 = tile * kRows, nrows = min(kRows, seq.n * a.group - row0);
-  if (nrows <= 0) return;                  // (the whole cluster)
-  const Kv4Smem at = kv4_smem(D, kRows, a.page, a.blocks);
-  int* const pages = reinterpret_cast<int*>(sm + at.pages);
+  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks);
+  const uint8_t** const pages = reinterpret_cast<const uint8_t**>(sm + at.pages);   // this head's block of each page of the run
   int* const small = reinterpret_cast<int*>(sm + at.small);
-  int* const lim = small;                                                            // [16]
-  int* const cta_top = small + 16;                                                   // [16]
-  int* const top = small + 32;                                                       // [16]
-  int* const warp_top = small + 48;                                                  // [8][16]
-  unsigned long long* const cta_den = reinterpret_cast<unsigned long long*>(small + 176);   // [16]
-  unsigned long long* const warp_den = cta_den + 16;                                 // [8][16]
+  int* const lim = small;                                                            // [16] keys that a row sees
+  int* const top = small + 16;                                                       // [16] maxima: of the rows ...
+  int* const cta_top = small + 544;                                                  // [16] ... and of this CTA's part of them
+  int* const warp_top = small + 32;                                                  // [8][16]
+  int* const cta_u = small + 160;                                                    // [2][16] sums of the weights' planes
+  unsigned long long* const row_den = reinterpret_cast<unsigned long long*>(small + 192);   // [16]
+  unsigned long long* const row_u = row_den + 16;                                    // [16]
+  unsigned long long* const row_recip = row_u + 16;                                  // [16]
+  unsigned long long* const warp_den = row_recip + 16;                               // [8][16]
+  unsigned long long* const row_out = reinterpret_cast<unsigned long long*>(small + 560);   // [16] where a row of O starts
+  unsigned long long* const cta_den = row_out + 16;                                  // [16]
+  static_assert(4 * 560 + 8 * 32 <= kKv4Small && 4 * 192 + 8 * (3 * 16 + kKv4Warps * 16) <= 4 * 544, "room for the rows' numbers");
+  int* const sums = reinterpret_cast<int*>(sm + at.sums);                            // [plane][row][half of the channels][channel of a lane][lane]
+  long long* const fin = reinterpret_cast<long long*>(sm + at.fin);                  // [256] parts of the cluster's sums
   const int score_ld = kv4_score_ld(a.blocks);
   int8_t* const score = reinterpret_cast<int8_t*>(sm + at.score);
-
-  // keys that some row of the tile sees, and this CTA's run of them
-  const int seen_all = kv4_seen(seq, (row0 + nrows - 1) / a.group), seen_min = kv4_seen(seq, row0 / a.group);
-  const int blk0 = rank * a.blocks, nblk = max(0, min(a.blocks, (seen_all + kKv4Block - 1) / kKv4Block - blk0));
-  const int page0 = blk0 * kKv4Block >> a.page_log;
-  for (int i = tid; i < (nblk > 0 ? ((blk0 + nblk) * kKv4Block - 1 >> a.page_log) - page0 + 1 : 0); i += 256) {
-    int pg = a.table[b * a.ldtable + page0 + i];
-    if (pg < 0 || pg >= a.pages) {
-      pg = -1;
-      *(volatile int*)a.status = IVIT_ERR_RANGE;
-    }
-    pages[i] = pg;
-  }
-  if (tid < kRows) lim[tid] = tid < nrows ? kv4_seen(seq, (row0 + tid) / a.group) : 0;
+  constexpr int kLd = D + 4;
+  // what needs nothing that a kernel in front may still be writing
+  for (int i = tid; i < 2 * kRows * kLd / 4; i += 256) reinterpret_cast<int4*>(sums)[i] = make_int4(0, 0, 0, 0);
+  if (tid < 32) cta_u[tid] = 0;
   {  // the exponentials, shifted so that a weight's 16 bits are the upper half of its product with a step
     const unsigned e = shiftexp(-tid, a.I0, a.N) << (16 - a.z);
     uint4* dst = reinterpret_cast<uint4*>(sm + at.table) + tid * (kKv4Copies / 4);
@@ -166,75 +155,113 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
     for (int i = 0; i < kKv4Copies / 4; ++i) dst[i] = make_uint4(e, e, e, e);
   }
+  const int row0 = tile * kRows;
+  int q_at[RN], q_head[RN];                            // query token and head (of the group's) of the lane's rows
+#pragma unroll
+  for (int j = 0; j < RN; ++j) {
+    q_at[j] = (row0 + 8 * j + n8) / a.group;
+    q_head[j] = row0 + 8 * j + n8 - q_at[j] * a.group;
+  }
+  pdl_wait();
+  pdl_trigger();
+  const Kv4Seq seq = kv4_sequence(a.q_start[b], a.q_start[b + 1], a.lens[b], a.tokens, a.max_q, a.max_len);
+  if (seq.bad && tid == 0) *(volatile int*)a.status = IVIT_ERR_RANGE;
+  const int nrows = min(kRows, seq.n * a.group - row0);
+  if (nrows <= 0) return;                  // (the whole cluster)
+  // keys that some row of the tile sees, and this CTA's run of them
+  const int seen_all = kv4_seen(seq, (row0 + nrows - 1) / a.group), seen_min = kv4_seen(seq, row0 / a.group);
+  const int blks = (seen_all + kKv4Block - 1) / kKv4Block, run = (blks + a.split - 1) / a.split;
+  const int blk0 = rank * run, nblk = max(0, min(run, blks - blk0));
+  const int page0 = blk0 * kKv4Block >> a.page_log;
+  bool bad = false;
+  for (int i = tid; i < (nblk > 0 ? ((blk0 + nblk) * kKv4Block - 1 >> a.page_log) - page0 + 1 : 0); i += 256) {
+    const int pg = a.table[b * a.ldtable + page0 + i];
+    const bool there = pg >= 0 && pg < a.pages;
+    if (!there) {
+      bad = true;
+      *(volatile int*)a.status = IVIT_ERR_RANGE;
+    }
+    pages[i] = there ? a.data + ((int64_t)pg * a.heads + h) * a.block_bytes : nullptr;
+  }
+  if (t4 == 0 && warp == 0)
+#pragma unroll
+    for (int j = 0; j < RN; ++j) {
+      lim[8 * j + n8] = 8 * j + n8 < nrows ? kv4_seen(seq, q_at[j]) : 0;
+      row_out[8 * j + n8] = (unsigned long long)((seq.q0 + q_at[j]) * a.ldo + (int64_t)(h * a.group + q_head[j]) * D);
+    }
   // B operand of the scores: the lane's query row of each tile of eight, bytes 32 g + 4 t.. and 32 g + 16 + 4 t..
   uint32_t q[RN][kG][2];
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
-    const int r = row0 + 8 * j + n8;
     const bool there = 8 * j + n8 < nrows;
-    const int8_t* src = a.Q + (seq.q0 + (there ? r / a.group : 0)) * a.ldq + (int64_t)(h * a.group + (there ? r % a.group : 0)) * D + 4 * t4;
+    const int8_t* src = a.Q + (there ? (seq.q0 + q_at[j]) * a.ldq + (int64_t)(h * a.group + q_head[j]) * D : 0) + 4 * t4;
 #pragma unroll
     for (int g = 0; g < kG; ++g) {
       q[j][g][0] = there ? *reinterpret_cast<const uint32_t*>(src + 32 * g) : 0;
       q[j][g][1] = there ? *reinterpret_cast<const uint32_t*>(src + 32 * g + 16) : 0;
     }
   }
-  __syncthreads();
+  const bool holes = __syncthreads_or(bad) != 0;   // a page of the run points nowhere: its keys are not seen
 
   uint8_t* const ring = sm + at.ring + warp * (kKv4Stages * kStage);
   // Requests a block's codes (at `code`) and steps (at `step` of the block of its page); the chunks of 16 bytes of a row are
   // exchanged (1 with 3, 0 with 2) in rows 2, 3 modulo 4, which spreads the lanes' reads of V over all banks.
-  auto request = [&](int lb, int stage, int code, int step, int step_bytes) {
+  const uint32_t put = smem_u32(ring) + 16 * (D == 128 ? lane ^ (lane >> 2 & 2) : lane), put_step = smem_u32(ring) + kKv4Block * (D / 2) + 16 * lane;
+  const int in_page = a.page / kKv4Block - 1, per_page = a.page_log - 5;
+  // page and place in it of the run's block lb: pages[(lb + first) >> per_page], (lb + first) & in_page
+  const int first = blk0 & in_page;
+  auto request = [&](int lb, uint32_t stage, int code, int step, int step_bytes) {
     if (lb < nblk) {
-      const int key = (blk0 + lb) * kKv4Block, pg = pages[(key >> a.page_log) - page0], o = key & (a.page - 1);
-      if (pg >= 0) {
-        const uint8_t* src = a.data + ((int64_t)pg * a.heads + h) * a.block_bytes;
-        const uint32_t dst = smem_u32(ring + stage * kStage);
+      const uint8_t* src = pages[(lb + first) >> per_page];
+      const int o = (lb + first) & in_page;
+      if (!holes || src) {
+        const uint8_t* from = src + (code + o * (kKv4Block * D / 2) + 16 * lane);
 #pragma unroll
-        for (int i = 0; i < D / 64 * 2; ++i) {
-          const int c = lane + 32 * i;                       // chunk of the block's codes
-          const int row = c / (D / 32), swap = D == 128 ? (row & 2) : 0;
-          cp16(dst + 16 * (c ^ swap), src + code + o * (D / 2) + 16 * c);
-        }
-        if (lane < step_bytes / 16) cp16(dst + kKv4Block * (D / 2) + 16 * lane, src + step + o * (step_bytes / kKv4Block) + 16 * lane);
+        for (int i = 0; i < D / 64 * 2; ++i) cp16(put + stage + 512 * i, from + 512 * i);
+        if (lane < step_bytes / 16) cp16(put_step + stage, src + (step + o * step_bytes + 16 * lane));
       }
     }
     cp_commit();
   };
   const int kstep = kv4_kstep(D, a.page, 0), vcode = kv4_vcode(D, a.page, 0), vstep = kv4_vstep(D, a.page, 0);
-  auto request_k = [&](int lb, int stage) { request(lb, stage, 0, kstep, kKv4Block * kG); };
-  auto request_v = [&](int lb, int stage) { request(lb, stage, vcode, vstep, kKv4Block); };
+  auto request_k = [&](int lb, uint32_t stage) { request(lb, stage, 0, kstep, kKv4Block * kG); };
+  auto request_v = [&](int lb, uint32_t stage) { request(lb, stage, vcode, vstep, kKv4Block); };
+
+  // the lane's place in a row of K, in K's steps, and in a row of V
+  const int k_at = D == 128 ? n8 * 64 + 16 * (t4 ^ (n8 & 2)) : n8 * 32 + 8 * t4, ks_at = kKv4Block * (D / 2) + n8 * kG;
+  const int v_at = D == 128 ? t4 * 64 + ((8 * n8) ^ ((t4 & 2) << 4)) : t4 * 32 + 4 * n8;
 
   // ---- scores
 #pragma unroll
-  for (int s = 0; s < kKv4Stages - 1; ++s) request_k(warp + 8 * s, s);
+  for (int s = 0; s < kKv4Stages - 1; ++s) request_k(warp + 8 * s, s * kStage);
   int best[RN][2];
 #pragma unroll
   for (int j = 0; j < RN; ++j) best[j][0] = best[j][1] = -128;
-  int stage = 0;
+  uint32_t stage = 0, behind = (kKv4Stages - 1) * kStage;   // the block at hand; where the one requested now goes
   for (int lb = warp; lb < nblk; lb += 8) {
     cp_wait<kKv4Stages - 2>();
     __syncwarp();
-    request_k(lb + 8 * (kKv4Stages - 1), (stage + kKv4Stages - 1) % kKv4Stages);
-    const uint8_t* buf = ring + stage * kStage;
-    stage = (stage + 1) % kKv4Stages;
+    request_k(lb + 8 * (kKv4Stages - 1), behind);
+    const uint8_t* buf = ring + stage;
+    behind = stage;
+    stage = stage == (kKv4Stages - 1) * kStage ? 0 : stage + kStage;
     const int key0 = (blk0 + lb) * kKv4Block;
-    if (pages[(key0 >> a.page_log) - page0] < 0) continue;
+    if (holes && !pages[(lb + first) >> per_page]) continue;
     int acc[RN][2][4];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       uint32_t w[2][kLaneWords], st[2];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int row = 16 * m + 8 * k + n8;
+        const int row = 16 * m + 8 * k;    // (and n8)
         if (D == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(buf + row * 64 + 16 * (t4 ^ (row & 2)));
+          const uint4 v = *reinterpret_cast<const uint4*>(buf + k_at + row * 64);
           w[k][0] = v.x; w[k][1] = v.y; w[k][kLaneWords - 2] = v.z; w[k][kLaneWords - 1] = v.w;
-          st[k] = *reinterpret_cast<const uint32_t*>(buf + kKv4Block * 64 + 4 * row);
+          st[k] = *reinterpret_cast<const uint32_t*>(buf + ks_at + 4 * row);
         } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(buf + row * 32 + 8 * t4);
+          const uint2 v = *reinterpret_cast<const uint2*>(buf + k_at + row * 32);
           w[k][0] = v.x; w[k][1] = v.y;
-          st[k] = *reinterpret_cast<const uint16_t*>(buf + kKv4Block * 32 + 2 * row);
+          st[k] = *reinterpret_cast<const uint16_t*>(buf + ks_at + 2 * row);
         }
       }
 #pragma unroll
@@ -244,7 +271,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
       for (int g = 0; g < kG; ++g) {
         const uint32_t a0 = low16(w[0][g]), a1 = low16(w[1][g]), a2 = high16(w[0][g]), a3 = high16(w[1][g]);
-        const int s0 = (st[0] >> (8 * g)) & 255, s1 = (st[1] >> (8 * g)) & 255;
+        const int s0 = __byte_perm(st[0], 0, 0x4440 | g), s1 = __byte_perm(st[1], 0, 0x4440 | g);
 #pragma unroll
         for (int j = 0; j < RN; ++j) {
           int c[4] = {0, 0, 0, 0};
@@ -271,13 +298,13 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
           for (int i = 0; i < 4; ++i) v[i] = 8 * i < left ? v[i] : -128;
         }
         best[j][e] = max(max(best[j][e], max(v[0], v[1])), max(v[2], v[3]));
-        *reinterpret_cast<uint32_t*>(score + row * score_ld + lb * kKv4Block + 4 * n8) = pack_sat(v[0], v[1], v[2], v[3]);
+        if (row < a.kept) *reinterpret_cast<uint32_t*>(score + row * score_ld + lb * kKv4Block + 4 * n8) = pack_sat(v[0], v[1], v[2], v[3]);
       }
   }
   cp_wait<0>();
   __syncwarp();
 #pragma unroll
-  for (int s = 0; s < kKv4Stages - 1; ++s) request_v(warp + 8 * s, s);
+  for (int s = 0; s < kKv4Stages - 1; ++s) request_v(warp + 8 * s, s * kStage);
 #pragma unroll
   for (int j = 0; j < RN; ++j)
 #pragma unroll
@@ -288,19 +315,22 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       if (lane < 4) warp_top[warp * 16 + 8 * j + 2 * lane + e] = v;
     }
   __syncthreads();
-  if (tid < kRows) {
-    int v = -128;
+  // sixteen lanes for a row: over the warps of the CTA, then over the CTAs of the cluster
+  const int pr = tid >> 4, pk = tid & 15;
+  if (pr < kRows) {
+    int v = pk < kKv4Warps ? warp_top[pk * 16 + pr] : -128;
 #pragma unroll
-    for (int i = 0; i < kKv4Warps; ++i) v = max(v, warp_top[i * 16 + tid]);
-    cta_top[tid] = v;
-    if (a.split == 1) top[tid] = v;
+    for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
+    if (pk == 0) (a.split == 1 ? top : cta_top)[pr] = v;
   }
   if (a.split > 1) {
-    cluster_sync();
-    if (tid < kRows) {
-      int v = -128;
-      for (int i = 0; i < a.split; ++i) v = max(v, peer_i32(peer_addr(smem_u32(cta_top + tid), i)));
-      top[tid] = v;
+    cluster_arrive();
+    cluster_wait();
+    if (pr < kRows) {
+      int v = pk < a.split ? peer_i32(peer_addr(smem_u32(cta_top + pr), pk)) : -128;
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
+      if (pk == 0) top[pr] = v;
     }
   }
   __syncthreads();
@@ -308,27 +338,32 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   // ---- values
   int lo[RN][kMu][4], hi[RN][kMu][4];
   unsigned long long den[RN];
+  unsigned ul[RN], uh[RN];                 // sums of the weights' planes
   uint32_t tab[RN];
+  const int8_t* mine[RN];                  // the lane's row of scores (rows that no sequence has: the last one that some can have)
   const uint32_t tab0 = smem_u32(sm + at.table) + 4 * (lane & (kKv4Copies - 1));
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
-    den[j] = 0;
-    tab[j] = tab0 + (uint32_t)(4 * kKv4Copies * top[8 * j + n8]);
+    den[j] = ul[j] = uh[j] = 0;
+    const int row = min(8 * j + n8, a.kept - 1);
+    mine[j] = score + row * score_ld + 4 * t4;
+    tab[j] = tab0 + (uint32_t)(4 * kKv4Copies * top[row]);
 #pragma unroll
     for (int m = 0; m < kMu; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i) lo[j][m][i] = hi[j][m][i] = 0;
   }
   constexpr uint32_t kSel = (uint32_t)(-4 * kKv4Copies) & 255u;
-  stage = 0;
+  stage = 0, behind = (kKv4Stages - 1) * kStage;
   for (int lb = warp; lb < nblk; lb += 8) {
     cp_wait<kKv4Stages - 2>();
     __syncwarp();
-    request_v(lb + 8 * (kKv4Stages - 1), (stage + kKv4Stages - 1) % kKv4Stages);
-    const uint8_t* buf = ring + stage * kStage;
-    stage = (stage + 1) % kKv4Stages;
+    request_v(lb + 8 * (kKv4Stages - 1), behind);
+    const uint8_t* buf = ring + stage;
+    behind = stage;
+    stage = stage == (kKv4Stages - 1) * kStage ? 0 : stage + kStage;
     const int key0 = (blk0 + lb) * kKv4Block;
-    if (pages[(key0 >> a.page_log) - page0] < 0) continue;
+    if (holes && !pages[(lb + first) >> per_page]) continue;
     // steps of the lane's keys t, t + 4, ..., t + 28
     uint32_t vs[8];
     {
@@ -344,12 +379,12 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       unsigned sum = 0;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const uint32_t s = *reinterpret_cast<const uint32_t*>(score + (8 * j + n8) * score_ld + lb * kKv4Block + 4 * (t4 + 4 * k));
+        const uint32_t s = *reinterpret_cast<const uint32_t*>(mine[j] + lb * kKv4Block + 16 * k);
         unsigned e[4], p[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) e[i] = exp_of(s, kSel << (8 * i), tab[j]);
         if (!whole) {
-          const int left = lim[8 * j + n8] - key0 - t4 - 4 * k;
+          const int left = lim[min(8 * j + n8, a.kept - 1)] - key0 - t4 - 4 * k;
 #pragma unroll
           for (int i = 0; i < 4; ++i) e[i] = 8 * i < left ? e[i] : 0;
         }
@@ -361,6 +396,8 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
         const uint32_t p01 = __byte_perm(p[0], p[1], 0x7362), p23 = __byte_perm(p[2], p[3], 0x7362);
         bl[j][k] = __byte_perm(p01, p23, 0x5410);
         bh[j][k] = __byte_perm(p01, p23, 0x7632);
+        ul[j] = __dp4a(bl[j][k], 0x01010101u, ul[j]);
+        uh[j] = __dp4a(bh[j][k], 0x01010101u, uh[j]);
       }
       den[j] += sum;
     }
@@ -369,13 +406,13 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     for (int k = 0; k < 2; ++k)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int row = t4 + 4 * k + 8 * i;
+        const int row = 4 * k + 8 * i;     // (and t4)
         if (D == 128) {
-          const uint2 v = *reinterpret_cast<const uint2*>(buf + row * 64 + ((8 * n8) ^ ((row & 2) << 4)));
+          const uint2 v = *reinterpret_cast<const uint2*>(buf + v_at + row * 64);
           x[0][k][i] = v.x;
           x[kVWords - 1][k][i] = v.y;
         } else {
-          x[0][k][i] = *reinterpret_cast<const uint32_t*>(buf + row * 32 + 4 * n8);
+          x[0][k][i] = *reinterpret_cast<const uint32_t*>(buf + v_at + row * 32);
         }
       }
 #pragma unroll
@@ -385,7 +422,8 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       transpose4(x[w][1], y[1]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const uint32_t a0 = low16(y[0][i]), a1 = high16(y[0][i]), a2 = low16(y[1][i]), a3 = high16(y[1][i]);
+        // code + 8 of the lower half's channel, 16 (code + 8) of the upper half's
+        const uint32_t a0 = y[0][i] & 0x0f0f0f0fu, a1 = y[0][i] & 0xf0f0f0f0u, a2 = y[1][i] & 0x0f0f0f0fu, a3 = y[1][i] & 0xf0f0f0f0u;
 #pragma unroll
         for (int j = 0; j < RN; ++j) {
           mma8<true>(lo[j][4 * w + i], a0, a1, a2, a3, bl[j][0], bl[j][1]);
@@ -395,118 +433,132 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     }
   }
   cp_wait<0>();
+
+  // ---- the CTA's sums, in shared memory: the warps add theirs (32 different banks at a time)
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
     unsigned long long v = den[j];
-    v += __shfl_xor_sync(~0u, v, 1);
-    v += __shfl_xor_sync(~0u, v, 2);
-    if (t4 == 0) warp_den[warp * 16 + 8 * j + n8] = v;
-  }
-
-  // ---- the CTA's sums: warp by warp into slabs [plane][row][channel], added up by the thread that has that row and four channels
-  constexpr int kLd = D + 8;
-  int* const slab = reinterpret_cast<int*>(sm + at.ring);
-  constexpr int kThreads = 8 * D / 4;          // threads that hold sums of a tile of eight rows
-  const int my_row = tid / (D / 4), my_ch = tid % (D / 4) * 4;
-  int4 sl[RN], sh[RN];
 #pragma unroll
-  for (int j = 0; j < RN; ++j) {
-    __syncthreads();
-    int* mine = slab + warp * (2 * 8 * kLd);
-    const int p = kMu * n8;
+    for (int o = 1; o < 4; o <<= 1) {
+      v += __shfl_xor_sync(~0u, v, o);
+      ul[j] += __shfl_xor_sync(~0u, ul[j], o);
+      uh[j] += __shfl_xor_sync(~0u, uh[j], o);
+    }
+    if (t4 == 0) {
+      warp_den[warp * 16 + 8 * j + n8] = v;
+      atomicAdd(cta_u + 8 * j + n8, (int)ul[j]);
+      atomicAdd(cta_u + 16 + 8 * j + n8, (int)uh[j]);
+    }
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
+    for (int e = 0; e < 4; ++e) {
+      int* dst = sums + (8 * j + 2 * t4 + (e & 1)) * kLd + (e >> 1) * (D / 2) + n8;
 #pragma unroll
-      for (int m = 0; m < kMu; m += 4) {
-        int* dst = mine + (2 * t4 + (e & 1)) * kLd + p + m + (e >> 1) * (D / 2);
-        *reinterpret_cast<int4*>(dst) = make_int4(lo[j][m][e], lo[j][m + 1][e], lo[j][m + 2][e], lo[j][m + 3][e]);
-        *reinterpret_cast<int4*>(dst + 8 * kLd) = make_int4(hi[j][m][e], hi[j][m + 1][e], hi[j][m + 2][e], hi[j][m + 3][e]);
+      for (int m = 0; m < kMu; ++m) {
+        atomicAdd(dst + 8 * m, lo[j][m][e]);
+        atomicAdd(dst + kRows * kLd + 8 * m, hi[j][m][e]);
       }
-    __syncthreads();
-    sl[j] = sh[j] = make_int4(0, 0, 0, 0);
-    if (tid < kThreads)
-#pragma unroll
-      for (int w = 0; w < kKv4Warps; ++w) {
-        const int4 x = *reinterpret_cast<const int4*>(slab + w * (2 * 8 * kLd) + my_row * kLd + my_ch);
-        const int4 y = *reinterpret_cast<const int4*>(slab + w * (2 * 8 * kLd) + (8 + my_row) * kLd + my_ch);
-        sl[j].x += x.x; sl[j].y += x.y; sl[j].z += x.z; sl[j].w += x.w;
-        sh[j].x += y.x; sh[j].y += y.y; sh[j].z += y.z; sh[j].w += y.w;
-      }
-  }
-  if (tid < kRows) {
-    unsigned long long v = 0;
-#pragma unroll
-    for (int i = 0; i < kKv4Warps; ++i) v += warp_den[i * 16 + tid];
-    cta_den[tid] = v;
+    }
   }
   __syncthreads();
-  if (a.split > 1) {
+  // ---- the rows' sums and the cluster's
+  unsigned long long row_d = 0, row_s = 0;   // denominator and sum of the weights, of this CTA
+  if (pr < kRows) {
+    row_d = pk < kKv4Warps ? warp_den[pk * 16 + pr] : 0;
 #pragma unroll
-    for (int j = 0; j < RN; ++j)
-      if (tid < kThreads) {
-        *reinterpret_cast<int4*>(slab + (8 * j + my_row) * kLd + my_ch) = sl[j];
-        *reinterpret_cast<int4*>(slab + (kRows + 8 * j + my_row) * kLd + my_ch) = sh[j];
-      }
-    cluster_sync();
+    for (int o = 1; o < 16; o <<= 1) row_d += __shfl_xor_sync(~0u, row_d, o);
+    row_s = (unsigned)cta_u[pr] + 256ull * (unsigned)cta_u[16 + pr];
   }
-  auto row_den = [&](int row) {
-    unsigned long long v = 0;
-    if (a.split == 1) v = cta_den[row];
-    else
-      for (int i = 0; i < a.split; ++i) v += peer_u64(peer_addr(smem_u32(cta_den + row), i));
-    return v >> (16 - a.z);
-  };
-
-  // ---- outputs: each CTA of the cluster takes its share of the (row, four channels)
-#pragma unroll
-  for (int j = 0; j < RN; ++j) {
-    const int share = kThreads / a.split;     // (split divides it: 128 or 256 by 1 ... 16)
-    int item = tid;
-    if (a.split > 1) item = tid < share ? rank * share + tid : kThreads;
-    const int row = 8 * j + item / (D / 4), ch = item % (D / 4) * 4;
-    if (item < kThreads && row < nrows) {
-      long long num[4];
-      if (a.split == 1) {
-        num[0] = sl[j].x + 256ll * sh[j].x; num[1] = sl[j].y + 256ll * sh[j].y;
-        num[2] = sl[j].z + 256ll * sh[j].z; num[3] = sl[j].w + 256ll * sh[j].w;
-      } else {
-        num[0] = num[1] = num[2] = num[3] = 0;
-        const uint32_t mine = smem_u32(slab + row * kLd + ch);
-        for (int i = 0; i < a.split; ++i) {
-          const uint32_t src = peer_addr(mine, i);
-          const int4 x = peer_i128(src), y = peer_i128(src + kRows * kLd * 4);
-          num[0] += x.x + 256ll * y.x; num[1] += x.y + 256ll * y.y;
-          num[2] += x.z + 256ll * y.z; num[3] += x.w + 256ll * y.w;
-        }
+  if (a.split > 1) {
+    if (pr < kRows && pk == 0) cta_den[pr] = row_d;
+    cluster_arrive();
+    cluster_wait();
+    if (pr < kRows) {
+      row_d = row_s = 0;
+      if (pk < a.split) {
+        row_d = peer_u64(peer_addr(smem_u32(cta_den + pr), pk));
+        row_s = (unsigned)peer_i32(peer_addr(smem_u32(cta_u + pr), pk)) + 256ull * (unsigned)peer_i32(peer_addr(smem_u32(cta_u + 16 + pr), pk));
       }
-      const unsigned long long dn = row_den(row);
-      int out[4] = {0, 0, 0, 0};
-      if (dn) {
-        const int cut = max(0, 32 - __clzll((long long)dn));
-        const unsigned long long r = ~0ull / (dn >> cut);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)   // (the codes came in sixteenfold: 2^(z+5) / 16)
-          out[i] = rq(small_quotient(num[i] * (1ll << (a.z + 1)), dn, cut, r), a.pv_mult, a.pv_shift);
+      for (int o = 1; o < 16; o <<= 1) {
+        row_d += __shfl_xor_sync(~0u, row_d, o);
+        row_s += __shfl_xor_sync(~0u, row_s, o);
       }
-      const int qr = row0 + row;
-      *reinterpret_cast<uint32_t*>(a.O + (seq.q0 + qr / a.group) * a.ldo + (int64_t)(h * a.group + qr % a.group) * D + ch) =
-          pack_sat(out[0], out[1], out[2], out[3]);
     }
+  }
+  if (pr < kRows && pk == 0) {
+    row_d >>= 16 - a.z;
+    row_den[pr] = row_d;
+    row_u[pr] = row_s;
+    row_recip[pr] = recip_of(row_d);
+  }
+  constexpr int kTurns = kRows * D / 256;
+  const int own = kRows * D / a.split;     // sums that this CTA finishes, in the order [row][half of the channels][channel of a lane][lane]
+  long long part[kTurns];
+  if (a.split == 1) {
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int item = tid + 256 * i;
+      const int* src = sums + item / D * kLd + item % D;
+      part[i] = src[0] + 256ll * src[kRows * kLd];
+    }
+  } else {
+    // 256 / own threads for one of them, each with some of the peers (eight at most), so that the lanes of a warp read one peer's words in a row
+    const int groups = own < 256 ? 256 / own : 1, g = own < 256 ? tid / own : 0;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      part[i] = 0;
+      if (256 * i < own) {
+        const int item = rank * own + (own < 256 ? tid % own : tid + 256 * i);
+        const uint32_t src = smem_u32(sums + item / D * kLd + item % D);
+        int x[8], y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          x[k] = y[k] = 0;
+          if (g + k * groups < a.split) {
+            const uint32_t from = peer_addr(src, g + k * groups);
+            x[k] = peer_i32(from);
+            y[k] = peer_i32(from + kRows * kLd * 4);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) part[i] += x[k] + 256ll * y[k];
+      }
+    }
+    cluster_arrive();                      // (waited for at the end: a CTA's sums stay until its peers have read them)
+    if (groups > 1) {
+      fin[tid] = part[0];
+      __syncthreads();
+      part[0] = 0;
+      for (int k = 0; k < groups; ++k) part[0] += fin[k * own + tid % own];
+    }
+  }
+  __syncthreads();
+
+  // ---- outputs
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int item = min(rank * own + tid + 256 * i, kRows * D - 1), row = item / D;
+    const int half = item % D / (D / 2), ch = half * (D / 2) + item % 8 * kMu + item % (D / 2) / 8;
+    const unsigned long long den_row = row_den[row];
+    // (codes came in as code + 8, those of the upper half sixteenfold; a row that sees nothing: every number is zero)
+    const long long num = (part[i] >> (4 * half)) - 8 * (long long)row_u[row];
+    const int t = small_quotient(num * (1ll << (a.z + 5)), den_row, cut_of(den_row), row_recip[row]);
+    if (tid + 256 * i < own && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
   }
 
   // ---- accumulated weights: floor(e 2^24 / den) of every difference of scores, row by row, then the sum over the rows of each key
   if (kWeights) {
-    unsigned* share = reinterpret_cast<unsigned*>(sm + at.ring + 2 * kRows * kLd * 4);
+    unsigned* share = reinterpret_cast<unsigned*>(sm + at.ring);
     for (int i = tid; i < nrows * 256; i += 256) {
-      const unsigned long long dn = row_den(i >> 8);
+      const unsigned long long den_row = row_den[i >> 8];
       const unsigned e = *reinterpret_cast<const unsigned*>(sm + at.table + (i & 255) * (4 * kKv4Copies)) >> (16 - a.z);
-      share[i] = dn ? (unsigned)(((unsigned long long)e << 24) / dn) : 0;
+      share[i] = den_row ? (unsigned)small_quotient((long long)e << 24, den_row, cut_of(den_row), row_recip[i >> 8]) : 0;
     }
     __syncthreads();
     unsigned long long* w = reinterpret_cast<unsigned long long*>(a.weights) + ((int64_t)b * a.heads + h) * a.ldw;
     for (int i = tid; i < nblk * 8; i += 256) {
       const int key0 = (blk0 + (i >> 3)) * kKv4Block, n = i & 7;
-      if (pages[(key0 >> a.page_log) - page0] < 0) continue;
+      if (holes && !pages[((i >> 3) + first) >> per_page]) continue;
       unsigned long long v[4] = {0, 0, 0, 0};
       for (int row = 0; row < nrows; ++row) {
         const uint32_t s = *reinterpret_cast<const uint32_t*>(score + row * score_ld + 4 * i);
@@ -520,7 +572,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
         if (v[k]) atomicAdd(w + key0 + n + 8 * k, v[k]);
     }
   }
-  if (a.split > 1) cluster_sync();   // a CTA's sums stay until its peers have read them
+  if (a.split > 1) cluster_wait();
 }
 
 template <class F>
@@ -567,7 +619,7 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_
   const int64_t top = (int64_t)smax.I0 << smax.N;
   while (top >> (a.z + 8)) ++a.z;
   a.O = O; a.ldo = ldo; a.weights = weights; a.ldw = ldw;
-  a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.tiles = p.tiles;
+  a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept;
   a.status = ctx->status_dev;
   LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * seqs * q_heads * max_q * max_len * d);
   cudaLaunchConfig_t cfg = {};

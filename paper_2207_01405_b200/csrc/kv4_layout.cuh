@@ -51,51 +51,56 @@ IVIT_KV4_FN int kv4_seen(const Kv4Seq& s, int t) {
 
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time
 constexpr int kKv4Warps = 8;
-constexpr int kKv4Stages = 4;      // blocks that a warp has requested ahead
+constexpr int kKv4Stages = 3;      // blocks that a warp holds: one it works on, the others on their way
 constexpr int kKv4Copies = 8;      // copies of the exponentials
+constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: 16 (code + 8) times the upper byte of a weight, over 32768 keys, stays below 2^31
+constexpr int kKv4Small = 2560;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
+constexpr int kKv4SmemHalf = 113 * 1024;   // two CTAs on an SM
 
 // Bytes of a row of scores in shared memory: 16 modulo 128, so that eight rows at the same keys lie in different banks.
 IVIT_KV4_FN int kv4_score_ld(int blocks) { return (blocks * kKv4Block + 127) / 128 * 128 + 16; }
 IVIT_KV4_FN int kv4_stage_bytes(int d) { return kKv4Block * (d / 2 + d / 32); }
+// Words of a row of sums: 4 modulo 32, so that the lanes of a warp add to different banks.
+IVIT_KV4_FN int kv4_sum_ld(int d) { return d + 4; }
 
 struct Kv4Smem {
-  int table, pages, small, ring, score, total;
+  int table, small, sums, fin, pages, ring, score, total;
 };
-// rows: query rows of a CTA (8 or 16); blocks: blocks of keys of a CTA.
-IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int page, int blocks) {
+// rows: query rows of a CTA (8 or 16); kept: those of them that some sequence can have, whose scores are kept; blocks: blocks of keys of a CTA.
+IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks) {
   Kv4Smem m;
   m.table = 0;
   m.small = m.table + 256 * kKv4Copies * 4;
-  m.pages = m.small + 2048;
-  m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 4 + 127) / 128 * 128;
-  // behind the passes the ring holds the warps' partial sums of eight rows (two planes of 32 bits), then a CTA's and the shares of the weights
-  int ring = kKv4Warps * kKv4Stages * kv4_stage_bytes(d);
-  const int slabs = kKv4Warps * 2 * 8 * (d + 8) * 4, behind = 2 * rows * (d + 8) * 4 + rows * 256 * 4;
-  ring = ring > slabs ? ring : slabs;
-  ring = ring > behind ? ring : behind;
-  m.score = m.ring + ring;
-  m.total = m.score + rows * kv4_score_ld(blocks);
+  m.sums = m.small + kKv4Small;
+  m.fin = m.sums + 2 * rows * kv4_sum_ld(d) * 4;
+  m.pages = m.fin + 256 * 8;
+  m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 8 + 127) / 128 * 128;
+  // behind the passes the ring holds the shares of the weights
+  const int ring = kKv4Warps * kKv4Stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
+  m.score = m.ring + (ring > shares ? ring : shares);
+  m.total = m.score + kept * kv4_score_ld(blocks);
   return m;
 }
 
 struct Kv4Plan {
-  int rows, split, blocks, tiles, smem;   // query rows of a CTA, CTAs of a cluster along the keys, blocks of each, row tiles, bytes
+  int rows, kept, split, blocks, tiles, smem;   // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, row tiles, bytes
 };
 inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms) {
   Kv4Plan p;
   const int64_t all = (max_len + kKv4Block - 1) / kKv4Block, q_rows = max_q * group;
   for (p.rows = q_rows <= 8 ? 8 : 16;; p.rows = 8) {
     p.tiles = (int)((q_rows + p.rows - 1) / p.rows);
+    p.kept = (int)(q_rows < p.rows ? q_rows : p.rows);
     const int64_t ctas = (int64_t)p.tiles * heads * seqs;
-    p.split = 1;
-    while (p.split < 16 && ctas * p.split < 2 * sms && all > (int64_t)p.split * kKv4Warps) p.split *= 2;
-    for (;; p.split *= 2) {
+    auto size = [&]() {
       p.blocks = (int)((all + p.split - 1) / p.split);
       if (p.blocks < 1) p.blocks = 1;
-      p.smem = kv4_smem(d, p.rows, page, p.blocks).total;
-      if (p.smem <= kKv4SmemMax || p.split == 16) break;
-    }
+      p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks).total;
+    };
+    p.split = 1;
+    while (p.split < 16 && ctas * p.split < sms && all > (int64_t)p.split * kKv4Warps) p.split *= 2;
+    for (size(); (p.blocks > kKv4Blocks || p.smem > (p.rows == 8 ? kKv4SmemHalf : kKv4SmemMax)) && p.split < 16; size()) p.split *= 2;
     if (p.smem <= kKv4SmemMax || p.rows == 8) return p;
   }
 }
