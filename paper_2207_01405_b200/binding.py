@@ -194,9 +194,12 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(-2) if t.dim() >= 2 else t.shape[-1]
 
 
-def _row_ld(t: torch.Tensor) -> int:
+def _row_ld(t: torch.Tensor, rows: int, cols: int) -> int:
     """Leading dimension of a 2-d tensor; one row (or none) has no use for it, and its stride may be anything."""
-    return t.stride(0) if t.shape[0] > 1 else (t.shape[1] + 15) // 16 * 16
+    return t.stride(0) if rows > 1 else (cols + 15) // 16 * 16
+
+
+_UNIT = CScale(None, None, 2 ** 31 - 1, 31)
 
 
 class DevScale:
@@ -238,7 +241,7 @@ class Kv4Cache:
         self.c = CKv4(pool.data_ptr(), pool.shape[0], pool.shape[1], d, page)
         if pool.numel() != load_library().ivit_kv4_cache_bytes(C.byref(self.c)):
             raise ValueError("ivit_kv4_cache_bytes rejected the cache: d is 64 or 128, page 32, 64, 128 or 256")
-        self.ref = C.byref(self.c)
+        self.ref, self.width, self.index = C.byref(self.c), self.heads * d, pool.get_device()
 
     @classmethod
     def empty(cls, pages: int, heads: int, d: int, page: int, device) -> "Kv4Cache":
@@ -275,6 +278,7 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("no CUDA device: the integer ViT library has no CPU path")
         self.device = torch.device("cuda", device)
+        self.index = device
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         h = C.c_void_p()
@@ -425,104 +429,118 @@ class Context:
         return out
 
     def _want(self, what: str, dtype, dim: int, t: torch.Tensor):
-        """Refuses a tensor that the C side would read as something else."""
-        if t.dtype != dtype or t.dim() != dim or t.device != self.device or (t.shape[-1] > 1 and t.stride(-1) != 1):
-            raise ValueError(f"{what}: want a {dim}-d {dtype} tensor on {self.device} with contiguous rows, got {tuple(t.shape)} "
+        """Refuses a tensor that the C side would read as something else; returns its shape."""
+        shape = t.shape
+        if t.dtype is not dtype or len(shape) != dim or t.get_device() != self.index or (shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{what}: want a {dim}-d {dtype} tensor on {self.device} with contiguous rows, got {tuple(shape)} "
                              f"{t.dtype} on {t.device}, strides {t.stride()}")
+        return shape
 
     def rmsnorm(self, x, gamma_scale: DevScale, x_scale: DevScale = None, res=None, res_scale: DevScale = None, M_ln=20, sum_out=None,
                 out=None, row_max=None):
         """ivit_rmsnorm: x (int8 or int32) [rows, C], with res added first (its sum goes to sum_out, which may be res); returns int8 rows.
         row_max (int32 [rows]): every row gets a scale of its own, written there."""
-        rows, Cc = x.shape
+        x8 = x.dtype is torch.int8
+        shape = self._want("x", torch.int8 if x8 else torch.int32, 2, x)
+        rows, Cc = shape
         if out is None:
             out = torch.empty((rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
-        self._want("x", torch.int8 if x.dtype == torch.int8 else torch.int32, 2, x)
-        self._want("out", torch.int8, 2, out)
-        if out.shape != x.shape or (res is None) != (res_scale is None):
-            raise ValueError("out has the shape of x, and res comes with res_scale")
-        for t, n in ((res, "res"), (sum_out, "sum_out")):
-            if t is not None:
-                self._want(n, torch.int8 if res is not None and res.dtype == torch.int8 else torch.int32, 2, t)
-                if t.shape != x.shape:
-                    raise ValueError(f"{n} has the shape of x")
-        if row_max is not None:
-            self._want("row_max", torch.int32, 1, row_max)
-            if row_max.shape[0] != rows:
-                raise ValueError("row_max has an entry for each row")
-        for s in (gamma_scale, x_scale):
-            if s is not None and s.mult_t is not None and s.mult_t.numel() != Cc:
+        elif self._want("out", torch.int8, 2, out) != shape:
+            raise ValueError("out has the shape of x")
+        r8, ld_res, ld_sum, p_res, p_sum, p_max, xs, rs = 0, 0, 0, None, None, None, _UNIT, _UNIT
+        if res is not None:
+            r8 = res.dtype is torch.int8
+            dt = torch.int8 if r8 else torch.int32
+            if x_scale is None or res_scale is None or self._want("res", dt, 2, res) != shape:
+                raise ValueError("res has the shape of x, and comes with x_scale and res_scale")
+            xs, rs, p_res, ld_res = x_scale.c, res_scale.c, res.data_ptr(), _row_ld(res, rows, Cc)
+            if x_scale.mult_t is not None and x_scale.mult_t.numel() != Cc:
                 raise ValueError("a per-channel scale has an entry for each channel")
-        one = CScale(None, None, 2 ** 31 - 1, 31)
-        _chk(self.lib.ivit_rmsnorm(self.h, x.data_ptr(), I8 if x.dtype == torch.int8 else I32, _row_ld(x),
-                                   x_scale.c if x_scale is not None else one, _ptr(res),
-                                   I8 if res is not None and res.dtype == torch.int8 else I32, _row_ld(res) if res is not None else 0,
-                                   res_scale.c if res_scale is not None else one, gamma_scale.c, M_ln, _ptr(sum_out),
-                                   _row_ld(sum_out) if sum_out is not None else 0, out.data_ptr(), _row_ld(out), _ptr(row_max), rows, Cc),
-             "ivit_rmsnorm")
+            if sum_out is not None:
+                if self._want("sum_out", dt, 2, sum_out) != shape:
+                    raise ValueError("sum_out has the shape of x")
+                p_sum, ld_sum = sum_out.data_ptr(), _row_ld(sum_out, rows, Cc)
+        elif sum_out is not None:
+            raise ValueError("sum_out comes with res")
+        if gamma_scale.mult_t is not None and gamma_scale.mult_t.numel() != Cc:
+            raise ValueError("a per-channel scale has an entry for each channel")
+        if row_max is not None:
+            if self._want("row_max", torch.int32, 1, row_max)[0] != rows:
+                raise ValueError("row_max has an entry for each row")
+            p_max = row_max.data_ptr()
+        rc = self.lib.ivit_rmsnorm(self.h, x.data_ptr(), I8 if x8 else I32, _row_ld(x, rows, Cc), xs, p_res, I8 if r8 else I32, ld_res, rs,
+                                   gamma_scale.c, M_ln, p_sum, ld_sum, out.data_ptr(), _row_ld(out, rows, Cc), p_max, rows, Cc)
+        if rc:
+            raise IvitError(rc, "ivit_rmsnorm")
         return out
 
     # ---- cache in 4 bits ----
 
     def kv4_append(self, cache: Kv4Cache, k, v, slots):
         """ivit_kv4_append: int8 rows [tokens, heads d] into the rows of the pool that slots (int64) names; negative: left out."""
-        self._want("k", torch.int8, 2, k)
-        self._want("v", torch.int8, 2, v)
-        self._want("slots", torch.int64, 1, slots)
-        if k.shape != v.shape or k.shape != (slots.shape[0], cache.heads * cache.d) or cache.pool.device != self.device:
+        shape = self._want("k", torch.int8, 2, k)
+        n, width = shape
+        if (self._want("v", torch.int8, 2, v) != shape or self._want("slots", torch.int64, 1, slots)[0] != n or width != cache.width or
+                cache.index != self.index):
             raise ValueError("k and v are [tokens, heads d], slots [tokens], the pool is on the context's device")
-        _chk(self.lib.ivit_kv4_append(self.h, cache.ref, k.data_ptr(), _row_ld(k), v.data_ptr(), _row_ld(v), slots.data_ptr(),
-                                      slots.shape[0]), "ivit_kv4_append")
+        rc = self.lib.ivit_kv4_append(self.h, cache.ref, k.data_ptr(), _row_ld(k, n, width), v.data_ptr(), _row_ld(v, n, width), slots.data_ptr(), n)
+        if rc:
+            raise IvitError(rc, "ivit_kv4_append")
 
     def kv4_attention(self, cache: Kv4Cache, q, q_start, lens, table, qk_scale: DevScale, smax, pv_scale: DevScale, max_q: int, max_len: int,
                       out=None, weights=None):
         """ivit_kv4_attention: query rows [tokens, query heads d] of len(lens) sequences over the cache; returns int8 rows of the same
         shape (a new one starts as zeros, rows of no sequence keep what out held).  weights (int64 [seqs, heads, >= max_len]) is added to."""
+        shape = self._want("q", torch.int8, 2, q)
+        n, width = shape
         if out is None:
-            out = torch.zeros_like(q, memory_format=torch.contiguous_format)
-        self._want("q", torch.int8, 2, q)
-        self._want("out", torch.int8, 2, out)
-        self._want("lens", torch.int32, 1, lens)
-        self._want("q_start", torch.int32, 1, q_start)
-        self._want("table", torch.int32, 2, table)
-        seqs = lens.shape[0]
-        if q.shape != out.shape or q.shape[1] % cache.d or q_start.shape[0] != seqs + 1 or table.shape[0] != seqs or cache.pool.device != self.device:
-            raise ValueError("q and out are [tokens, query heads d], q_start [seqs + 1], table [seqs, pages], the pool is on the context's device")
-        if table.shape[1] * cache.page < max_len:
-            raise ValueError("table names pages for max_len keys of each sequence")
-        ldw = 0
+            out = torch.zeros((n, width), dtype=torch.int8, device=q.device)
+        elif self._want("out", torch.int8, 2, out) != shape:
+            raise ValueError("out has the shape of q")
+        seqs, = self._want("lens", torch.int32, 1, lens)
+        t_rows, t_cols = self._want("table", torch.int32, 2, table)
+        if (self._want("q_start", torch.int32, 1, q_start)[0] != seqs + 1 or t_rows != seqs or width % cache.d or t_cols * cache.page < max_len or
+                cache.index != self.index):
+            raise ValueError("q is [tokens, query heads d], q_start [seqs + 1], table [seqs, pages for max_len keys], the pool is on the context's device")
+        p_w, ldw = None, 0
         if weights is not None:
-            self._want("weights", torch.int64, 3, weights)
-            ldw = weights.shape[2]
-            if weights.shape[:2] != (seqs, cache.heads) or not weights.is_contiguous():
+            w_seqs, w_heads, ldw = self._want("weights", torch.int64, 3, weights)
+            if w_seqs != seqs or w_heads != cache.heads or not weights.is_contiguous():
                 raise ValueError("weights is a contiguous [seqs, heads, keys]")
-        _chk(self.lib.ivit_kv4_attention(self.h, cache.ref, q.data_ptr(), _row_ld(q), q.shape[1] // cache.d, q.shape[0], q_start.data_ptr(),
-                                         lens.data_ptr(), table.data_ptr(), _row_ld(table), qk_scale.c, _cexp(smax), pv_scale.c,
-                                         out.data_ptr(), _row_ld(out), _ptr(weights), ldw, seqs, max_q, max_len), "ivit_kv4_attention")
+            p_w = weights.data_ptr()
+        rc = self.lib.ivit_kv4_attention(self.h, cache.ref, q.data_ptr(), _row_ld(q, n, width), width // cache.d, n, q_start.data_ptr(),
+                                         lens.data_ptr(), table.data_ptr(), _row_ld(table, seqs, t_cols), qk_scale.c,
+                                         smax if type(smax) is CExp else _cexp(smax), pv_scale.c, out.data_ptr(), _row_ld(out, n, width), p_w, ldw,
+                                         seqs, max_q, max_len)
+        if rc:
+            raise IvitError(rc, "ivit_kv4_attention")
         return out
 
     def kv4_evict(self, cache: Kv4Cache, weights, lens, table, keep: int, sinks: int, recent: int, max_len: int, dst_table=None,
                   weights_out=None, kept=None, new_lens=None):
         """ivit_kv4_evict: at most `keep` keys of each sequence and head stay; in place unless dst_table and weights_out are given.
         Returns (kept [seqs, heads, keep], new_lens [seqs])."""
-        seqs = lens.shape[0]
+        seqs, = self._want("lens", torch.int32, 1, lens)
         dst_table = table if dst_table is None else dst_table
         weights_out = weights if weights_out is None else weights_out
         kept = torch.empty((seqs, cache.heads, keep), dtype=torch.int32, device=self.device) if kept is None else kept
         new_lens = torch.empty_like(lens) if new_lens is None else new_lens
-        for n, t, dt, dim in (("weights", weights, torch.int64, 3), ("weights_out", weights_out, torch.int64, 3), ("lens", lens, torch.int32, 1),
-                              ("new_lens", new_lens, torch.int32, 1), ("table", table, torch.int32, 2), ("dst_table", dst_table, torch.int32, 2),
-                              ("kept", kept, torch.int32, 3)):
-            self._want(n, dt, dim, t)
-            if t.shape[0] != seqs or (dim == 3 and (t.shape[1] != cache.heads or not t.is_contiguous())):
-                raise ValueError(f"{n} has an entry for each of the {seqs} sequences (and {cache.heads} heads), contiguous")
-        if kept.shape[2] != keep or cache.pool.device != self.device:
-            raise ValueError("kept is [seqs, heads, keep], the pool is on the context's device")
-        if table.shape[1] * cache.page < max_len or dst_table.shape[1] * cache.page < min(keep, max_len):
+        ws, wh, ldw = self._want("weights", torch.int64, 3, weights)
+        os_, oh, ldo = self._want("weights_out", torch.int64, 3, weights_out)
+        ks, kh, kk = self._want("kept", torch.int32, 3, kept)
+        ts, tc = self._want("table", torch.int32, 2, table)
+        ds, dc = self._want("dst_table", torch.int32, 2, dst_table)
+        if not (ws == os_ == ks == ts == ds == seqs == self._want("new_lens", torch.int32, 1, new_lens)[0] and wh == oh == kh == cache.heads and
+                weights.is_contiguous() and weights_out.is_contiguous() and kept.is_contiguous() and kk == keep and cache.index == self.index):
+            raise ValueError("lens and new_lens are [seqs], weights and weights_out contiguous [seqs, heads, keys], kept contiguous "
+                             "[seqs, heads, keep], the tables [seqs, pages], the pool is on the context's device")
+        if tc * cache.page < max_len or dc * cache.page < min(keep, max_len):
             raise ValueError("the tables name pages for max_len and keep keys of each sequence")
-        _chk(self.lib.ivit_kv4_evict(self.h, cache.ref, weights.data_ptr(), weights.shape[2], lens.data_ptr(), table.data_ptr(), _row_ld(table),
-                                     dst_table.data_ptr(), _row_ld(dst_table), weights_out.data_ptr(), weights_out.shape[2], kept.data_ptr(),
-                                     new_lens.data_ptr(), seqs, max_len, keep, sinks, recent), "ivit_kv4_evict")
+        rc = self.lib.ivit_kv4_evict(self.h, cache.ref, weights.data_ptr(), ldw, lens.data_ptr(), table.data_ptr(), _row_ld(table, seqs, tc),
+                                     dst_table.data_ptr(), _row_ld(dst_table, seqs, dc), weights_out.data_ptr(), ldo, kept.data_ptr(),
+                                     new_lens.data_ptr(), seqs, max_len, keep, sinks, recent)
+        if rc:
+            raise IvitError(rc, "ivit_kv4_evict")
         return kept, new_lens
 
     def patchify(self, img, P, window=0):

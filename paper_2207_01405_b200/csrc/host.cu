@@ -1092,7 +1092,7 @@ int ivit_rmsnorm(ivit_ctx* ctx, const void* x, int32_t x_dtype, int64_t ldx, ivi
   if (!ctx || rows < 0 || C < 1 || (rows > 0 && (!x || !out)) || (sum && !res)) return IVIT_ERR_INVALID_ARG;
   if (x_dtype != IVIT_I8 && x_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
   if (res && res_dtype != IVIT_I8 && res_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
-  if (C % 4 || C > 16384 || rows > (1ll << 40)) return IVIT_ERR_UNSUPPORTED;
+  if (C % 4 || C > 16384 || rows > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
   if (M_ln < 8 || M_ln > 22) return IVIT_ERR_RANGE;
   if (ldx < C || ldout < C || (res && ldres < C) || (sum && ldsum < C)) return IVIT_ERR_INVALID_ARG;
   auto misaligned = [](const void* p, int64_t ld, int dtype) { return !aligned16(p) || ld % (dtype == IVIT_I8 ? 16 : 4); };
@@ -1124,7 +1124,7 @@ int ivit_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K,
   int rc = check_kv4(cache, true);
   if (rc) return rc;
   if (ldk < cache->heads * cache->d || ldv < cache->heads * cache->d) return IVIT_ERR_INVALID_ARG;
-  if (tokens > (1ll << 40)) return IVIT_ERR_UNSUPPORTED;
+  if (tokens > (1ll << 40) || tokens * cache->heads > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
   if (!aligned16(K) || !aligned16(V) || ldk % 16 || ldv % 16 || (reinterpret_cast<uintptr_t>(slots) & 7)) return IVIT_ERR_ALIGNMENT;
   DeviceGuard guard(ctx);
   if (!guard.ok) return IVIT_ERR_CUDA;

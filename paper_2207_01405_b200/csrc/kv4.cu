@@ -32,56 +32,84 @@ static Cache to_dev(const ivit_kv4_cache* c) {
 
 // ---------------------------------------------------------------- append
 
-__device__ __forceinline__ int kv4_code(int x, int step) {
-  if (step == 0) return 8;
-  return (16 * x + step + 16 * step) / (2 * step);   // + 8 keeps the numerator positive
+__device__ __forceinline__ int signed_byte(uint32_t w, int b) {
+  int d;
+  asm("prmt.b32 %0, %1, %1, %2;" : "=r"(d) : "r"(w), "r"(0x8880 + 0x1111 * b));
+  return d;
+}
+__device__ __forceinline__ int top_of(uint32_t w) {   // largest magnitude of four int8
+  return max(max(abs(signed_byte(w, 0)), abs(signed_byte(w, 1))), max(abs(signed_byte(w, 2)), abs(signed_byte(w, 3))));
+}
+// ceil(8 top / 7), top <= 128.
+__device__ __forceinline__ int step_of(int top) { return (8 * top + 6) / 7; }
+// code + 8 of four values, one in each byte: floor((16 x + 17 step) / (2 step)), the numerator below 4548 and the quotient below 16, by a
+// product with floor(2^24 / (2 step)) + 1 (off by less than 4548 / 2^24 < 1 / (2 step)); 8 where the step is 0.
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, int step) {
+  if (step == 0) return 0x08080808u;
+  const unsigned r = (1u << 23) / (unsigned)step + 1u;
+  uint32_t c = 0;
+#pragma unroll
+  for (int b = 0; b < 4; ++b) c |= ((unsigned)(16 * signed_byte(w, b) + 17 * step) * r >> 24) << (8 * b);
+  return c;
 }
 
-// One warp per (token, head).
-__global__ void __launch_bounds__(256) kv4_append_kernel(Cache c, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
-                                                         const int64_t* slots, int64_t tokens, int* status) {
+// D / 4 lanes take a row of one token and head: four channels each of K and of V, so that loads and stores of codes are runs of words; the
+// lanes with a word's low and high halves are 4 apart in K, D / 8 apart in V.  U rows at a time keep loads in flight: the 20011 tokens
+// x 8 heads x 64 of a prompt take 6 us instead of 12 with one.
+template <int D, int U>
+__global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const int8_t* __restrict__ K, int64_t ldk, const int8_t* __restrict__ V,
+                                                         int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, int* status) {
+  constexpr int L = D / 4, kPer = 256 / L;       // lanes of a row, rows of a CTA
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const int64_t n = tokens * c.heads;
-  for (int64_t i = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) >> 5; i < n; i += ((int64_t)gridDim.x * blockDim.x) >> 5) {
-    const int64_t t = i / c.heads;
-    const int h = (int)(i - t * c.heads);
-    const int64_t slot = slots[t];
-    if (slot < 0) continue;
-    if (slot >> c.page_log >= c.pages) {
-      if (lane == 0) report(status, IVIT_ERR_RANGE);
+  const int l = threadIdx.x & (L - 1);
+  const unsigned r0 = blockIdx.x * (kPer * U) + threadIdx.x / L;
+  uint32_t k[U], v[U];
+  long long slot[U];
+  int h[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const unsigned r = min(r0 + u * kPer, rows - 1), t = r / (unsigned)c.heads;
+    h[u] = (int)(r - t * c.heads);
+    k[u] = *reinterpret_cast<const uint32_t*>(K + t * ldk + h[u] * D + 4 * l);
+    v[u] = *reinterpret_cast<const uint32_t*>(V + t * ldv + h[u] * D + 4 * l);
+    slot[u] = r0 + u * kPer < rows ? slots[t] : -1;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    int kt = top_of(k[u]), vt = top_of(v[u]);
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) kt = max(kt, __shfl_xor_sync(~0u, kt, o));
+#pragma unroll
+    for (int o = 1; o < L; o <<= 1) vt = max(vt, __shfl_xor_sync(~0u, vt, o));
+    const int ks = step_of(kt), vs = step_of(vt);
+    const uint32_t kc = codes_of(k[u], ks), vc = codes_of(v[u], vs);
+    const uint32_t kw = kc | __shfl_down_sync(~0u, kc, 4) << 4, vw = vc | __shfl_down_sync(~0u, vc, L / 2) << 4;
+    if (slot[u] < 0) continue;
+    if (slot[u] >> c.page_log >= c.pages) {
+      if (l == 0) report(status, IVIT_ERR_RANGE);
       continue;
     }
-    const Block b = c.block(slot >> c.page_log, h);
-    const int o = (int)(slot & (c.page - 1));
-    const int8_t* k = K + t * ldk + h * c.d;
-    const int8_t* v = V + t * ldv + h * c.d;
-    int vmax = 0;
-    for (int ch = lane; ch < c.d; ch += 32) vmax = max(vmax, abs((int)v[ch]));
-    vmax = __reduce_max_sync(~0u, vmax);
-    const int vs = (8 * vmax + 6) / 7;
-    for (int p = lane; p < c.d / 2; p += 32)
-      b.vcode(o)[p] = (uint8_t)(kv4_code(v[p], vs) | kv4_code(v[p + c.d / 2], vs) << 4);
-    if (lane == 0) *b.vstep(o) = (uint8_t)vs;
-    const int G = c.d / 32;
-    for (int g = 0; g < G; ++g) {
-      const int x = k[32 * g + lane];
-      const int ks = (8 * __reduce_max_sync(~0u, abs(x)) + 6) / 7;
-      const int lo = kv4_code(x, ks), hi = __shfl_down_sync(~0u, lo, 16);
-      if (lane < 16) b.kcode(o)[4 * (G * (lane >> 2) + g) + (lane & 3)] = (uint8_t)(lo | hi << 4);
-      if (lane == 0) b.kstep(o)[g] = (uint8_t)ks;
-    }
+    const Block b = c.block(slot[u] >> c.page_log, h[u]);
+    const int o = (int)(slot[u] & (c.page - 1)), g = l >> 3;
+    if ((l & 4) == 0) reinterpret_cast<uint32_t*>(b.kcode(o))[D / 32 * (l & 3) + g] = kw;
+    if (l < L / 2) reinterpret_cast<uint32_t*>(b.vcode(o))[l] = vw;
+    if ((l & 7) == 0) b.kstep(o)[g] = (uint8_t)ks;
+    if (l == 1) *b.vstep(o) = (uint8_t)vs;
   }
 }
 
 int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
                       const int64_t* slots, int64_t tokens) {
   if (tokens == 0) return IVIT_OK;
-  LaunchScope ls(ctx, KIND_MOVE, (double)tokens * cache->heads * 3 * cache->d);
-  const int64_t ctas = (tokens * cache->heads + 7) / 8;
-  launch_k(kv4_append_kernel, (int)(ctas < 8 * ctx->sm_count ? ctas : 8 * ctx->sm_count), 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv,
-           slots, tokens, ctx->status_dev);
+  LaunchScope ls(ctx, KIND_MOVE, (double)tokens * cache->heads * (3 * cache->d + cache->d / 32 + 1));
+  const unsigned rows = (unsigned)(tokens * cache->heads);
+  const int per = cache->d == 128 ? 8 : 16;
+  const bool many = rows >= 64u * (unsigned)ctx->sm_count;    // (below, the rows are better spread over the SMs)
+  const unsigned grid = (rows + (many ? 4 * per : per) - 1) / (many ? 4 * per : per);
+  auto go = [&](auto k) { launch_k(k, grid, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, ctx->status_dev); };
+  if (cache->d == 128) many ? go(kv4_append_kernel<128, 4>) : go(kv4_append_kernel<128, 1>);
+  else many ? go(kv4_append_kernel<64, 4>) : go(kv4_append_kernel<64, 1>);
   return ls.done();
 }
 
@@ -109,12 +137,26 @@ __device__ __forceinline__ int evict_len(const EvictArgs& a, int b) {
   return len;
 }
 
-// One CTA per (sequence, head): finds the smallest weight that stays by its bytes from the top, then lists the keys in order.
-__global__ void __launch_bounds__(1024) kv4_select_kernel(EvictArgs a) {
-  __shared__ unsigned hist[256];
+// First digit of a weight's order: its bit length and the five bits behind the leading one.  Accumulated weights are spread over many powers
+// of two: digits of that kind leave few keys in the one that holds the threshold, and few lanes that count in the same place.
+constexpr int kDigits = 2048;
+__device__ __forceinline__ int first_digit(unsigned long long k) {
+  const int e = 64 - __clzll((long long)k);
+  return e <= 5 ? (int)k : ((e - 5) << 5) + (int)((k >> (e - 6)) & 31);
+}
+
+// One CTA for each (sequence, head), its warps on runs of keys one behind the other (kRegs: of at most 512 keys, held in registers; else
+// read again in each pass).  Finds the smallest weight that stays, then lists the keys in order:
+//   1. counts of the first digits, and the digit in which `need` of the largest are reached;
+//   2. the keys of that digit: up to 1024 of them are ranked against one another, more (many equal weights) are told apart byte by byte;
+//   3. each warp counts what stays of its run, and writes it behind what stays of the runs in front.
+template <bool kRegs>
+__global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
+  constexpr int kKeys = 16;
+  __shared__ unsigned hist[kDigits];
+  __shared__ unsigned long long list[1024];
+  __shared__ unsigned count, need_s, digit_s, sums[32], ties_s[32];
   __shared__ unsigned long long prefix_s;
-  __shared__ unsigned need_s;
-  __shared__ unsigned sums[32][2];
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -127,102 +169,186 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(EvictArgs a) {
     return;
   }
   const int64_t* w = a.w + bh * a.ldw;
-  const int lo = a.sinks, hi = len - a.recent;      // candidates
+  const int lo = a.sinks, hi = len - a.recent;               // candidates
   unsigned need = (unsigned)(a.keep - a.sinks - a.recent);   // of them
-  unsigned long long prefix = 0;
-  for (int shift = 56; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
+  const int run = (len + 1023) / 1024 * 32, j0 = min(len, warp * run), j1 = min(len, j0 + run);
+  unsigned long long keys[kRegs ? kKeys : 1];
+  if (kRegs) {
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+      const int j = j0 + 32 * i + lane;
+      keys[kRegs ? i : 0] = j < j1 ? order_key(w[j]) : 0;
+    }
+  }
+  // f(index, key, there) for the warp's keys, 32 at a time
+  auto each = [&](auto f) {
+    if (kRegs) {
+#pragma unroll
+      for (int i = 0; i < kKeys; ++i)
+        if (j0 + 32 * i < j1) f(j0 + 32 * i + lane, keys[kRegs ? i : 0], j0 + 32 * i + lane < j1);
+    } else {
+      for (int jb = j0; jb < j1; jb += 32) f(jb + lane, jb + lane < j1 ? order_key(w[jb + lane]) : 0ull, jb + lane < j1);
+    }
+  };
+  unsigned long long prefix = ~0ull;   // need == 0: nothing is above, nothing equal stays
+  if (need > 0) {
+    // (order_key flips the sign: zero is 2^63.  The digits are those of the weight itself, negative ones all in the first.)
+    auto digit = [&](unsigned long long k) { return k >> 63 ? first_digit(k & ~(1ull << 63)) : 0; };
+    for (int i = tid; i < kDigits; i += 1024) hist[i] = 0;
+    if (tid == 0) count = 0;
     __syncthreads();
-    for (int j = lo + tid; j < hi; j += 1024) {
-      const unsigned long long k = order_key(w[j]);
-      if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1u);
+    unsigned none = 0;   // digit 0 (weights of zero are common): counted lane by lane
+    each([&](int j, unsigned long long k, bool) {
+      if (j >= lo && j < hi) {
+        const int g = digit(k);
+        if (g) atomicAdd(&hist[g], 1u);
+        else ++none;
+      }
+    });
+    none = __reduce_add_sync(~0u, none);
+    if (lane == 0 && none) atomicAdd(&hist[0], none);
+    __syncthreads();
+    {  // thread t has digits 2047 - 2 t and 2046 - 2 t: sums over what is above
+      const unsigned x = hist[kDigits - 1 - 2 * tid], y = hist[kDigits - 2 - 2 * tid];
+      unsigned s = x + y;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned v = __shfl_up_sync(~0u, s, o);
+        if (lane >= o) s += v;
+      }
+      if (lane == 31) sums[warp] = s;
+      __syncthreads();
+      unsigned front = lane < warp ? sums[lane] : 0;
+      front = __reduce_add_sync(~0u, front) + s - x - y;      // above this thread's two digits
+      if (front < need && need <= front + x) { digit_s = kDigits - 1 - 2 * tid; need_s = need - front; }
+      else if (front + x < need && need <= front + x + y) { digit_s = kDigits - 2 - 2 * tid; need_s = need - front - x; }
     }
     __syncthreads();
-    if (tid == 0) {
-      unsigned n = need;
-      int v = 255;
-      while (v > 0 && hist[v] < n) n -= hist[v--];
-      prefix_s = prefix | (unsigned long long)v << shift;
-      need_s = n;
-    }
-    __syncthreads();
-    prefix = prefix_s;
+    const int at = (int)digit_s;
     need = need_s;
-  }
-  // weights above `prefix` stay, and the first `need` of those equal to it
-  int base = 0, ties = 0;
-  for (int j0 = 0; j0 < len; j0 += 1024) {
-    const int j = j0 + tid;
-    bool above = false, tie = false;
-    if (j < len) {
-      const unsigned long long k = order_key(w[j]);
-      above = j < lo || j >= hi || k > prefix;
-      tie = !above && k == prefix;
+    const unsigned in_digit = hist[at];
+    if (in_digit <= 1024) {
+      each([&](int j, unsigned long long k, bool) {
+        if (j >= lo && j < hi && digit(k) == at) list[atomicAdd(&count, 1u)] = k;
+      });
+      __syncthreads();
+      if (tid < (int)in_digit) {
+        const unsigned long long k = list[tid];
+        unsigned above = 0, same = 0;
+        for (unsigned i = 0; i < in_digit; ++i) {
+          above += list[i] > k;
+          same += list[i] == k;
+        }
+        if (above < need && need <= above + same) { prefix_s = k; need_s = need - above; }   // (equal keys all say the same)
+      }
+      __syncthreads();
+      prefix = prefix_s;
+      need = need_s;
+    } else {
+      prefix = 0;
+      for (int shift = 56; shift >= 0; shift -= 8) {
+        __syncthreads();
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+        each([&](int j, unsigned long long k, bool) {
+          const bool in = j >= lo && j < hi && digit(k) == at && (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)));
+          const unsigned v = in ? (unsigned)(k >> shift) & 255u : 256u, peers = __match_any_sync(~0u, v);   // (many are equal: one addition for all of a warp)
+          if (in && lane == __ffs(peers) - 1) atomicAdd(&hist[v], (unsigned)__popc(peers));
+        });
+        __syncthreads();
+        if (tid == 0) {
+          unsigned n = need;
+          int v = 255;
+          while (v > 0 && hist[v] < n) n -= hist[v--];
+          prefix_s = prefix | (unsigned long long)v << shift;
+          need_s = n;
+        }
+        __syncthreads();
+        prefix = prefix_s;
+        need = need_s;
+      }
     }
-    const unsigned ma = __ballot_sync(~0u, above), mt = __ballot_sync(~0u, tie), below = (1u << lane) - 1;
-    if (lane == 0) { sums[warp][0] = __popc(ma); sums[warp][1] = __popc(mt); }
-    __syncthreads();
-    int nt = ties + __popc(mt & below), na = base + __popc(ma & below), all_a = 0, all_t = 0;
-    for (int i = 0; i < 32; ++i) {
-      if (i < warp) { na += sums[i][0]; nt += sums[i][1]; }
-      all_a += sums[i][0];
-      all_t += sums[i][1];
-    }
-    // (base counts the keys above only; ties in front of this one that stay: min(nt, need))
-    const int at = na + min(nt, (int)need);
-    if (above || (tie && nt < (int)need)) kept[at] = j;
-    base += all_a;
-    ties += all_t;
-    __syncthreads();
   }
+  // ---- weights above `prefix` stay, and the first `need` of those equal to it
+  unsigned above = 0, ties = 0;
+  each([&](int j, unsigned long long k, bool there) {
+    const bool up = there && (j < lo || j >= hi || k > prefix);
+    above += __popc(__ballot_sync(~0u, up));
+    ties += __popc(__ballot_sync(~0u, there && !up && k == prefix));
+  });
+  __syncthreads();   // (sums was read above)
+  if (lane == 0) { sums[warp] = above; ties_s[warp] = ties; }
+  __syncthreads();
+  unsigned at_above = __reduce_add_sync(~0u, lane < warp ? sums[lane] : 0), at_ties = __reduce_add_sync(~0u, lane < warp ? ties_s[lane] : 0);
+  const unsigned below = (1u << lane) - 1;
+  each([&](int j, unsigned long long k, bool there) {
+    const bool up = there && (j < lo || j >= hi || k > prefix), tie = there && !up && k == prefix;
+    const unsigned mu = __ballot_sync(~0u, up), mt = __ballot_sync(~0u, tie);
+    const unsigned t = at_ties + __popc(mt & below);
+    if (up || (tie && t < need)) kept[at_above + __popc(mu & below) + min(t, need)] = j;
+    at_above += __popc(mu);
+    at_ties += __popc(mt);
+  });
 }
 
-// One CTA per (sequence, head) moves the rows in order: rows that are read later lie behind those that are written.
-__global__ void __launch_bounds__(256) kv4_compact_kernel(EvictArgs a) {
+// Moves the rows that stay, 16 bytes of codes to a thread.  kOrdered (in place): one CTA for each (sequence, head), group of rows behind
+// group of rows, each loaded before any of it is stored; rows that are read later lie behind those that are written.  Else the groups of rows are shared out.
+template <int D, bool kOrdered>
+__global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const EvictArgs a) {
+  constexpr int kParts = D / 32, kLanes = 2 * kParts, U = 4;       // chunks of a row of K or V; threads of a row; rows of a thread
+  constexpr int kThreads = kOrdered ? 512 : 256, kRows = kThreads / kLanes;
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x;
-  const int h = blockIdx.x, b = blockIdx.y, d = a.c.d;
+  const int tid = threadIdx.x, sub = tid % kLanes, part = sub % kParts;
+  const int h = blockIdx.y, b = blockIdx.z;
+  const bool value = sub >= kParts;
   const int n = min(evict_len(a, b), a.keep);
   const int64_t bh = (int64_t)b * a.c.heads + h;
-  for (int i0 = 0; i0 < n; i0 += 256) {
-    const int i = i0 + tid;
-    Block s{nullptr, 0, 0}, t{nullptr, 0, 0};
-    int so = 0, to = 0;
-    int64_t w = 0;
-    if (i < n) {
-      const int j = a.kept[bh * a.keep + i];
-      const int64_t sp = a.table[b * a.ldtable + (j >> a.c.page_log)], dp = a.dst[b * a.ld_dst + (i >> a.c.page_log)];
-      w = a.w[bh * a.ldw + j];
-      so = j & (a.c.page - 1);
-      to = i & (a.c.page - 1);
-      if (sp >= 0 && sp < a.c.pages && dp >= 0 && dp < a.c.pages) { s = a.c.block(sp, h); t = a.c.block(dp, h); }
-      else report(a.status, IVIT_ERR_RANGE);
-    }
-    uint4 k[4], v[4];
-    unsigned ks = 0, vs = 0;
-    if (s.p) {
-      for (int q = 0; q < d / 32; ++q) {
-        k[q] = reinterpret_cast<const uint4*>(s.kcode(so))[q];
-        v[q] = reinterpret_cast<const uint4*>(s.vcode(so))[q];
-        ks |= (unsigned)s.kstep(so)[q] << (8 * q);
+  for (int i0 = blockIdx.x * (kRows * U); i0 < n; i0 += gridDim.x * (kRows * U)) {
+    uint4 x[U];
+    uint32_t st[U];
+    int64_t w[U];
+    uint8_t* to[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kRows + tid / kLanes;
+      to[u] = nullptr;
+      if (i < n) {
+        const int j = a.kept[bh * a.keep + i];
+        const int64_t sp = a.table[b * a.ldtable + (j >> a.c.page_log)], dp = a.dst[b * a.ld_dst + (i >> a.c.page_log)];
+        const int o = j & (a.c.page - 1);
+        if (sub == 0) w[u] = a.w[bh * a.ldw + j];
+        if (sp >= 0 && sp < a.c.pages && dp >= 0 && dp < a.c.pages) {
+          const Block s = a.c.block(sp, h);
+          to[u] = a.c.block(dp, h).p;
+          x[u] = reinterpret_cast<const uint4*>(value ? s.vcode(o) : s.kcode(o))[part];
+          if (sub == 0) st[u] = D == 128 ? *reinterpret_cast<const uint32_t*>(s.kstep(o)) : *reinterpret_cast<const uint16_t*>(s.kstep(o));
+          if (sub == kParts) st[u] = *s.vstep(o);
+        } else if (sub == 0) {
+          report(a.status, IVIT_ERR_RANGE);
+        }
       }
-      vs = *s.vstep(so);
     }
-    __syncthreads();
-    if (s.p) {
-      for (int q = 0; q < d / 32; ++q) {
-        reinterpret_cast<uint4*>(t.kcode(to))[q] = k[q];
-        reinterpret_cast<uint4*>(t.vcode(to))[q] = v[q];
-        t.kstep(to)[q] = (uint8_t)(ks >> (8 * q));
+    if (kOrdered) __syncthreads();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kRows + tid / kLanes;
+      if (i < n && sub == 0) a.w_out[bh * a.ldw_out + i] = w[u];
+      if (to[u]) {
+        const Block t{to[u], D, a.c.page};
+        const int o = i & (a.c.page - 1);
+        reinterpret_cast<uint4*>(value ? t.vcode(o) : t.kcode(o))[part] = x[u];
+        if (sub == 0) {
+          if (D == 128) *reinterpret_cast<uint32_t*>(t.kstep(o)) = st[u];
+          else *reinterpret_cast<uint16_t*>(t.kstep(o)) = (uint16_t)st[u];
+        }
+        if (sub == kParts) *t.vstep(o) = (uint8_t)st[u];
       }
-      *t.vstep(to) = (uint8_t)vs;
     }
-    if (i < n) a.w_out[bh * a.ldw_out + i] = w;
-    __syncthreads();
+    if (kOrdered) __syncthreads();
   }
-  for (int64_t i = n + tid; i < a.ldw_out; i += 256) a.w_out[bh * a.ldw_out + i] = 0;
-  if (h == 0 && tid == 0) a.new_lens[b] = n;
+  for (int64_t i = n + (int64_t)blockIdx.x * kThreads + tid; i < a.ldw_out; i += (int64_t)gridDim.x * kThreads) a.w_out[bh * a.ldw_out + i] = 0;
+  if (h == 0 && blockIdx.x == 0 && tid == 0) a.new_lens[b] = n;
 }
 
 int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens, const int32_t* table,
@@ -231,15 +357,21 @@ int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* 
   if (seqs == 0) return IVIT_OK;
   const EvictArgs a{to_dev(cache), weights, ldw, lens, table, ldtable, dst_table, ld_dst, weights_out, ldw_out, kept, new_lens, (int)max_len,
                     (int)keep, (int)sinks, (int)recent, ctx->status_dev};
-  const dim3 grid((unsigned)cache->heads, (unsigned)seqs);
   int rc;
   {
     LaunchScope ls(ctx, KIND_MOVE, 8.0 * seqs * cache->heads * max_len);
-    launch_k(kv4_select_kernel, grid, 1024, 0, ctx->stream, a);
+    const dim3 grid((unsigned)cache->heads, (unsigned)seqs);
+    if (max_len <= 16384) launch_k(kv4_select_kernel<true>, grid, 1024, 0, ctx->stream, a);
+    else launch_k(kv4_select_kernel<false>, grid, 1024, 0, ctx->stream, a);
     if ((rc = ls.done())) return rc;
   }
   LaunchScope ls(ctx, KIND_MOVE, 2.0 * seqs * cache->heads * keep * (cache->d + cache->d / 32 + 9));
-  launch_k(kv4_compact_kernel, grid, 256, 0, ctx->stream, a);
+  // in place (of the pages, or of the weights): in order
+  const bool ordered = dst_table == table || weights_out == weights;
+  const int64_t rows = keep < max_len ? keep : max_len, per = 4 * 256 / (cache->d / 16);
+  const dim3 grid(ordered ? 1u : (unsigned)(rows > per ? (rows + per - 1) / per : 1), (unsigned)cache->heads, (unsigned)seqs);
+  if (cache->d == 128) ordered ? launch_k(kv4_compact_kernel<128, true>, grid, 512, 0, ctx->stream, a) : launch_k(kv4_compact_kernel<128, false>, grid, 256, 0, ctx->stream, a);
+  else ordered ? launch_k(kv4_compact_kernel<64, true>, grid, 512, 0, ctx->stream, a) : launch_k(kv4_compact_kernel<64, false>, grid, 256, 0, ctx->stream, a);
   return ls.done();
 }
 

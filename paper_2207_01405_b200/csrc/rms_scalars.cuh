@@ -38,7 +38,7 @@ IVIT_ISQRT_FN RmsRow rms_row(unsigned long long V, int M_ln) {
   RmsRow k{0, 0};
   if (sd) {
     k.e = bits64(sd);
-    k.F = (int)((1ull << (M_ln + k.e)) / sd);
+    k.F = M_ln + k.e < 32 ? (int)((1u << (M_ln + k.e)) / sd) : (int)((1ull << (M_ln + k.e)) / sd);   // (the 32-bit division is a quarter of the other)
   }
   return k;
 }
