@@ -18,16 +18,14 @@ struct Block {
 struct Cache {
   uint8_t* data;
   int64_t pages;
-  int heads, d, page, page_log;
-  __device__ __forceinline__ Block block(int64_t pg, int h) const {
-    return Block{data + (pg * heads + h) * ((int64_t)page * (d + d / 32 + 1)), d, page};
-  }
+  int heads, d, page, page_log, block_bytes;
+  __device__ __forceinline__ Block block(int pg, int h) const { return Block{data + ((int64_t)pg * heads + h) * block_bytes, d, page}; }
 };
 
 static Cache to_dev(const ivit_kv4_cache* c) {
   int lg = 0;
   while ((1 << lg) < c->page) ++lg;
-  return Cache{c->data, c->pages, (int)c->heads, (int)c->d, (int)c->page, lg};
+  return Cache{c->data, c->pages, (int)c->heads, (int)c->d, (int)c->page, lg, (int)(c->page * (c->d + c->d / 32 + 1))};
 }
 
 // ---------------------------------------------------------------- append
@@ -43,59 +41,81 @@ __device__ __forceinline__ int top_of(uint32_t w) {   // largest magnitude of fo
 // ceil(8 top / 7), top <= 128.
 __device__ __forceinline__ int step_of(int top) { return (8 * top + 6) / 7; }
 // code + 8 of four values, one in each byte: floor((16 x + 17 step) / (2 step)), the numerator below 4548 and the quotient below 16, by a
-// product with floor(2^24 / (2 step)) + 1 (off by less than 4548 / 2^24 < 1 / (2 step)); 8 where the step is 0.
-__device__ __forceinline__ uint32_t codes_of(uint32_t w, int step) {
-  if (step == 0) return 0x08080808u;
-  const unsigned r = (1u << 23) / (unsigned)step + 1u;
-  uint32_t c = 0;
+// product with r = floor(2^23 / step) + 1 (off by less than 4548 / 2^24 < 1 / (2 step)), whose upper byte is the quotient.  r = 0 and
+// eight in the end where the step is 0.
+__device__ __forceinline__ uint32_t codes_of(uint32_t w, int step, unsigned r) {
+  unsigned p[4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) c |= ((unsigned)(16 * signed_byte(w, b) + 17 * step) * r >> 24) << (8 * b);
-  return c;
+  for (int b = 0; b < 4; ++b) p[b] = (unsigned)(16 * signed_byte(w, b) + 17 * step) * r;
+  const uint32_t c = __byte_perm(__byte_perm(p[0], p[1], 0x0073), __byte_perm(p[2], p[3], 0x0073), 0x5410);
+  return step ? c : 0x08080808u;
 }
 
-// D / 4 lanes take a row of one token and head: four channels each of K and of V, so that loads and stores of codes are runs of words; the
-// lanes with a word's low and high halves are 4 apart in K, D / 8 apart in V.  U rows at a time keep loads in flight: the 20011 tokens
-// x 8 heads x 64 of a prompt take 6 us instead of 12 with one.
+struct HeadDiv {   // quotient of n < 2^31 by the number of heads: the product's upper word, shifted (multiplier of 32 bits, rounded up)
+  unsigned d, m;
+  int s;
+};
+static HeadDiv head_div(unsigned d) {
+  int l = 0;
+  while ((1u << l) < d) ++l;
+  return HeadDiv{d, d > 1 ? (unsigned)(((1ull << (31 + l)) + d - 1) / d) : 0u, l - 1};
+}
+
+// D / 8 lanes take a row of one token and head: eight channels each of K and of V, so that loads and stores of codes are runs of double
+// words; the lanes with a word's low and high halves are 2 apart in K, D / 16 apart in V.  U rows at a time keep loads in flight.  What
+// bounds it is the issue of instructions; with four channels a lane, and a division for each step and for the head, it took twice the time.
 template <int D, int U>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const int8_t* __restrict__ K, int64_t ldk, const int8_t* __restrict__ V,
-                                                         int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, int* status) {
-  constexpr int L = D / 4, kPer = 256 / L;       // lanes of a row, rows of a CTA
+                                                         int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, HeadDiv by_heads, int* status) {
+  constexpr int L = D / 8, kPer = 256 / L;       // lanes of a row, rows of a CTA
+  __shared__ unsigned recip[256];
+  if (threadIdx.x < 148) recip[threadIdx.x] = threadIdx.x ? (1u << 23) / threadIdx.x + 1u : 0u;
   pdl_wait();
   pdl_trigger();
   const int l = threadIdx.x & (L - 1);
   const unsigned r0 = blockIdx.x * (kPer * U) + threadIdx.x / L;
-  uint32_t k[U], v[U];
+  uint2 k[U], v[U];
   long long slot[U];
   int h[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const unsigned r = min(r0 + u * kPer, rows - 1), t = r / (unsigned)c.heads;
-    h[u] = (int)(r - t * c.heads);
-    k[u] = *reinterpret_cast<const uint32_t*>(K + t * ldk + h[u] * D + 4 * l);
-    v[u] = *reinterpret_cast<const uint32_t*>(V + t * ldv + h[u] * D + 4 * l);
+    const unsigned r = min(r0 + u * kPer, rows - 1), t = by_heads.d == 1 ? r : __umulhi(r, by_heads.m) >> by_heads.s;
+    h[u] = (int)(r - t * by_heads.d);
+    k[u] = *reinterpret_cast<const uint2*>(K + t * ldk + (h[u] * D + 8 * l));
+    v[u] = *reinterpret_cast<const uint2*>(V + t * ldv + (h[u] * D + 8 * l));
     slot[u] = r0 + u * kPer < rows ? slots[t] : -1;
   }
+  __syncthreads();
+  const int vcode = c.page * (D / 2 + D / 32), kstep = c.page * (D / 2), vstep = c.page * (D + D / 32);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    int kt = top_of(k[u]), vt = top_of(v[u]);
+    int kt = max(top_of(k[u].x), top_of(k[u].y)), vt = max(top_of(v[u].x), top_of(v[u].y));
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) kt = max(kt, __shfl_xor_sync(~0u, kt, o));
+    for (int o = 1; o < 4; o <<= 1) kt = max(kt, __shfl_xor_sync(~0u, kt, o));
 #pragma unroll
     for (int o = 1; o < L; o <<= 1) vt = max(vt, __shfl_xor_sync(~0u, vt, o));
     const int ks = step_of(kt), vs = step_of(vt);
-    const uint32_t kc = codes_of(k[u], ks), vc = codes_of(v[u], vs);
-    const uint32_t kw = kc | __shfl_down_sync(~0u, kc, 4) << 4, vw = vc | __shfl_down_sync(~0u, vc, L / 2) << 4;
+    const unsigned kr = recip[ks], vr = recip[vs];
+    uint32_t k0 = codes_of(k[u].x, ks, kr), k1 = codes_of(k[u].y, ks, kr), v0 = codes_of(v[u].x, vs, vr), v1 = codes_of(v[u].y, vs, vr);
+    k0 |= __shfl_down_sync(~0u, k0, 2) << 4;
+    k1 |= __shfl_down_sync(~0u, k1, 2) << 4;
+    v0 |= __shfl_down_sync(~0u, v0, L / 2) << 4;
+    v1 |= __shfl_down_sync(~0u, v1, L / 2) << 4;
     if (slot[u] < 0) continue;
     if (slot[u] >> c.page_log >= c.pages) {
       if (l == 0) report(status, IVIT_ERR_RANGE);
       continue;
     }
-    const Block b = c.block(slot[u] >> c.page_log, h[u]);
-    const int o = (int)(slot[u] & (c.page - 1)), g = l >> 3;
-    if ((l & 4) == 0) reinterpret_cast<uint32_t*>(b.kcode(o))[D / 32 * (l & 3) + g] = kw;
-    if (l < L / 2) reinterpret_cast<uint32_t*>(b.vcode(o))[l] = vw;
-    if ((l & 7) == 0) b.kstep(o)[g] = (uint8_t)ks;
-    if (l == 1) *b.vstep(o) = (uint8_t)vs;
+    uint8_t* p = c.block((int)(slot[u] >> c.page_log), h[u]).p;
+    const int o = (int)slot[u] & (c.page - 1), g = l >> 2;
+    if ((l & 2) == 0) {                          // words 2 (l & 1) and the next one of group g
+      uint32_t* dst = reinterpret_cast<uint32_t*>(p + o * (D / 2)) + D / 32 * (2 * (l & 1)) + g;
+      dst[0] = k0;
+      dst[D / 32] = k1;
+    }
+    if (l < L / 2) *reinterpret_cast<uint2*>(p + vcode + o * (D / 2) + 8 * l) = make_uint2(v0, v1);
+    if ((l & 3) == 0) p[kstep + o * (D / 32) + g] = (uint8_t)ks;
+    if (l == 1) p[vstep + o] = (uint8_t)vs;
   }
 }
 
@@ -104,10 +124,12 @@ int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* 
   if (tokens == 0) return IVIT_OK;
   LaunchScope ls(ctx, KIND_MOVE, (double)tokens * cache->heads * (3 * cache->d + cache->d / 32 + 1));
   const unsigned rows = (unsigned)(tokens * cache->heads);
-  const int per = cache->d == 128 ? 8 : 16;
+  const int per = cache->d == 128 ? 16 : 32;
   const bool many = rows >= 64u * (unsigned)ctx->sm_count;    // (below, the rows are better spread over the SMs)
   const unsigned grid = (rows + (many ? 4 * per : per) - 1) / (many ? 4 * per : per);
-  auto go = [&](auto k) { launch_k(k, grid, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, ctx->status_dev); };
+  auto go = [&](auto k) {
+    launch_k(k, grid, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, head_div((unsigned)cache->heads), ctx->status_dev);
+  };
   if (cache->d == 128) many ? go(kv4_append_kernel<128, 4>) : go(kv4_append_kernel<128, 1>);
   else many ? go(kv4_append_kernel<64, 4>) : go(kv4_append_kernel<64, 1>);
   return ls.done();
@@ -148,7 +170,7 @@ __device__ __forceinline__ int first_digit(unsigned long long k) {
 // One CTA for each (sequence, head), its warps on runs of keys one behind the other (kRegs: of at most 512 keys, held in registers; else
 // read again in each pass).  Finds the smallest weight that stays, then lists the keys in order:
 //   1. counts of the first digits, and the digit in which `need` of the largest are reached;
-//   2. the keys of that digit: up to 1024 of them are ranked against one another, more (many equal weights) are told apart byte by byte;
+//   2. the keys of that digit: one value (small weights; all equal) needs no more, up to 1024 are ranked against one another, more are told apart byte by byte;
 //   3. each warp counts what stays of its run, and writes it behind what stays of the runs in front.
 template <bool kRegs>
 __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
@@ -156,7 +178,7 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
   __shared__ unsigned hist[kDigits];
   __shared__ unsigned long long list[1024];
   __shared__ unsigned count, need_s, digit_s, sums[32], ties_s[32];
-  __shared__ unsigned long long prefix_s;
+  __shared__ unsigned long long prefix_s, low_s, high_s;
   pdl_wait();
   pdl_trigger();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -195,7 +217,8 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
     // (order_key flips the sign: zero is 2^63.  The digits are those of the weight itself, negative ones all in the first.)
     auto digit = [&](unsigned long long k) { return k >> 63 ? first_digit(k & ~(1ull << 63)) : 0; };
     for (int i = tid; i < kDigits; i += 1024) hist[i] = 0;
-    if (tid == 0) count = 0;
+    if (tid == 0) count = 0, low_s = ~0ull, high_s = 0;
+    bool negative = false;
     __syncthreads();
     unsigned none = 0;   // digit 0 (weights of zero are common): counted lane by lane
     each([&](int j, unsigned long long k, bool) {
@@ -203,8 +226,10 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
         const int g = digit(k);
         if (g) atomicAdd(&hist[g], 1u);
         else ++none;
+        negative |= !(k >> 63);
       }
     });
+    negative = __syncthreads_or(negative) != 0;
     none = __reduce_add_sync(~0u, none);
     if (lane == 0 && none) atomicAdd(&hist[0], none);
     __syncthreads();
@@ -227,7 +252,9 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
     const int at = (int)digit_s;
     need = need_s;
     const unsigned in_digit = hist[at];
-    if (in_digit <= 1024) {
+    if (at < 64 && !(at == 0 && negative)) {
+      prefix = order_key(at);              // (digits below 64 are the weights themselves)
+    } else if (in_digit <= 1024) {
       each([&](int j, unsigned long long k, bool) {
         if (j >= lo && j < hi && digit(k) == at) list[atomicAdd(&count, 1u)] = k;
       });
@@ -245,8 +272,15 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
       prefix = prefix_s;
       need = need_s;
     } else {
-      prefix = 0;
-      for (int shift = 56; shift >= 0; shift -= 8) {
+      // (all of them equal: the one value)
+      unsigned long long low = ~0ull, high = 0;
+      each([&](int j, unsigned long long k, bool) {
+        if (j >= lo && j < hi && digit(k) == at) low = min(low, k), high = max(high, k);
+      });
+      if (low <= high) atomicMin(&low_s, low), atomicMax(&high_s, high);
+      __syncthreads();
+      prefix = low_s;
+      for (int shift = low_s == high_s ? -8 : 56; shift >= 0; shift -= 8) {
         __syncthreads();
         if (tid < 256) hist[tid] = 0;
         __syncthreads();
@@ -260,7 +294,7 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
           unsigned n = need;
           int v = 255;
           while (v > 0 && hist[v] < n) n -= hist[v--];
-          prefix_s = prefix | (unsigned long long)v << shift;
+          prefix_s = (shift == 56 ? 0ull : prefix) | (unsigned long long)v << shift;
           need_s = n;
         }
         __syncthreads();
@@ -308,25 +342,34 @@ __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const
     uint4 x[U];
     uint32_t st[U];
     int64_t w[U];
-    uint8_t* to[U];
+    uint8_t *to[U];
+    int j[U], sp[U], dp[U];
+    // (index, pages, rows: three loads behind one another, each of them for all U rows at once)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kRows + tid / kLanes;
-      to[u] = nullptr;
-      if (i < n) {
-        const int j = a.kept[bh * a.keep + i];
-        const int64_t sp = a.table[b * a.ldtable + (j >> a.c.page_log)], dp = a.dst[b * a.ld_dst + (i >> a.c.page_log)];
-        const int o = j & (a.c.page - 1);
-        if (sub == 0) w[u] = a.w[bh * a.ldw + j];
-        if (sp >= 0 && sp < a.c.pages && dp >= 0 && dp < a.c.pages) {
-          const Block s = a.c.block(sp, h);
-          to[u] = a.c.block(dp, h).p;
-          x[u] = reinterpret_cast<const uint4*>(value ? s.vcode(o) : s.kcode(o))[part];
-          if (sub == 0) st[u] = D == 128 ? *reinterpret_cast<const uint32_t*>(s.kstep(o)) : *reinterpret_cast<const uint16_t*>(s.kstep(o));
-          if (sub == kParts) st[u] = *s.vstep(o);
-        } else if (sub == 0) {
-          report(a.status, IVIT_ERR_RANGE);
-        }
+      const int i = min(i0 + u * kRows + tid / kLanes, n - 1);
+      j[u] = a.kept[bh * a.keep + i];
+      dp[u] = a.dst[b * a.ld_dst + (i >> a.c.page_log)];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) sp[u] = a.table[b * a.ldtable + (j[u] >> a.c.page_log)];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kRows + tid / kLanes, o = j[u] & (a.c.page - 1);
+      const bool there = i < n && sp[u] >= 0 && sp[u] < a.c.pages && dp[u] >= 0 && dp[u] < a.c.pages;
+      const Block s = a.c.block(there ? sp[u] : 0, h);
+      to[u] = there ? a.c.block(dp[u], h).p : nullptr;
+      x[u] = make_uint4(0, 0, 0, 0);
+      st[u] = 0;
+      w[u] = 0;
+      if (there) {
+        x[u] = reinterpret_cast<const uint4*>(value ? s.vcode(o) : s.kcode(o))[part];
+        if (sub == 0) st[u] = D == 128 ? *reinterpret_cast<const uint32_t*>(s.kstep(o)) : *reinterpret_cast<const uint16_t*>(s.kstep(o));
+        if (sub == kParts) st[u] = *s.vstep(o);
+      }
+      if (sub == 0 && i < n) {
+        w[u] = a.w[bh * a.ldw + j[u]];
+        if (!there) report(a.status, IVIT_ERR_RANGE);
       }
     }
     if (kOrdered) __syncthreads();

@@ -2,6 +2,8 @@
 #include "common.cuh"
 #include "rms_scalars.cuh"
 
+#include <type_traits>
+
 namespace ivit {
 
 constexpr int kStreamMax = 1 << 20;   // bound of an int32 stream: its squares sum to less than 2^55
@@ -19,11 +21,8 @@ struct RmsArgs {
   int xvec, gvec;    // per-channel scales that can be read four channels at a time
 };
 
-__device__ __forceinline__ int mad_hi(int a, int b, int c) {
-  int d;
-  asm("mad.hi.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
+// (one instruction with the addend needs it in a register pair of its own, and took longer)
+__device__ __forceinline__ int mul_hi_add(int a, int b, int c) { return __mulhi(a, b) + c; }
 __device__ __forceinline__ int add_sat(int a, int b) {
   int d;
   asm("add.sat.s32 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
@@ -43,24 +42,23 @@ __device__ __forceinline__ int pack4(int x0, int x1, int x2, int x3) {   // satu
 }
 
 // Requantisation of values below 2^(31 - kUp) in magnitude as a high product word, an addition and a shift: the value comes in times 2^kUp,
-// which makes the shift s + kUp; from 33 on the rounding constant is a whole number in the product's upper word.  Where all values
-// round to zero (|v m| < 2^(62 - kUp) <= 2^(s - 1)) the constants are zeros.  kUp = 0 has no such form for s = 31 and 32 (`wide`).
+// which makes the shift s + kUp; from 33 on the rounding constant is a whole number in the product's upper word.  A shift of that word beyond 31
+// stays 31: then all values round to zero, and so does the sum of the word (2^30 in magnitude at most, not reached by positive ones) and 2^30.
+// kUp = 0 has no such form for s = 31 and 32 (`wide`).
 template <int kUp>
 struct Requant {
   int m, add, sh;
   bool wide;
   __device__ __forceinline__ void set(int mult, int shift) {
-    const int s = clamp_shift(shift) + kUp;
-    wide = s < 33;
-    const bool none = s - 32 > 31;          // kUp = 2: s >= 62; kUp = 24: s >= 40
-    m = none ? 0 : mult;
-    sh = none ? 0 : s - 32;
-    add = none || wide ? 0 : 1 << (sh - 1);
-    if (wide) sh = s;
+    const int s = clamp_shift(shift);
+    wide = kUp == 0 && s < 33;
+    m = mult;
+    sh = wide ? s : min(s + (kUp - 32), 31);
+    add = 1 << ((sh - 1) & 31);
   }
   __device__ __forceinline__ int operator()(int v) const {
     if (kUp == 0 && wide) return rq(v, m, sh);
-    return mad_hi(v, m, add) >> sh;
+    return mul_hi_add(v, m, add) >> sh;
   }
 };
 
@@ -80,51 +78,50 @@ __device__ __forceinline__ void scale_of(const ScaleDev& s, int vec, int word, i
 }
 
 // A CTA takes R rows; its threads hold WPT words of four channels of each, from the loads to the output: a row is read once.  Two
-// passes over what the registers hold, with the sum of squares between them (and a third behind the maximum of |z| where
-// rows get scales of their own).  R = 4 where there are rows enough: the constants of the channels (10 bytes for each, more than an
-// int8 row's own 4) are fetched and prepared once for four rows.  The int8 form takes about 14 instructions for a value: byte, mad.hi
-// and shift for each of the three requantisations, half a saturating pack twice, a quarter of a dp4a, multiply-add and shift for y.
-// XI, HI: x, res are int32 (HI = -1: no residual).
-template <int XI, int HI, int WPT, int R>
+// passes over what the registers hold, with the sum of squares between them (kDyn: and a third behind the maximum of |z|, where
+// rows get scales of their own).  Many rows are taken eight (int32 streams: four) at a time: the constants of the channels (10 bytes
+// for each, more than an int8 row's own 4) are fetched and prepared once for all of them, and a lane has a row for the root and the division.
+// The int8 form takes about 14 instructions for a value: byte, mad.hi and shift for each of the three requantisations, half a
+// saturating pack twice, a quarter of a dp4a, multiply-add and shift for y; the three mad.hi (4 cycles of a scheduler's multiplier) are
+// what bounds it next to the memory.
+// XI, HI: x, res are int32 (HI = -1: no residual).  kExact: the threads' words are the row's, none is masked.
+template <int XI, int HI, int WPT, int R, bool kDyn, bool kExact>
 __global__ void __launch_bounds__(R == 1 ? 1024 : 512) rmsnorm_kernel(const RmsArgs a) {
   constexpr bool kWide = HI == 1 || (HI < 0 && XI == 1);   // h is int32
   __shared__ unsigned long long red[R][32];
-  __shared__ int redm[R][32];
+  __shared__ int row_F[R], row_e[R];
+  __shared__ int redm[kDyn ? R : 1][32];
   const int tid = threadIdx.x, T = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = T >> 5, nwords = a.C >> 2;
   const int64_t r0 = (int64_t)blockIdx.x * R;
+  const int rows = (int)min((int64_t)R, a.rows - r0);
   pdl_wait();
   pdl_trigger();
   // h: packed int8, or four int32
   int h[R][WPT][kWide ? 4 : 1];
   {
     int x[R][WPT][XI ? 4 : 1], q[R][WPT][HI == 1 ? 4 : 1];
+    const char* px = static_cast<const char*>(a.x) + r0 * a.ldx * (XI ? 4 : 1) + tid * (XI ? 16 : 4);
+    const char* pq = HI < 0 ? nullptr : static_cast<const char*>(a.res) + r0 * a.ldres * (HI ? 4 : 1) + tid * (HI ? 16 : 4);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int64_t row = min(r0 + r, a.rows - 1);       // (rows past the end: the last one again, not stored)
 #pragma unroll
       for (int i = 0; i < WPT; ++i) {
-        const int w = tid + i * T;
-#pragma unroll
-        for (int k = 0; k < (XI ? 4 : 1); ++k) x[r][i][k] = 0;
-#pragma unroll
-        for (int k = 0; k < (HI == 1 ? 4 : 1); ++k) q[r][i][k] = 0;
-        if (w < nwords) {
-          if (XI) {
-            const int4 v = *reinterpret_cast<const int4*>(static_cast<const int*>(a.x) + row * a.ldx + 4 * w);
-            x[r][i][0] = v.x;
-            if constexpr (XI) { x[r][i][1] = v.y; x[r][i][2] = v.z; x[r][i][3] = v.w; }
-          } else {
-            x[r][i][0] = *reinterpret_cast<const int*>(static_cast<const int8_t*>(a.x) + row * a.ldx + 4 * w);
-          }
-          if (HI == 1) {
-            const int4 v = *reinterpret_cast<const int4*>(static_cast<const int*>(a.res) + row * a.ldres + 4 * w);
-            q[r][i][0] = v.x;
-            if constexpr (HI == 1) { q[r][i][1] = v.y; q[r][i][2] = v.z; q[r][i][3] = v.w; }
-          } else if (HI == 0) {
-            q[r][i][0] = *reinterpret_cast<const int*>(static_cast<const int8_t*>(a.res) + row * a.ldres + 4 * w);
-          }
+        const bool there = kExact || tid + i * T < nwords;
+        if constexpr (XI) {
+          const int4 v = there ? *reinterpret_cast<const int4*>(px + i * T * 16) : make_int4(0, 0, 0, 0);
+          x[r][i][0] = v.x; x[r][i][1] = v.y; x[r][i][2] = v.z; x[r][i][3] = v.w;
+        } else {
+          x[r][i][0] = there ? *reinterpret_cast<const int*>(px + i * T * 4) : 0;
+        }
+        if constexpr (HI == 1) {
+          const int4 v = there ? *reinterpret_cast<const int4*>(pq + i * T * 16) : make_int4(0, 0, 0, 0);
+          q[r][i][0] = v.x; q[r][i][1] = v.y; q[r][i][2] = v.z; q[r][i][3] = v.w;
+        } else if constexpr (HI == 0) {
+          q[r][i][0] = there ? *reinterpret_cast<const int*>(pq + i * T * 4) : 0;
         }
       }
+      px += r + 1 < rows ? a.ldx * (XI ? 4 : 1) : 0;        // (rows past the end: the last one again, not stored)
+      if (HI >= 0) pq += r + 1 < rows ? a.ldres * (HI ? 4 : 1) : 0;
     }
     if constexpr (HI >= 0) {
       Requant<HI ? 0 : 24> rs;
@@ -133,10 +130,11 @@ __global__ void __launch_bounds__(R == 1 ? 1024 : 512) rmsnorm_kernel(const RmsA
       for (int i = 0; i < WPT; ++i) {
         const int w = tid + i * T;
         int m[4] = {1, 1, 1, 1}, s[4] = {40, 40, 40, 40};
-        if (w < nwords) scale_of(a.xs, a.xvec, w, m, s);
+        if (kExact || w < nwords) scale_of(a.xs, a.xvec, w, m, s);
         Requant<XI ? 0 : 24> xs[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) xs[k].set(m[k], s[k]);
+        char* ps = static_cast<char*>(a.sum) + (r0 * a.ldsum + 4 * w) * (HI ? 4 : 1);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
           int v[4];
@@ -146,16 +144,16 @@ __global__ void __launch_bounds__(R == 1 ? 1024 : 512) rmsnorm_kernel(const RmsA
             const int qv = HI ? rs(q[r][i][HI == 1 ? k : 0]) : rs(byte_on_top(q[r][i][0], k));
             v[k] = XI || HI ? add_sat(xv, qv) : xv + qv;
           }
+          const bool store = a.sum && (kExact || w < nwords) && r < rows;
           if constexpr (kWide) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) h[r][i][k] = max(-kStreamMax, min(kStreamMax, v[k]));
+            if (store) *reinterpret_cast<int4*>(ps) = make_int4(h[r][i][0], h[r][i][1], h[r][i][2], h[r][i][3]);
           } else {
             h[r][i][0] = pack4(v[0], v[1], v[2], v[3]);
+            if (store) *reinterpret_cast<int*>(ps) = h[r][i][0];
           }
-          if (a.sum && w < nwords && r0 + r < a.rows) {
-            if constexpr (kWide) *reinterpret_cast<int4*>(static_cast<int*>(a.sum) + (r0 + r) * a.ldsum + 4 * w) = make_int4(h[r][i][0], h[r][i][1], h[r][i][2], h[r][i][3]);
-            else *reinterpret_cast<int*>(static_cast<int8_t*>(a.sum) + (r0 + r) * a.ldsum + 4 * w) = h[r][i][0];
-          }
+          ps += a.ldsum * (HI ? 4 : 1);
         }
       }
     } else {
@@ -188,87 +186,94 @@ __global__ void __launch_bounds__(R == 1 ? 1024 : 512) rmsnorm_kernel(const RmsA
     }
   }
   __syncthreads();
-  // lane l has row l % R's scalars
-  RmsRow mine;
-  {
+  // lane l of the first warp has row l % R's scalars (computed by every warp for itself they were an eighth of all instructions)
+  if (warp == 0) {
     unsigned long long V = 0;
     for (int w = lane / R; w < warps; w += 32 / R) V += red[lane % R][w];
 #pragma unroll
     for (int o = R; o < 32; o <<= 1) V += __shfl_xor_sync(~0u, V, o);
-    mine = rms_row(V, a.M_ln);
+    const RmsRow mine = rms_row(V, a.M_ln);
+    if (lane < R) row_F[lane] = mine.F, row_e[lane] = mine.e;
   }
-  int z[R][WPT][4], A[R], F[R], e[R];
+  __syncthreads();
+  int z[kDyn ? R : 1][kDyn ? WPT : 1][4], A[R];
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    A[r] = 0;
-    F[r] = __shfl_sync(~0u, mine.F, r);
-    e[r] = __shfl_sync(~0u, mine.e, r);
-  }
+  for (int r = 0; r < R; ++r) A[r] = 0;
 #pragma unroll
   for (int i = 0; i < WPT; ++i) {
     const int w = tid + i * T;
     int m[4] = {1, 1, 1, 1}, s[4] = {62, 62, 62, 62};
-    if (w < nwords) scale_of(a.gs, a.gvec, w, m, s);
-    Requant<2> gs[4];
+    if (kExact || w < nwords) scale_of(a.gs, a.gvec, w, m, s);
+    Requant<0> gs[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) gs[k].set(m[k], s[k]);
+    auto rows_out = [&](auto slow) {
+      int8_t* po = a.out + r0 * a.ldout + 4 * w;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int F = row_F[r], e = row_e[r];
+        [[maybe_unused]] const int half = e ? 1 << (e - 1) : 0;
+        int v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if constexpr (kWide) v[k] = mul_hi_add(h[r][i][k] << (31 - e), F << 2, 1) >> 1;   // |h| <= sd < 2^e; floor(2 h F / 2^e), then half of it, rounded
+          else v[k] = (byte_of(h[r][i][0], k) * F + half) >> e;                             // 8 + 23 bits
+          v[k] = decltype(slow)::value ? rq(v[k], m[k], clamp_shift(s[k])) : mul_hi_add(v[k], gs[k].m, gs[k].add) >> gs[k].sh;
+          if constexpr (kDyn) {
+            z[r][i][k] = v[k];
+            A[r] = max(A[r], abs(v[k]));
+          }
+        }
+        if (!kDyn && (kExact || w < nwords) && r < rows) *reinterpret_cast<int*>(po) = pack4(v[0], v[1], v[2], v[3]);
+        po += a.ldout;
+      }
+    };
+    // (ratios above a quarter: the shift of 31 or 32 has no short form)
+    if (gs[0].wide || gs[1].wide || gs[2].wide || gs[3].wide) rows_out(std::true_type{});
+    else rows_out(std::false_type{});
+  }
+  if constexpr (kDyn) {
+    // ---- a scale for each row
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int half = e[r] ? 1 << (e[r] - 1) : 0;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        int y;
-        if constexpr (kWide) y = (mad_hi(h[r][i][k] << (31 - e[r]), F[r] << 2, 1)) >> 1;   // |h| <= sd < 2^e; floor(2 h F / 2^e), then half of it, rounded
-        else y = (byte_of(h[r][i][0], k) * F[r] + half) >> e[r];                              // 8 + 23 bits
-        z[r][i][k] = gs[k](y << 2);
-        if (a.row_max) A[r] = max(A[r], abs(z[r][i][k]));
-      }
-      if (!a.row_max && w < nwords && r0 + r < a.rows)
-        *reinterpret_cast<int*>(a.out + (r0 + r) * a.ldout + 4 * w) = pack4(z[r][i][0], z[r][i][1], z[r][i][2], z[r][i][3]);
+      const int v = __reduce_max_sync(~0u, A[r]);
+      if (lane == 0) redm[r][warp] = v;
     }
-  }
-  if (!a.row_max) return;
-  // ---- a scale for each row
+    __syncthreads();
+    int top = 0, factor, shift;
+    for (int w = lane / R; w < warps; w += 32 / R) top = max(top, redm[lane % R][w]);
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int v = __reduce_max_sync(~0u, A[r]);
-    if (lane == 0) redm[r][warp] = v;
-  }
-  __syncthreads();
-  int top = 0, factor, shift;
-  for (int w = lane / R; w < warps; w += 32 / R) top = max(top, redm[lane % R][w]);
+    for (int o = R; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
+    if (tid < rows) a.row_max[r0 + tid] = top;
+    rms_row_scale(top, factor, shift);
 #pragma unroll
-  for (int o = R; o < 32; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
-  if (tid < R && r0 + tid < a.rows) a.row_max[r0 + tid] = top;
-  rms_row_scale(top, factor, shift);
+    for (int r = 0; r < R; ++r) {
+      const int f = __shfl_sync(~0u, factor, r), up = 54 - __shfl_sync(~0u, shift, r);   // shift = 23 + a: |z| < 2^a, up = 31 - a
 #pragma unroll
-  for (int r = 0; r < R; ++r) {
-    const int f = __shfl_sync(~0u, factor, r), up = 54 - __shfl_sync(~0u, shift, r);   // shift = 23 + a: |z| < 2^a, up = 31 - a
+      for (int i = 0; i < WPT; ++i) {
+        const int w = tid + i * T;
+        int v[4];
 #pragma unroll
-    for (int i = 0; i < WPT; ++i) {
-      const int w = tid + i * T;
-      int v[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = mad_hi(z[r][i][k] << up, f, 1 << 21) >> 22;     // z R / 2^(a+1), then 22 bits more
-      if (w < nwords && r0 + r < a.rows) *reinterpret_cast<int*>(a.out + (r0 + r) * a.ldout + 4 * w) = pack4(v[0], v[1], v[2], v[3]);
+        for (int k = 0; k < 4; ++k) v[k] = mul_hi_add(z[r][i][k] << up, f, 1 << 21) >> 22;     // z R / 2^(a+1), then 22 bits more
+        if ((kExact || w < nwords) && r < rows) *reinterpret_cast<int*>(a.out + (r0 + r) * a.ldout + 4 * w) = pack4(v[0], v[1], v[2], v[3]);
+      }
     }
   }
 }
 
-template <int XI, int HI>
+template <int XI, int HI, bool kDyn>
 static void launch_rows(ivit_ctx* ctx, const RmsArgs& a) {
+  constexpr int R = XI || HI == 1 || kDyn ? 4 : 8;
   const int nwords = a.C >> 2;
   auto threads = [&](int wpt) { return ((nwords + wpt - 1) / wpt + 31) / 32 * 32; };
-  const unsigned one = (unsigned)a.rows, four = (unsigned)((a.rows + 3) / 4);
-  // Four rows at a time from two groups of four for each SM on, up to 4096 channels (registers); below, and beyond, one row, as many threads as there are words.
-  if (a.rows >= 8 * ctx->sm_count && nwords <= 1024) {
-    if (nwords >= 64) launch_k(rmsnorm_kernel<XI, HI, 2, 4>, four, threads(2), 0, ctx->stream, a);
-    else launch_k(rmsnorm_kernel<XI, HI, 1, 4>, four, threads(1), 0, ctx->stream, a);
-  } else if (nwords <= 1024) {
-    launch_k(rmsnorm_kernel<XI, HI, 1, 1>, one, threads(1), 0, ctx->stream, a);
-  } else {
-    launch_k(rmsnorm_kernel<XI, HI, 4, 1>, one, threads(4), 0, ctx->stream, a);
-  }
+  // R rows at a time from two groups for each SM on, up to 4096 channels (registers); below, and beyond, one row, as many threads as there are words.
+  if (a.rows >= 2 * R * ctx->sm_count && nwords <= 1024)
+    launch_k(nwords % 64 ? rmsnorm_kernel<XI, HI, 2, R, kDyn, false> : rmsnorm_kernel<XI, HI, 2, R, kDyn, true>, (unsigned)((a.rows + R - 1) / R),
+             threads(2), 0, ctx->stream, a);
+  else if (nwords <= 1024)
+    launch_k(rmsnorm_kernel<XI, HI, 1, 1, kDyn, false>, (unsigned)a.rows, threads(1), 0, ctx->stream, a);
+  else
+    launch_k(rmsnorm_kernel<XI, HI, 4, 1, kDyn, false>, (unsigned)a.rows, threads(4), 0, ctx->stream, a);
 }
 
 int launch_rmsnorm(ivit_ctx* ctx, const void* x, int x_dtype, int64_t ldx, ScaleDev xs, const void* res, int res_dtype, int64_t ldres,
@@ -279,9 +284,17 @@ int launch_rmsnorm(ivit_ctx* ctx, const void* x, int x_dtype, int64_t ldx, Scale
   const RmsArgs a{x, ldx, xs, res, ldres, rs, gs, M_ln, sum, ldsum, out, ldout, row_max, rows, (int)C, vec(xs), vec(gs)};
   const int xb = x_dtype == IVIT_I8 ? 1 : 4, hb = res_dtype == IVIT_I8 ? 1 : 4;
   LaunchScope ls(ctx, KIND_LAYERNORM, (double)rows * C * (xb + 1 + (res ? hb : 0) + (sum ? hb : 0)));
-  if (!res) x_dtype == IVIT_I8 ? launch_rows<0, -1>(ctx, a) : launch_rows<1, -1>(ctx, a);
-  else if (x_dtype == IVIT_I8) res_dtype == IVIT_I8 ? launch_rows<0, 0>(ctx, a) : launch_rows<0, 1>(ctx, a);
-  else res_dtype == IVIT_I8 ? launch_rows<1, 0>(ctx, a) : launch_rows<1, 1>(ctx, a);
+  auto go = [&](auto xi, auto hi) {
+    if (row_max) launch_rows<decltype(xi)::value, decltype(hi)::value, true>(ctx, a);
+    else launch_rows<decltype(xi)::value, decltype(hi)::value, false>(ctx, a);
+  };
+  using std::integral_constant;
+  const integral_constant<int, -1> none;
+  const integral_constant<int, 0> i8;
+  const integral_constant<int, 1> i32;
+  if (!res) x_dtype == IVIT_I8 ? go(i8, none) : go(i32, none);
+  else if (x_dtype == IVIT_I8) res_dtype == IVIT_I8 ? go(i8, i8) : go(i8, i32);
+  else res_dtype == IVIT_I8 ? go(i32, i8) : go(i32, i32);
   return ls.done();
 }
 
