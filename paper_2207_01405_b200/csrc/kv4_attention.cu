@@ -14,6 +14,7 @@ struct AttendArgs {
   const int32_t *q_start, *lens, *table;
   int64_t ldtable;
   int qk_mult, qk_add, qk_sh;      // s = (hi32(16 a qk_mult) + qk_add) >> qk_sh
+  unsigned sixteen;                // 16, not known to the compiler: a multiplication where a shift would take the busier unit
   int pv_mult, pv_shift, I0, N, z;
   int8_t* O; int64_t ldo;
   int64_t* weights; int64_t ldw;
@@ -61,8 +62,15 @@ __device__ __forceinline__ void mma8(int (&c)[4], uint32_t a0, uint32_t a1, uint
 
 // Sixteen times the codes of the low (high) halves of four bytes, as signed bytes: code + 8 with its top bit flipped is the code in
 // two's complement, and a nibble in the upper half of a byte needs no sign extension.
-__device__ __forceinline__ uint32_t low16(uint32_t w) { return ((w << 4) ^ 0x80808080u) & 0xf0f0f0f0u; }
+__device__ __forceinline__ uint32_t low16(uint32_t w, uint32_t sixteen) { return ((w * sixteen) ^ 0x80808080u) & 0xf0f0f0f0u; }
 __device__ __forceinline__ uint32_t high16(uint32_t w) { return (w ^ 0x80808080u) & 0xf0f0f0f0u; }
+
+// High word of a product plus c (c in a register pair that stays: the same for all values).
+__device__ __forceinline__ int mad_hi(int a, int b, int c) {
+  int d;
+  asm("mad.hi.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
 
 // Four 32-bit values saturated to int8 and packed, x0 in the low byte.
 __device__ __forceinline__ uint32_t pack_sat(int x0, int x1, int x2, int x3) {
@@ -72,20 +80,16 @@ __device__ __forceinline__ uint32_t pack_sat(int x0, int x1, int x2, int x3) {
   return r;
 }
 
-// y_i = byte i of x0, x1, x2, x3.
-__device__ __forceinline__ void transpose4(const uint32_t (&x)[4], uint32_t (&y)[4]) {
-  const uint32_t a = __byte_perm(x[0], x[1], 0x5140), b = __byte_perm(x[2], x[3], 0x5140);
-  const uint32_t c = __byte_perm(x[0], x[1], 0x7362), d = __byte_perm(x[2], x[3], 0x7362);
-  y[0] = __byte_perm(a, b, 0x5410);
-  y[1] = __byte_perm(a, b, 0x7632);
-  y[2] = __byte_perm(c, d, 0x5410);
-  y[3] = __byte_perm(c, d, 0x7632);
+// Two 16 x 16 blocks of bytes, transposed on the way from shared memory: lane 4 n + t gets rows 4 t .. 4 t + 3 of columns n (y0) and n + 8
+// (y1) of the first, y2 and y3 of the second.  Lane l names row l of the two.
+__device__ __forceinline__ void load_transposed(uint32_t addr, uint32_t& y0, uint32_t& y1, uint32_t& y2, uint32_t& y3) {
+  asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(y0), "=r"(y1), "=r"(y2), "=r"(y3) : "r"(addr) : "memory");
 }
 
 // Entry of the exponentials for the score in one byte of w: `sel` holds -4 kKv4Copies in that byte, t = table + copy + 4 kKv4Copies max.
 __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t) {
   unsigned e;
-  asm volatile("{\n\t.reg .u32 a;\n\tdp4a.s32.s32 a, %1, %2, %3;\n\tld.shared.u32 %0, [a];\n\t}" : "=r"(e) : "r"(w), "r"(sel), "r"(t));
+  asm("{\n\t.reg .u32 a;\n\tdp4a.s32.s32 a, %1, %2, %3;\n\tld.shared.u32 %0, [a];\n\t}" : "=r"(e) : "r"(w), "r"(sel), "r"(t));
   return e;
 }
 
@@ -119,7 +123,6 @@ template <int D, int RN, bool kWeights>
 __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(const AttendArgs a) {
   constexpr int kG = D / 32;               // groups of a key
   constexpr int kLaneWords = D / 32;       // words of a K row that a lane takes
-  constexpr int kVWords = D / 64;          // words of a V row that a lane takes
   constexpr int kMu = D / 16;              // tiles of 16 channels
   constexpr int kRows = 8 * RN, kStage = kKv4Block * (D / 2 + D / 32);
   extern __shared__ __align__(128) uint8_t sm[];
@@ -140,7 +143,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   unsigned long long* const row_out = reinterpret_cast<unsigned long long*>(small + 560);   // [16] where a row of O starts
   unsigned long long* const cta_den = row_out + 16;                                  // [16]
   static_assert(4 * 560 + 8 * 32 <= kKv4Small && 4 * 192 + 8 * (3 * 16 + kKv4Warps * 16) <= 4 * 544, "room for the rows' numbers");
-  int* const sums = reinterpret_cast<int*>(sm + at.sums);                            // [plane][row][half of the channels][channel of a lane][lane]
+  int* const sums = reinterpret_cast<int*>(sm + at.sums);                            // [plane][row][channel]
   long long* const fin = reinterpret_cast<long long*>(sm + at.fin);                  // [256] parts of the cluster's sums
   const int score_ld = kv4_score_ld(a.blocks);
   int8_t* const score = reinterpret_cast<int8_t*>(sm + at.score);
@@ -204,9 +207,12 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   const bool holes = __syncthreads_or(bad) != 0;   // a page of the run points nowhere: its keys are not seen
 
   uint8_t* const ring = sm + at.ring + warp * (kKv4Stages * kStage);
-  // Requests a block's codes (at `code`) and steps (at `step` of the block of its page); the chunks of 16 bytes of a row are
-  // exchanged (1 with 3, 0 with 2) in rows 2, 3 modulo 4, which spreads the lanes' reads of V over all banks.
-  const uint32_t put = smem_u32(ring) + 16 * (D == 128 ? lane ^ (lane >> 2 & 2) : lane), put_step = smem_u32(ring) + kKv4Block * (D / 2) + 16 * lane;
+  // A block's codes lie in the ring as rows of 16-byte chunks, at a place of their own for each (row, chunk) that keeps three kinds of
+  // access off the same banks: eight rows one behind the other (V, transposed), every fourth row (K), and the rows as they come in.
+  auto place = [](int row, int chunk) {
+    return D == 128 ? 64 * (row ^ (row >> 2 & 1)) + 16 * (chunk ^ (row >> 1 & 3)) : 32 * (row ^ (row >> 2 & 3)) + 16 * (chunk ^ (row >> 2 & 1));
+  };
+  const uint32_t ring32 = smem_u32(ring), put = ring32 + place(lane / (D / 32), lane % (D / 32)), put_step = ring32 + kKv4Block * (D / 2) + 16 * lane;
   const int in_page = a.page / kKv4Block - 1, per_page = a.page_log - 5;
   // page and place in it of the run's block lb: pages[(lb + first) >> per_page], (lb + first) & in_page
   const int first = blk0 & in_page;
@@ -227,9 +233,12 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   auto request_k = [&](int lb, uint32_t stage) { request(lb, stage, 0, kstep, kKv4Block * kG); };
   auto request_v = [&](int lb, uint32_t stage) { request(lb, stage, vcode, vstep, kKv4Block); };
 
-  // the lane's place in a row of K, in K's steps, and in a row of V
-  const int k_at = D == 128 ? n8 * 64 + 16 * (t4 ^ (n8 & 2)) : n8 * 32 + 8 * t4, ks_at = kKv4Block * (D / 2) + n8 * kG;
-  const int v_at = D == 128 ? t4 * 64 + ((8 * n8) ^ ((t4 & 2) << 4)) : t4 * 32 + 4 * n8;
+  // where the lane's parts of K rows 4 n8 + i lie, and its row of V, chunk by chunk
+  int k_at[4], v_at[D / 32];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k_at[i] = D == 128 ? place(4 * n8 + i, t4) : place(4 * n8 + i, t4 >> 1) + 8 * (t4 & 1);
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) v_at[c] = place(lane, c);
 
   // ---- scores
 #pragma unroll
@@ -248,20 +257,19 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     const int key0 = (blk0 + lb) * kKv4Block;
     if (holes && !pages[(lb + first) >> per_page]) continue;
     int acc[RN][2][4];
+    // steps, byte by byte: the unit of shared memory has time for that, the one that would take words apart has not
+    const uint8_t* step = buf + kKv4Block * (D / 2) + 4 * n8 * kG;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      uint32_t w[2][kLaneWords], st[2];
+      uint32_t w[2][kLaneWords];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int row = 16 * m + 8 * k;    // (and n8)
         if (D == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(buf + k_at + row * 64);
+          const uint4 v = *reinterpret_cast<const uint4*>(buf + k_at[2 * m + k]);
           w[k][0] = v.x; w[k][1] = v.y; w[k][kLaneWords - 2] = v.z; w[k][kLaneWords - 1] = v.w;
-          st[k] = *reinterpret_cast<const uint32_t*>(buf + ks_at + 4 * row);
         } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(buf + k_at + row * 32);
+          const uint2 v = *reinterpret_cast<const uint2*>(buf + k_at[2 * m + k]);
           w[k][0] = v.x; w[k][1] = v.y;
-          st[k] = *reinterpret_cast<const uint16_t*>(buf + ks_at + 2 * row);
         }
       }
 #pragma unroll
@@ -270,8 +278,8 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
         for (int i = 0; i < 4; ++i) acc[j][m][i] = 0;
 #pragma unroll
       for (int g = 0; g < kG; ++g) {
-        const uint32_t a0 = low16(w[0][g]), a1 = low16(w[1][g]), a2 = high16(w[0][g]), a3 = high16(w[1][g]);
-        const int s0 = __byte_perm(st[0], 0, 0x4440 | g), s1 = __byte_perm(st[1], 0, 0x4440 | g);
+        const uint32_t a0 = low16(w[0][g], a.sixteen), a1 = low16(w[1][g], a.sixteen), a2 = high16(w[0][g]), a3 = high16(w[1][g]);
+        const int s0 = step[2 * m * kG + g], s1 = step[(2 * m + 1) * kG + g];
 #pragma unroll
         for (int j = 0; j < RN; ++j) {
           int c[4] = {0, 0, 0, 0};
@@ -288,14 +296,14 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     for (int j = 0; j < RN; ++j)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        int v[4];   // keys n8, n8 + 8, n8 + 16, n8 + 24 of row 2 t4 + e
+        int v[4];   // keys 4 n8 .. 4 n8 + 3 of row 2 t4 + e
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (__mulhi(acc[j][i >> 1][2 * (i & 1) + e], a.qk_mult) + a.qk_add) >> a.qk_sh;
+        for (int i = 0; i < 4; ++i) v[i] = mad_hi(acc[j][i >> 1][2 * (i & 1) + e], a.qk_mult, a.qk_add) >> a.qk_sh;
         const int row = 8 * j + 2 * t4 + e;
         if (!whole) {   // what the row does not see: a score that is no larger than any, and whose weight is left out below
-          const int left = lim[row] - key0 - n8;
+          const int left = lim[row] - key0 - 4 * n8;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = 8 * i < left ? v[i] : -128;
+          for (int i = 0; i < 4; ++i) v[i] = i < left ? v[i] : -128;
         }
         best[j][e] = max(max(best[j][e], max(v[0], v[1])), max(v[2], v[3]));
         if (row < a.kept) *reinterpret_cast<uint32_t*>(score + row * score_ld + lb * kKv4Block + 4 * n8) = pack_sat(v[0], v[1], v[2], v[3]);
@@ -364,15 +372,13 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     stage = stage == (kKv4Stages - 1) * kStage ? 0 : stage + kStage;
     const int key0 = (blk0 + lb) * kKv4Block;
     if (holes && !pages[(lb + first) >> per_page]) continue;
-    // steps of the lane's keys t, t + 4, ..., t + 28
-    uint32_t vs[8];
-    {
-      const uint4 s0 = *reinterpret_cast<const uint4*>(buf + kKv4Block * (D / 2)), s1 = *reinterpret_cast<const uint4*>(buf + kKv4Block * (D / 2) + 16);
-      const uint32_t w[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
+    // steps of the lane's keys 4 t4 .. and 16 + 4 t4 ..
+    uint32_t vs[2][4];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) vs[i] = __byte_perm(w[i], 0, 0x4440 | t4);
-    }
-    uint32_t bl[RN][2], bh[RN][2];   // B operands: word 0 holds keys t + 8 i, word 1 keys t + 4 + 8 i
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vs[k][i] = buf[kKv4Block * (D / 2) + 16 * k + 4 * t4 + i];
+    uint32_t bl[RN][2], bh[RN][2];   // B operands: word 0 holds keys 4 t4 .., word 1 keys 16 + 4 t4 ..
     const bool whole = key0 + kKv4Block <= seen_min;
 #pragma unroll
     for (int j = 0; j < RN; ++j) {
@@ -384,14 +390,14 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
         for (int i = 0; i < 4; ++i) e[i] = exp_of(s, kSel << (8 * i), tab[j]);
         if (!whole) {
-          const int left = lim[min(8 * j + n8, a.kept - 1)] - key0 - t4 - 4 * k;
+          const int left = lim[min(8 * j + n8, a.kept - 1)] - key0 - 4 * t4 - 16 * k;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] = 8 * i < left ? e[i] : 0;
+          for (int i = 0; i < 4; ++i) e[i] = i < left ? e[i] : 0;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           sum += e[i];
-          p[i] = e[i] * vs[2 * i + k] + 0x8000u;
+          p[i] = e[i] * vs[k][i] + 0x8000u;
         }
         const uint32_t p01 = __byte_perm(p[0], p[1], 0x7362), p23 = __byte_perm(p[2], p[3], 0x7362);
         bl[j][k] = __byte_perm(p01, p23, 0x5410);
@@ -401,33 +407,20 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       }
       den[j] += sum;
     }
-    uint32_t x[kVWords][2][4];
+    // 16 bytes of V's rows at a time: byte p holds channels p and p + D/2, so that a tile of 16 bytes is 8 + 8 rows of each of two tiles
+    uint32_t y[D / 32][4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int c = 0; c < D / 32; ++c) load_transposed(smem_u32(buf) + v_at[c], y[c][0], y[c][1], y[c][2], y[c][3]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 4 * k + 8 * i;     // (and t4)
-        if (D == 128) {
-          const uint2 v = *reinterpret_cast<const uint2*>(buf + v_at + row * 64);
-          x[0][k][i] = v.x;
-          x[kVWords - 1][k][i] = v.y;
-        } else {
-          x[0][k][i] = *reinterpret_cast<const uint32_t*>(buf + v_at + row * 32);
-        }
-      }
+    for (int c = 0; c < D / 32; ++c) {
+      // 16 (code + 8) of the upper halves' channels; whole bytes, from whose sums those of the upper halves are taken away in the end, for the lower
 #pragma unroll
-    for (int w = 0; w < kVWords; ++w) {
-      uint32_t y[2][4];
-      transpose4(x[w][0], y[0]);
-      transpose4(x[w][1], y[1]);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        // code + 8 of the lower half's channel, 16 (code + 8) of the upper half's
-        const uint32_t a0 = y[0][i] & 0x0f0f0f0fu, a1 = y[0][i] & 0xf0f0f0f0u, a2 = y[1][i] & 0x0f0f0f0fu, a3 = y[1][i] & 0xf0f0f0f0u;
+      for (int half = 0; half < 2; ++half) {
+        const uint32_t mask = half ? 0xf0f0f0f0u : ~0u;
 #pragma unroll
         for (int j = 0; j < RN; ++j) {
-          mma8<true>(lo[j][4 * w + i], a0, a1, a2, a3, bl[j][0], bl[j][1]);
-          mma8<true>(hi[j][4 * w + i], a0, a1, a2, a3, bh[j][0], bh[j][1]);
+          mma8<true>(lo[j][2 * c + half], y[c][0] & mask, y[c][1] & mask, y[c][2] & mask, y[c][3] & mask, bl[j][0], bl[j][1]);
+          mma8<true>(hi[j][2 * c + half], y[c][0] & mask, y[c][1] & mask, y[c][2] & mask, y[c][3] & mask, bh[j][0], bh[j][1]);
         }
       }
     }
@@ -451,11 +444,11 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      int* dst = sums + (8 * j + 2 * t4 + (e & 1)) * kLd + (e >> 1) * (D / 2) + n8;
+      int* dst = sums + (8 * j + 2 * t4 + (e & 1)) * kLd + 8 * (e >> 1) + n8;
 #pragma unroll
       for (int m = 0; m < kMu; ++m) {
-        atomicAdd(dst + 8 * m, lo[j][m][e]);
-        atomicAdd(dst + kRows * kLd + 8 * m, hi[j][m][e]);
+        atomicAdd(dst + (m & 1) * (D / 2) + 16 * (m >> 1), lo[j][m][e]);
+        atomicAdd(dst + kRows * kLd + (m & 1) * (D / 2) + 16 * (m >> 1), hi[j][m][e]);
       }
     }
   }
@@ -492,7 +485,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     row_recip[pr] = recip_of(row_d);
   }
   constexpr int kTurns = kRows * D / 256;
-  const int own = kRows * D / a.split;     // sums that this CTA finishes, in the order [row][half of the channels][channel of a lane][lane]
+  const int own = kRows * D / a.split;     // sums that this CTA finishes, in the order [row][channel]
   long long part[kTurns];
   if (a.split == 1) {
 #pragma unroll
@@ -500,6 +493,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       const int item = tid + 256 * i;
       const int* src = sums + item / D * kLd + item % D;
       part[i] = src[0] + 256ll * src[kRows * kLd];
+      if (item % D < D / 2) part[i] -= src[D / 2] + 256ll * src[kRows * kLd + D / 2];
     }
   } else {
     // 256 / own threads for one of them, each with some of the peers (eight at most), so that the lanes of a warp read one peer's words in a row
@@ -518,6 +512,10 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
             const uint32_t from = peer_addr(src, g + k * groups);
             x[k] = peer_i32(from);
             y[k] = peer_i32(from + kRows * kLd * 4);
+            if (item % D < D / 2) {
+              x[k] -= peer_i32(from + D * 2);
+              y[k] -= peer_i32(from + kRows * kLd * 4 + D * 2);
+            }
           }
         }
 #pragma unroll
@@ -538,10 +536,10 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
     const int item = min(rank * own + tid + 256 * i, kRows * D - 1), row = item / D;
-    const int half = item % D / (D / 2), ch = half * (D / 2) + item % 8 * kMu + item % (D / 2) / 8;
+    const int ch = item % D;
     const unsigned long long den_row = row_den[row];
-    // (codes came in as code + 8, those of the upper half sixteenfold; a row that sees nothing: every number is zero)
-    const long long num = (part[i] >> (4 * half)) - 8 * (long long)row_u[row];
+    // (codes came in as code + 8, the upper half's sixteenfold; a row that sees nothing: every number is zero)
+    const long long num = (part[i] >> (ch < D / 2 ? 0 : 4)) - 8 * (long long)row_u[row];
     const int t = small_quotient(num * (1ll << (a.z + 5)), den_row, cut_of(den_row), row_recip[row]);
     if (tid + 256 * i < own && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
   }
@@ -562,14 +560,14 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       unsigned long long v[4] = {0, 0, 0, 0};
       for (int row = 0; row < nrows; ++row) {
         const uint32_t s = *reinterpret_cast<const uint32_t*>(score + row * score_ld + 4 * i);
-        const int left = lim[row] - key0 - n, base = top[row];
+        const int left = lim[row] - key0 - 4 * n, base = top[row];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          if (8 * k < left) v[k] += share[row * 256 + base - (int)(int8_t)(s >> (8 * k))];
+          if (k < left) v[k] += share[row * 256 + base - (int)(int8_t)(s >> (8 * k))];
       }
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (v[k]) atomicAdd(w + key0 + n + 8 * k, v[k]);
+        if (v[k]) atomicAdd(w + key0 + 4 * n + k, v[k]);
     }
   }
   if (a.split > 1) cluster_wait();
@@ -620,6 +618,7 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_
   while (top >> (a.z + 8)) ++a.z;
   a.O = O; a.ldo = ldo; a.weights = weights; a.ldw = ldw;
   a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept;
+  a.sixteen = 16;
   a.status = ctx->status_dev;
   LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * seqs * q_heads * max_q * max_len * d);
   cudaLaunchConfig_t cfg = {};

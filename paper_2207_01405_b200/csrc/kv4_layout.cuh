@@ -53,7 +53,7 @@ constexpr int kKv4Block = 32;      // keys that a warp takes at a time
 constexpr int kKv4Warps = 8;
 constexpr int kKv4Stages = 3;      // blocks that a warp holds: one it works on, the others on their way
 constexpr int kKv4Copies = 8;      // copies of the exponentials
-constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: 16 (code + 8) times the upper byte of a weight, over 32768 keys, stays below 2^31
+constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: a byte of codes times a byte of a weight, over 32768 keys, stays below 2^31
 constexpr int kKv4Small = 2560;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
 constexpr int kKv4SmemHalf = 113 * 1024;   // two CTAs on an SM

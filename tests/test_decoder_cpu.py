@@ -173,8 +173,8 @@ def test_every_launch_fits(layout):
                     assert len({(r * ld // 4 + t) % 32 for r in range(8) for t in range(4)}) == 32
                     assert len({(2 * t * ld // 4 + n) % 32 for t in range(4) for n in range(8)}) == 32
                     assert len({(2 * t * sum_ld + n) % 32 for t in range(4) for n in range(8)}) == 32
-                    # sums of a CTA stay below 2^31: 16 (code + 8) times the upper byte of a weight
-                    assert 240 * 255 * 32 * blocks < 2 ** 31
+                    # sums of a CTA stay below 2^31: a byte of codes times a byte of a weight
+                    assert 255 * 255 * 32 * blocks < 2 ** 31
 
 
 def test_what_a_sequence_may_touch(layout):
