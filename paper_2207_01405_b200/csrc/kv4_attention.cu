@@ -1,6 +1,8 @@
 // Attention of query rows over a key/value cache held in 4 bits (ivit_kv4_attention), sm_100a.
-#include "common.cuh"
 #include "kv4_layout.cuh"
+#include "tc_ptx.cuh"
+
+#include <type_traits>
 
 namespace ivit {
 
@@ -18,19 +20,24 @@ struct AttendArgs {
   int pv_mult, pv_shift, I0, N, z;
   int8_t* O; int64_t ldo;
   int64_t* weights; int64_t ldw;
-  int max_q, max_len, split, blocks, kept;
+  int max_q, max_len, split, blocks, kept, stages;
   int* status;
 };
 
 // ---------------------------------------------------------------- instructions
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+// 16 bytes to shared memory where ok, without a branch (which would keep the instructions around it apart).
+__device__ __forceinline__ void cp16_if(bool ok, uint32_t dst, const void* src) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.s32 p, %2, 0;\n\t@p cp.async.cg.shared.global [%0], [%1], 16;\n\t}" ::"r"(dst), "l"(src), "r"((int)ok) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// All but the last `stages` - 2 groups (3 or 4 stages).
+__device__ __forceinline__ void cp_wait_stages(int stages) {
+  if (stages == 4) cp_wait<2>();
+  else cp_wait<1>();
+}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_addr(uint32_t a, int rank) {
@@ -38,15 +45,15 @@ __device__ __forceinline__ uint32_t peer_addr(uint32_t a, int rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
   return r;
 }
-__device__ __forceinline__ int peer_i32(uint32_t a) {
-  int v;
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
+// A value into a peer's shared memory, counted by a barrier of that peer: no fence, no answer to wait for.
+__device__ __forceinline__ void send_i32(uint32_t a, int v, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.s32 [%0], %1, [%2];" ::"r"(a), "r"(v), "r"(bar) : "memory");
 }
-__device__ __forceinline__ unsigned long long peer_u64(uint32_t a) {
-  unsigned long long v;
-  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a));
-  return v;
+__device__ __forceinline__ void send_u64(uint32_t a, unsigned long long v, uint32_t bar) {
+  asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u64 [%0], %1, [%2];" ::"r"(a), "l"(v), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t n) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(n) : "memory");
 }
 
 // D += A B on 16 x 32 by 32 x 8 bytes; both signed or both unsigned.
@@ -64,13 +71,6 @@ __device__ __forceinline__ void mma8(int (&c)[4], uint32_t a0, uint32_t a1, uint
 // two's complement, and a nibble in the upper half of a byte needs no sign extension.
 __device__ __forceinline__ uint32_t low16(uint32_t w, uint32_t sixteen) { return ((w * sixteen) ^ 0x80808080u) & 0xf0f0f0f0u; }
 __device__ __forceinline__ uint32_t high16(uint32_t w) { return (w ^ 0x80808080u) & 0xf0f0f0f0u; }
-
-// High word of a product plus c (c in a register pair that stays: the same for all values).
-__device__ __forceinline__ int mad_hi(int a, int b, int c) {
-  int d;
-  asm("mad.hi.s32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
-  return d;
-}
 
 // Four 32-bit values saturated to int8 and packed, x0 in the low byte.
 __device__ __forceinline__ uint32_t pack_sat(int x0, int x1, int x2, int x3) {
@@ -128,12 +128,12 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   extern __shared__ __align__(128) uint8_t sm[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n8 = lane >> 2, t4 = lane & 3;
   const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split, h = blockIdx.y, b = blockIdx.z;
-  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks);
+  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks, a.split, a.stages);
   const uint8_t** const pages = reinterpret_cast<const uint8_t**>(sm + at.pages);   // this head's block of each page of the run
   int* const small = reinterpret_cast<int*>(sm + at.small);
   int* const lim = small;                                                            // [16] keys that a row sees
-  int* const top = small + 16;                                                       // [16] maxima: of the rows ...
-  int* const cta_top = small + 544;                                                  // [16] ... and of this CTA's part of them
+  int* const top = small + 16;                                                       // [16] maxima of the rows
+  const uint32_t bar0 = smem_u32(small + 544), bar1 = bar0 + 8;                      // what peers send: maxima; sums
   int* const warp_top = small + 32;                                                  // [8][16]
   int* const cta_u = small + 160;                                                    // [2][16] sums of the weights' planes
   unsigned long long* const row_den = reinterpret_cast<unsigned long long*>(small + 192);   // [16]
@@ -141,16 +141,29 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   unsigned long long* const row_recip = row_u + 16;                                  // [16]
   unsigned long long* const warp_den = row_recip + 16;                               // [8][16]
   unsigned long long* const row_out = reinterpret_cast<unsigned long long*>(small + 560);   // [16] where a row of O starts
-  unsigned long long* const cta_den = row_out + 16;                                  // [16]
-  static_assert(4 * 560 + 8 * 32 <= kKv4Small && 4 * 192 + 8 * (3 * 16 + kKv4Warps * 16) <= 4 * 544, "room for the rows' numbers");
+  static_assert(4 * 560 + 8 * 16 <= kKv4Small && 4 * 192 + 8 * (3 * 16 + kKv4Warps * 16) <= 4 * 544, "room for the rows' numbers");
   int* const sums = reinterpret_cast<int*>(sm + at.sums);                            // [plane][row][channel]
-  long long* const fin = reinterpret_cast<long long*>(sm + at.fin);                  // [256] parts of the cluster's sums
+  // what the CTAs of the cluster send: [rank][row] maxima, [denominator, weights][rank][row], [rank][this CTA's share of the sums]
+  int* const top_in = reinterpret_cast<int*>(sm + at.peers);
+  unsigned long long* const row_in = reinterpret_cast<unsigned long long*>(sm + at.peers + 4 * 16 * kRows);
+  long long* const part_in = reinterpret_cast<long long*>(row_in + 2 * 16 * kRows);
   const int score_ld = kv4_score_ld(a.blocks);
   int8_t* const score = reinterpret_cast<int8_t*>(sm + at.score);
   constexpr int kLd = D + 4;
   // what needs nothing that a kernel in front may still be writing
   for (int i = tid; i < 2 * kRows * kLd / 4; i += 256) reinterpret_cast<int4*>(sums)[i] = make_int4(0, 0, 0, 0);
   if (tid < 32) cta_u[tid] = 0;
+  const int own = kRows * D / a.split;     // sums that this CTA finishes, in the order [row][channel]
+  if (a.split > 1) {
+    if (tid == 0) {
+      mbar_init(bar0, 1);
+      mbar_init(bar1, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      expect_bytes(bar0, 4 * a.split * kRows);
+      expect_bytes(bar1, 16 * a.split * kRows + 8 * kRows * D);
+    }
+    cluster_arrive();
+  }
   {  // the exponentials, shifted so that a weight's 16 bits are the upper half of its product with a step
     const unsigned e = shiftexp(-tid, a.I0, a.N) << (16 - a.z);
     uint4* dst = reinterpret_cast<uint4*>(sm + at.table) + tid * (kKv4Copies / 4);
@@ -170,7 +183,10 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   const Kv4Seq seq = kv4_sequence(a.q_start[b], a.q_start[b + 1], a.lens[b], a.tokens, a.max_q, a.max_len);
   if (seq.bad && tid == 0) *(volatile int*)a.status = IVIT_ERR_RANGE;
   const int nrows = min(kRows, seq.n * a.group - row0);
-  if (nrows <= 0) return;                  // (the whole cluster)
+  if (nrows <= 0) {                        // (the whole cluster)
+    if (a.split > 1) cluster_wait();
+    return;
+  }
   // keys that some row of the tile sees, and this CTA's run of them
   const int seen_all = kv4_seen(seq, (row0 + nrows - 1) / a.group), seen_min = kv4_seen(seq, row0 / a.group);
   const int blks = (seen_all + kKv4Block - 1) / kKv4Block, run = (blks + a.split - 1) / a.split;
@@ -206,7 +222,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   const bool holes = __syncthreads_or(bad) != 0;   // a page of the run points nowhere: its keys are not seen
 
-  uint8_t* const ring = sm + at.ring + warp * (kKv4Stages * kStage);
+  uint8_t* const ring = sm + at.ring + warp * (a.stages * kStage);
   // A block's codes lie in the ring as rows of 16-byte chunks, at a place of their own for each (row, chunk) that keeps three kinds of
   // access off the same banks: eight rows one behind the other (V, transposed), every fourth row (K), and the rows as they come in.
   auto place = [](int row, int chunk) {
@@ -216,22 +232,18 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   const int in_page = a.page / kKv4Block - 1, per_page = a.page_log - 5;
   // page and place in it of the run's block lb: pages[(lb + first) >> per_page], (lb + first) & in_page
   const int first = blk0 & in_page;
-  auto request = [&](int lb, uint32_t stage, int code, int step, int step_bytes) {
-    if (lb < nblk) {
-      const uint8_t* src = pages[(lb + first) >> per_page];
-      const int o = (lb + first) & in_page;
-      if (!holes || src) {
-        const uint8_t* from = src + (code + o * (kKv4Block * D / 2) + 16 * lane);
+  const int kstep = kv4_kstep(D, a.page, 0), vcode = kv4_vcode(D, a.page, 0), vstep = kv4_vstep(D, a.page, 0);
+  auto page_of = [&](int lb) { return lb < nblk ? pages[(lb + first) >> per_page] : nullptr; };
+  auto request = [&](int lb, const uint8_t* src, uint32_t stage, int code, int step, int step_bytes) {
+    const int o = (lb + first) & in_page;
+    const uint8_t* from = src + (code + o * (kKv4Block * D / 2) + 16 * lane);
 #pragma unroll
-        for (int i = 0; i < D / 64 * 2; ++i) cp16(put + stage + 512 * i, from + 512 * i);
-        if (lane < step_bytes / 16) cp16(put_step + stage, src + (step + o * step_bytes + 16 * lane));
-      }
-    }
+    for (int i = 0; i < D / 64 * 2; ++i) cp16_if(src != nullptr, put + stage + 512 * i, from + 512 * i);
+    cp16_if(src != nullptr && lane < step_bytes / 16, put_step + stage, src + (step + o * step_bytes + 16 * lane));
     cp_commit();
   };
-  const int kstep = kv4_kstep(D, a.page, 0), vcode = kv4_vcode(D, a.page, 0), vstep = kv4_vstep(D, a.page, 0);
-  auto request_k = [&](int lb, uint32_t stage) { request(lb, stage, 0, kstep, kKv4Block * kG); };
-  auto request_v = [&](int lb, uint32_t stage) { request(lb, stage, vcode, vstep, kKv4Block); };
+  auto request_k = [&](int lb, const uint8_t* src, uint32_t stage) { request(lb, src, stage, 0, kstep, kKv4Block * kG); };
+  auto request_v = [&](int lb, const uint8_t* src, uint32_t stage) { request(lb, src, stage, vcode, vstep, kKv4Block); };
 
   // where the lane's parts of K rows 4 n8 + i lie, and its row of V, chunk by chunk
   int k_at[4], v_at[D / 32];
@@ -241,78 +253,85 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   for (int c = 0; c < D / 32; ++c) v_at[c] = place(lane, c);
 
   // ---- scores
-#pragma unroll
-  for (int s = 0; s < kKv4Stages - 1; ++s) request_k(warp + 8 * s, s * kStage);
+  for (int s = 0; s < a.stages - 1; ++s) request_k(warp + 8 * s, page_of(warp + 8 * s), s * kStage);
   int best[RN][2];
 #pragma unroll
   for (int j = 0; j < RN; ++j) best[j][0] = best[j][1] = -128;
-  uint32_t stage = 0, behind = (kKv4Stages - 1) * kStage;   // the block at hand; where the one requested now goes
+  const int ahead = 8 * (a.stages - 1);
+  const uint32_t last = (a.stages - 1) * kStage;
+  uint32_t stage = 0, behind = last;                        // the block at hand; where the one requested now goes
+  const uint8_t* next = page_of(warp + ahead);             // (looked up a turn before it is needed)
   for (int lb = warp; lb < nblk; lb += 8) {
-    cp_wait<kKv4Stages - 2>();
+    cp_wait_stages(a.stages);
     __syncwarp();
-    request_k(lb + 8 * (kKv4Stages - 1), behind);
     const uint8_t* buf = ring + stage;
+    // what the turn reads, then the request, then the arithmetic: the first is on its way while the second is issued
+    uint32_t w[4][kLaneWords];      // the lane's words of K rows 4 n8 + i
+    int step[4][kG];                // their steps, byte by byte: the unit of shared memory has time for that, the one that would take words apart has not
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (D == 128) {
+        const uint4 v = *reinterpret_cast<const uint4*>(buf + k_at[i]);
+        w[i][0] = v.x; w[i][1] = v.y; w[i][kLaneWords - 2] = v.z; w[i][kLaneWords - 1] = v.w;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(buf + k_at[i]);
+        w[i][0] = v.x; w[i][1] = v.y;
+      }
+#pragma unroll
+      for (int g = 0; g < kG; ++g) step[i][g] = buf[kKv4Block * (D / 2) + (4 * n8 + i) * kG + g];
+    }
+    request_k(lb + ahead, next, behind);
+    next = page_of(lb + ahead + 8);
     behind = stage;
-    stage = stage == (kKv4Stages - 1) * kStage ? 0 : stage + kStage;
+    stage = stage == last ? 0 : stage + kStage;
     const int key0 = (blk0 + lb) * kKv4Block;
-    if (holes && !pages[(lb + first) >> per_page]) continue;
+    if (holes && !page_of(lb)) continue;
     int acc[RN][2][4];
-    // steps, byte by byte: the unit of shared memory has time for that, the one that would take words apart has not
-    const uint8_t* step = buf + kKv4Block * (D / 2) + 4 * n8 * kG;
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      uint32_t w[2][kLaneWords];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (D == 128) {
-          const uint4 v = *reinterpret_cast<const uint4*>(buf + k_at[2 * m + k]);
-          w[k][0] = v.x; w[k][1] = v.y; w[k][kLaneWords - 2] = v.z; w[k][kLaneWords - 1] = v.w;
-        } else {
-          const uint2 v = *reinterpret_cast<const uint2*>(buf + k_at[2 * m + k]);
-          w[k][0] = v.x; w[k][1] = v.y;
-        }
-      }
 #pragma unroll
       for (int j = 0; j < RN; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[j][m][i] = 0;
 #pragma unroll
       for (int g = 0; g < kG; ++g) {
-        const uint32_t a0 = low16(w[0][g], a.sixteen), a1 = low16(w[1][g], a.sixteen), a2 = high16(w[0][g]), a3 = high16(w[1][g]);
-        const int s0 = step[2 * m * kG + g], s1 = step[(2 * m + 1) * kG + g];
+        const uint32_t a0 = low16(w[2 * m][g], a.sixteen), a1 = low16(w[2 * m + 1][g], a.sixteen), a2 = high16(w[2 * m][g]), a3 = high16(w[2 * m + 1][g]);
 #pragma unroll
         for (int j = 0; j < RN; ++j) {
           int c[4] = {0, 0, 0, 0};
           mma8<false>(c, a0, a1, a2, a3, q[j][g][0], q[j][g][1]);
-          acc[j][m][0] += c[0] * s0;
-          acc[j][m][1] += c[1] * s0;
-          acc[j][m][2] += c[2] * s1;
-          acc[j][m][3] += c[3] * s1;
+          acc[j][m][0] += c[0] * step[2 * m][g];
+          acc[j][m][1] += c[1] * step[2 * m][g];
+          acc[j][m][2] += c[2] * step[2 * m + 1][g];
+          acc[j][m][3] += c[3] * step[2 * m + 1][g];
         }
       }
     }
-    const bool whole = key0 + kKv4Block <= seen_min;
+    auto keep = [&](auto whole) {
 #pragma unroll
-    for (int j = 0; j < RN; ++j)
+      for (int j = 0; j < RN; ++j)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        int v[4];   // keys 4 n8 .. 4 n8 + 3 of row 2 t4 + e
+        for (int e = 0; e < 2; ++e) {
+          int v[4];   // keys 4 n8 .. 4 n8 + 3 of row 2 t4 + e
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = mad_hi(acc[j][i >> 1][2 * (i & 1) + e], a.qk_mult, a.qk_add) >> a.qk_sh;
-        const int row = 8 * j + 2 * t4 + e;
-        if (!whole) {   // what the row does not see: a score that is no larger than any, and whose weight is left out below
-          const int left = lim[row] - key0 - 4 * n8;
+          for (int i = 0; i < 4; ++i) v[i] = mad_hi(acc[j][i >> 1][2 * (i & 1) + e], a.qk_mult, a.qk_add) >> a.qk_sh;
+          const int row = 8 * j + 2 * t4 + e;
+          if (!decltype(whole)::value) {   // what the row does not see: a score that is no larger than any, and whose weight is left out below
+            const int left = lim[row] - key0 - 4 * n8;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = i < left ? v[i] : -128;
+            for (int i = 0; i < 4; ++i) v[i] = i < left ? v[i] : -128;
+          }
+          best[j][e] = max(max(best[j][e], max(v[0], v[1])), max(v[2], v[3]));
+          if (row < a.kept) *reinterpret_cast<uint32_t*>(score + row * score_ld + lb * kKv4Block + 4 * n8) = pack_sat(v[0], v[1], v[2], v[3]);
         }
-        best[j][e] = max(max(best[j][e], max(v[0], v[1])), max(v[2], v[3]));
-        if (row < a.kept) *reinterpret_cast<uint32_t*>(score + row * score_ld + lb * kKv4Block + 4 * n8) = pack_sat(v[0], v[1], v[2], v[3]);
-      }
+    };
+    if (key0 + kKv4Block <= seen_min) keep(std::true_type{});
+    else keep(std::false_type{});
   }
   cp_wait<0>();
   __syncwarp();
-#pragma unroll
-  for (int s = 0; s < kKv4Stages - 1; ++s) request_v(warp + 8 * s, s * kStage);
+  for (int s = 0; s < a.stages - 1; ++s) request_v(warp + 8 * s, page_of(warp + 8 * s), s * kStage);
+  next = page_of(warp + ahead);
 #pragma unroll
   for (int j = 0; j < RN; ++j)
 #pragma unroll
@@ -325,17 +344,19 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   __syncthreads();
   // sixteen lanes for a row: over the warps of the CTA, then over the CTAs of the cluster
   const int pr = tid >> 4, pk = tid & 15;
+  if (a.split > 1) cluster_wait();         // (the peers' barriers are set up)
   if (pr < kRows) {
     int v = pk < kKv4Warps ? warp_top[pk * 16 + pr] : -128;
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
-    if (pk == 0) (a.split == 1 ? top : cta_top)[pr] = v;
-  }
-  if (a.split > 1) {
-    cluster_arrive();
-    cluster_wait();
-    if (pr < kRows) {
-      int v = pk < a.split ? peer_i32(peer_addr(smem_u32(cta_top + pr), pk)) : -128;
+    if (a.split == 1) {
+      if (pk == 0) top[pr] = v;
+    } else if (pk < a.split) {
+      send_i32(peer_addr(smem_u32(top_in + rank * kRows + pr), pk), v, peer_addr(bar0, pk));
+    }
+    if (a.split > 1) {
+      mbar_wait(bar0, 0, a.status);
+      v = pk < a.split ? top_in[pk * kRows + pr] : -128;
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
       if (pk == 0) top[pr] = v;
@@ -362,55 +383,59 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       for (int i = 0; i < 4; ++i) lo[j][m][i] = hi[j][m][i] = 0;
   }
   constexpr uint32_t kSel = (uint32_t)(-4 * kKv4Copies) & 255u;
-  stage = 0, behind = (kKv4Stages - 1) * kStage;
+  stage = 0, behind = last;
   for (int lb = warp; lb < nblk; lb += 8) {
-    cp_wait<kKv4Stages - 2>();
+    cp_wait_stages(a.stages);
     __syncwarp();
-    request_v(lb + 8 * (kKv4Stages - 1), behind);
     const uint8_t* buf = ring + stage;
-    behind = stage;
-    stage = stage == (kKv4Stages - 1) * kStage ? 0 : stage + kStage;
-    const int key0 = (blk0 + lb) * kKv4Block;
-    if (holes && !pages[(lb + first) >> per_page]) continue;
-    // steps of the lane's keys 4 t4 .. and 16 + 4 t4 ..
-    uint32_t vs[2][4];
+    uint32_t sc[RN][2], vs[2][4], y[D / 32][4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
+    for (int k = 0; k < 2; ++k) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vs[k][i] = buf[kKv4Block * (D / 2) + 16 * k + 4 * t4 + i];
-    uint32_t bl[RN][2], bh[RN][2];   // B operands: word 0 holds keys 4 t4 .., word 1 keys 16 + 4 t4 ..
-    const bool whole = key0 + kKv4Block <= seen_min;
+      for (int j = 0; j < RN; ++j) sc[j][k] = *reinterpret_cast<const uint32_t*>(mine[j] + lb * kKv4Block + 16 * k);   // keys 4 t4 .., 16 + 4 t4 ..
 #pragma unroll
-    for (int j = 0; j < RN; ++j) {
-      unsigned sum = 0;
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t s = *reinterpret_cast<const uint32_t*>(mine[j] + lb * kKv4Block + 16 * k);
-        unsigned e[4], p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = exp_of(s, kSel << (8 * i), tab[j]);
-        if (!whole) {
-          const int left = lim[min(8 * j + n8, a.kept - 1)] - key0 - 4 * t4 - 16 * k;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) e[i] = i < left ? e[i] : 0;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          sum += e[i];
-          p[i] = e[i] * vs[k][i] + 0x8000u;
-        }
-        const uint32_t p01 = __byte_perm(p[0], p[1], 0x7362), p23 = __byte_perm(p[2], p[3], 0x7362);
-        bl[j][k] = __byte_perm(p01, p23, 0x5410);
-        bh[j][k] = __byte_perm(p01, p23, 0x7632);
-        ul[j] = __dp4a(bl[j][k], 0x01010101u, ul[j]);
-        uh[j] = __dp4a(bh[j][k], 0x01010101u, uh[j]);
-      }
-      den[j] += sum;
+      for (int i = 0; i < 4; ++i) vs[k][i] = buf[kKv4Block * (D / 2) + 16 * k + 4 * t4 + i];                           // their steps
     }
-    // 16 bytes of V's rows at a time: byte p holds channels p and p + D/2, so that a tile of 16 bytes is 8 + 8 rows of each of two tiles
-    uint32_t y[D / 32][4];
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) load_transposed(smem_u32(buf) + v_at[c], y[c][0], y[c][1], y[c][2], y[c][3]);
+    request_v(lb + ahead, next, behind);
+    next = page_of(lb + ahead + 8);
+    behind = stage;
+    stage = stage == last ? 0 : stage + kStage;
+    const int key0 = (blk0 + lb) * kKv4Block;
+    if (holes && !page_of(lb)) continue;
+    uint32_t bl[RN][2], bh[RN][2];   // B operands: word 0 holds keys 4 t4 .., word 1 keys 16 + 4 t4 ..
+    auto weigh = [&](auto whole) {
+#pragma unroll
+      for (int j = 0; j < RN; ++j) {
+        unsigned sum = 0;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          unsigned e[4], p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) e[i] = exp_of(sc[j][k], kSel << (8 * i), tab[j]);
+          if (!decltype(whole)::value) {
+            const int left = lim[min(8 * j + n8, a.kept - 1)] - key0 - 4 * t4 - 16 * k;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e[i] = i < left ? e[i] : 0;
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            sum += e[i];
+            p[i] = e[i] * vs[k][i] + 0x8000u;
+          }
+          const uint32_t p01 = __byte_perm(p[0], p[1], 0x7362), p23 = __byte_perm(p[2], p[3], 0x7362);
+          bl[j][k] = __byte_perm(p01, p23, 0x5410);
+          bh[j][k] = __byte_perm(p01, p23, 0x7632);
+          ul[j] = __dp4a(bl[j][k], 0x01010101u, ul[j]);
+          uh[j] = __dp4a(bh[j][k], 0x01010101u, uh[j]);
+        }
+        den[j] += sum;
+      }
+    };
+    if (key0 + kKv4Block <= seen_min) weigh(std::true_type{});
+    else weigh(std::false_type{});
+    // 16 bytes of V's rows at a time: byte p holds channels p and p + D/2, so that a tile of 16 bytes is 8 + 8 rows of each of two tiles
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
       // 16 (code + 8) of the upper halves' channels; whole bytes, from whose sums those of the upper halves are taken away in the end, for the lower
@@ -454,81 +479,54 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   __syncthreads();
   // ---- the rows' sums and the cluster's
-  unsigned long long row_d = 0, row_s = 0;   // denominator and sum of the weights, of this CTA
+  constexpr int kTurns = kRows * D / 256;
+  long long part[kTurns];
+#pragma unroll
+  for (int i = 0; i < kTurns; ++i) {
+    const int item = tid + 256 * i;
+    const int* src = sums + item / D * kLd + item % D;
+    part[i] = src[0] + 256ll * src[kRows * kLd];
+    if (item % D < D / 2) part[i] -= src[D / 2] + 256ll * src[kRows * kLd + D / 2];
+    if (a.split > 1) {
+      const int to = item / own;
+      send_u64(peer_addr(smem_u32(part_in + rank * own + (item - to * own)), to), (unsigned long long)part[i], peer_addr(bar1, to));
+    }
+  }
   if (pr < kRows) {
-    row_d = pk < kKv4Warps ? warp_den[pk * 16 + pr] : 0;
+    unsigned long long row_d = pk < kKv4Warps ? warp_den[pk * 16 + pr] : 0;   // denominator and sum of the weights, of this CTA
+    unsigned long long row_s = (unsigned)cta_u[pr] + 256ull * (unsigned)cta_u[16 + pr];
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) row_d += __shfl_xor_sync(~0u, row_d, o);
-    row_s = (unsigned)cta_u[pr] + 256ull * (unsigned)cta_u[16 + pr];
-  }
-  if (a.split > 1) {
-    if (pr < kRows && pk == 0) cta_den[pr] = row_d;
-    cluster_arrive();
-    cluster_wait();
-    if (pr < kRows) {
-      row_d = row_s = 0;
+    if (a.split > 1) {
       if (pk < a.split) {
-        row_d = peer_u64(peer_addr(smem_u32(cta_den + pr), pk));
-        row_s = (unsigned)peer_i32(peer_addr(smem_u32(cta_u + pr), pk)) + 256ull * (unsigned)peer_i32(peer_addr(smem_u32(cta_u + 16 + pr), pk));
+        send_u64(peer_addr(smem_u32(row_in + rank * kRows + pr), pk), row_d, peer_addr(bar1, pk));
+        send_u64(peer_addr(smem_u32(row_in + (16 + rank) * kRows + pr), pk), row_s, peer_addr(bar1, pk));
       }
+      mbar_wait(bar1, 0, a.status);
+      row_d = pk < a.split ? row_in[pk * kRows + pr] : 0;
+      row_s = pk < a.split ? row_in[(16 + pk) * kRows + pr] : 0;
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) {
         row_d += __shfl_xor_sync(~0u, row_d, o);
         row_s += __shfl_xor_sync(~0u, row_s, o);
       }
     }
-  }
-  if (pr < kRows && pk == 0) {
-    row_d >>= 16 - a.z;
-    row_den[pr] = row_d;
-    row_u[pr] = row_s;
-    row_recip[pr] = recip_of(row_d);
-  }
-  constexpr int kTurns = kRows * D / 256;
-  const int own = kRows * D / a.split;     // sums that this CTA finishes, in the order [row][channel]
-  long long part[kTurns];
-  if (a.split == 1) {
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      const int item = tid + 256 * i;
-      const int* src = sums + item / D * kLd + item % D;
-      part[i] = src[0] + 256ll * src[kRows * kLd];
-      if (item % D < D / 2) part[i] -= src[D / 2] + 256ll * src[kRows * kLd + D / 2];
+    if (pk == 0) {
+      row_d >>= 16 - a.z;
+      row_den[pr] = row_d;
+      row_u[pr] = row_s;
+      row_recip[pr] = recip_of(row_d);
     }
-  } else {
-    // 256 / own threads for one of them, each with some of the peers (eight at most), so that the lanes of a warp read one peer's words in a row
-    const int groups = own < 256 ? 256 / own : 1, g = own < 256 ? tid / own : 0;
+  }
+  if (a.split > 1) {
+    mbar_wait(bar1, 0, a.status);
+    cluster_arrive();                      // (waited for at the end: no CTA leaves while a peer may still send to it, not even when a wait gave up)
 #pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      part[i] = 0;
-      if (256 * i < own) {
-        const int item = rank * own + (own < 256 ? tid % own : tid + 256 * i);
-        const uint32_t src = smem_u32(sums + item / D * kLd + item % D);
-        int x[8], y[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          x[k] = y[k] = 0;
-          if (g + k * groups < a.split) {
-            const uint32_t from = peer_addr(src, g + k * groups);
-            x[k] = peer_i32(from);
-            y[k] = peer_i32(from + kRows * kLd * 4);
-            if (item % D < D / 2) {
-              x[k] -= peer_i32(from + D * 2);
-              y[k] -= peer_i32(from + kRows * kLd * 4 + D * 2);
-            }
-          }
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) part[i] += x[k] + 256ll * y[k];
+    for (int i = 0; i < kTurns; ++i)
+      if (tid + 256 * i < own) {
+        part[i] = 0;
+        for (int k = 0; k < a.split; ++k) part[i] += part_in[k * own + tid + 256 * i];
       }
-    }
-    cluster_arrive();                      // (waited for at the end: a CTA's sums stay until its peers have read them)
-    if (groups > 1) {
-      fin[tid] = part[0];
-      __syncthreads();
-      part[0] = 0;
-      for (int k = 0; k < groups; ++k) part[0] += fin[k * own + tid % own];
-    }
   }
   __syncthreads();
 
@@ -556,7 +554,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     unsigned long long* w = reinterpret_cast<unsigned long long*>(a.weights) + ((int64_t)b * a.heads + h) * a.ldw;
     for (int i = tid; i < nblk * 8; i += 256) {
       const int key0 = (blk0 + (i >> 3)) * kKv4Block, n = i & 7;
-      if (holes && !pages[((i >> 3) + first) >> per_page]) continue;
+      if (holes && !page_of(i >> 3)) continue;
       unsigned long long v[4] = {0, 0, 0, 0};
       for (int row = 0; row < nrows; ++row) {
         const uint32_t s = *reinterpret_cast<const uint32_t*>(score + row * score_ld + 4 * i);
@@ -617,7 +615,7 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_
   const int64_t top = (int64_t)smax.I0 << smax.N;
   while (top >> (a.z + 8)) ++a.z;
   a.O = O; a.ldo = ldo; a.weights = weights; a.ldw = ldw;
-  a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept;
+  a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept; a.stages = p.stages;
   a.sixteen = 16;
   a.status = ctx->status_dev;
   LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * seqs * q_heads * max_q * max_len * d);

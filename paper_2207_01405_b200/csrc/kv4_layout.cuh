@@ -51,9 +51,9 @@ IVIT_KV4_FN int kv4_seen(const Kv4Seq& s, int t) {
 
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time
 constexpr int kKv4Warps = 8;
-constexpr int kKv4Stages = 3;      // blocks that a warp holds: one it works on, the others on their way
 constexpr int kKv4Copies = 8;      // copies of the exponentials
 constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: a byte of codes times a byte of a weight, over 32768 keys, stays below 2^31
+constexpr int kKv4Split = 32;      // blocks of a CTA below which it is not halved once more: the exchange costs what four of a warp's blocks do
 constexpr int kKv4Small = 2560;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
 constexpr int kKv4SmemHalf = 113 * 1024;   // two CTAs on an SM
@@ -65,26 +65,28 @@ IVIT_KV4_FN int kv4_stage_bytes(int d) { return kKv4Block * (d / 2 + d / 32); }
 IVIT_KV4_FN int kv4_sum_ld(int d) { return d + 4; }
 
 struct Kv4Smem {
-  int table, small, sums, fin, pages, ring, score, total;
+  int table, small, sums, peers, pages, ring, score, total;
 };
-// rows: query rows of a CTA (8 or 16); kept: those of them that some sequence can have, whose scores are kept; blocks: blocks of keys of a CTA.
-IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks) {
+// rows: query rows of a CTA (8 or 16); kept: those of them that some sequence can have, whose scores are kept; blocks: blocks of keys of a CTA;
+// split: CTAs of a cluster; stages: blocks that a warp holds, one it works on and the others on their way.
+IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, int split, int stages) {
   Kv4Smem m;
   m.table = 0;
   m.small = m.table + 256 * kKv4Copies * 4;
   m.sums = m.small + kKv4Small;
-  m.fin = m.sums + 2 * rows * kv4_sum_ld(d) * 4;
-  m.pages = m.fin + 256 * 8;
+  m.peers = m.sums + 2 * rows * kv4_sum_ld(d) * 4;
+  m.pages = m.peers + (split > 1 ? 16 * rows * (4 + 2 * 8) + rows * d * 8 : 0);   // (see the kernel)
   m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 8 + 127) / 128 * 128;
   // behind the passes the ring holds the shares of the weights
-  const int ring = kKv4Warps * kKv4Stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
+  const int ring = kKv4Warps * stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
   m.score = m.ring + (ring > shares ? ring : shares);
   m.total = m.score + kept * kv4_score_ld(blocks);
   return m;
 }
 
 struct Kv4Plan {
-  int rows, kept, split, blocks, tiles, smem;   // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, row tiles, bytes
+  // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, blocks a warp holds, row tiles, bytes
+  int rows, kept, split, blocks, stages, tiles, smem;
 };
 inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms) {
   Kv4Plan p;
@@ -93,15 +95,22 @@ inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t s
     p.tiles = (int)((q_rows + p.rows - 1) / p.rows);
     p.kept = (int)(q_rows < p.rows ? q_rows : p.rows);
     const int64_t ctas = (int64_t)p.tiles * heads * seqs;
-    auto size = [&]() {
+    // three blocks under way for each warp where there is room, else two; bytes within the limit for the rows' form
+    auto fits = [&]() {
       p.blocks = (int)((all + p.split - 1) / p.split);
       if (p.blocks < 1) p.blocks = 1;
-      p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks).total;
+      const int limit = p.rows == 8 && (ctas * p.split > sms || p.split == 16) ? kKv4SmemHalf : kKv4SmemMax;
+      for (p.stages = 4; p.stages >= 3; --p.stages) {
+        p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.stages).total;
+        if (p.smem <= limit) return p.blocks <= kKv4Blocks;
+      }
+      p.stages = 3;
+      return false;
     };
     p.split = 1;
-    while (p.split < 16 && ctas * p.split < sms && all > (int64_t)p.split * kKv4Warps) p.split *= 2;
-    for (size(); (p.blocks > kKv4Blocks || p.smem > (p.rows == 8 ? kKv4SmemHalf : kKv4SmemMax)) && p.split < 16; size()) p.split *= 2;
-    if (p.smem <= kKv4SmemMax || p.rows == 8) return p;
+    while (p.split < 16 && ctas * p.split < sms && all > (int64_t)p.split * kKv4Split) p.split *= 2;
+    while (!fits() && p.split < 16) p.split *= 2;
+    if ((p.smem <= kKv4SmemMax && p.blocks <= kKv4Blocks) || p.rows == 8) return p;
   }
 }
 
