@@ -429,10 +429,17 @@ int ivit_isqrt_range(ivit_ctx* ctx, uint32_t n0, uint32_t count, uint16_t* out);
  * sum has the type of res, may be res itself, or NULL (not wanted).  x_scale and gamma_scale per-channel or per-tensor, res_scale
  * per-tensor.  8 <= M_ln <= 22, C % 4 == 0, C <= 16384; pointers 16-byte aligned, leading dimensions multiples of 16 bytes (row_max and
  * the scales' arrays of their own size).  out may not overlap the other tensors. */
-int ivit_rmsnorm(ivit_ctx* ctx, const void* x, int32_t x_dtype, int64_t ldx, ivit_scale x_scale,
-                 const void* res, int32_t res_dtype, int64_t ldres, ivit_scale res_scale,
-                 ivit_scale gamma_scale, int32_t M_ln, void* sum, int64_t ldsum,
-                 int8_t* out, int64_t ldout, int32_t* row_max, int64_t rows, int64_t C);
+typedef struct {
+  const void* x; int64_t ldx;              /* [rows, C] */
+  const void* res; int64_t ldres;          /* [rows, C] or NULL */
+  void* sum; int64_t ldsum;                /* [rows, C] of res' type, or NULL */
+  int8_t* out; int64_t ldout;              /* [rows, C] */
+  int32_t* row_max;                        /* [rows] or NULL */
+  int64_t rows, C;
+  ivit_scale x_scale, res_scale, gamma_scale;
+  int32_t x_dtype, res_dtype, M_ln;
+} ivit_rmsnorm_params;
+int ivit_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params* p);
 
 /* A pool of pages that holds keys and values in 4 bits.  A page takes `page` tokens; its part for one head is a block of
  * page (d + d/32 + 1) bytes, at data + (page_index heads + head) times that:
@@ -474,10 +481,17 @@ int ivit_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K,
  * tokens or keys (the launch is sized by them; ldtable >= ceil(max_len / page), ldw >= max_len); max_len <= IVIT_KV4_MAX_LEN.  A sequence
  * that breaks them, a q_start outside 0 .. tokens, or a page outside the pool is reported by ivit_ctx_poll_status (IVIT_ERR_RANGE) and read only as
  * far as it is valid: keys of such a page are not seen, query rows past max_q or tokens are not written, keys past max_len do not exist. */
-int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
-                       const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable,
-                       ivit_scale qk_scale, ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo,
-                       int64_t* weights, int64_t ldw, int64_t seqs, int64_t max_q, int64_t max_len);
+typedef struct {
+  const int8_t* Q; int64_t ldq;            /* [tokens, q_heads d] */
+  int8_t* O; int64_t ldo;                  /* [tokens, q_heads d] */
+  const int32_t *q_start, *lens;           /* [seqs + 1], [seqs] */
+  const int32_t* table; int64_t ldtable;   /* [seqs, >= ceil(max_len / page)] */
+  int64_t* weights; int64_t ldw;           /* [seqs, heads, ldw] or NULL */
+  int64_t q_heads, tokens, seqs, max_q, max_len;
+  ivit_scale qk_scale, pv_scale;           /* per-tensor */
+  ivit_exp_params smax;
+} ivit_kv4_attention_params;
+int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_attention_params* p);
 
 /* Eviction by accumulated weight.  Of every sequence and head with lens[b] > keep keys, keeps the first `sinks`, the last `recent`, and
  * of the others those of largest weight (of equal ones the lower index) until `keep` are left, in their order; new_lens[b] = min(lens[b], keep).
@@ -486,10 +500,16 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t*
  * In place: dst_table == table and weights_out == weights (with the same leading dimensions).  Else the pages of dst_table hold no
  * source row, and weights_out does not overlap weights.  new_lens may be lens.  sinks + recent <= keep; ldw >= max_len, ldw_out >= keep, ldtable >=
  * ceil(max_len / page), ld_dst >= ceil(min(keep, max_len) / page); max_len < 2^31.  lens above max_len and pages outside the pool are reported as above (such rows are not moved). */
-int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens,
-                   const int32_t* table, int64_t ldtable, const int32_t* dst_table, int64_t ld_dst,
-                   int64_t* weights_out, int64_t ldw_out, int32_t* kept, int32_t* new_lens,
-                   int64_t seqs, int64_t max_len, int64_t keep, int64_t sinks, int64_t recent);
+typedef struct {
+  const int64_t* weights; int64_t ldw;     /* [seqs, heads, ldw] */
+  int64_t* weights_out; int64_t ldw_out;   /* [seqs, heads, ldw_out] */
+  const int32_t* lens; int32_t* new_lens;  /* [seqs] */
+  const int32_t* table; int64_t ldtable;   /* [seqs, ldtable] */
+  const int32_t* dst_table; int64_t ld_dst;
+  int32_t* kept;                           /* [seqs, heads, keep] */
+  int64_t seqs, max_len, keep, sinks, recent;
+} ivit_kv4_evict_params;
+int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_evict_params* p);
 
 /* ---- data movement helpers (not in the paper; needed by the full models) ---- */
 

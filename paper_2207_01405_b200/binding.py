@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -156,13 +157,12 @@ def load_library():
     L.ivit_isqrt_range.argtypes = [vp, C.c_uint32, C.c_uint32, vp]
     L.ivit_kernel_kind_name.argtypes = [i32]
     L.ivit_kernel_kind_name.restype = C.c_char_p
-    L.ivit_rmsnorm.argtypes = [vp, vp, i32, i64, CScale, vp, i32, i64, CScale, CScale, i32, vp, i64, vp, i64, vp, i64, i64]
+    L.ivit_rmsnorm.argtypes = [vp, vp]
     L.ivit_kv4_cache_bytes.argtypes = [C.POINTER(CKv4)]
     L.ivit_kv4_cache_bytes.restype = C.c_size_t
     L.ivit_kv4_append.argtypes = [vp, C.POINTER(CKv4), vp, i64, vp, i64, vp, i64]
-    L.ivit_kv4_attention.argtypes = [vp, C.POINTER(CKv4), vp, i64, i64, i64, vp, vp, vp, i64, CScale, CExp, CScale, vp, i64, vp, i64,
-                                     i64, i64, i64]
-    L.ivit_kv4_evict.argtypes = [vp, C.POINTER(CKv4), vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i64]
+    L.ivit_kv4_attention.argtypes = [vp, C.POINTER(CKv4), vp]
+    L.ivit_kv4_evict.argtypes = [vp, C.POINTER(CKv4), vp]
     L.ivit_patchify.argtypes = [vp, vp, i64, i64, i64, i64, i64, i64, vp, i64]
     L.ivit_gather_rows.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64]
     L.ivit_fill_rows.argtypes = [vp, vp, i64, vp, i64, i64]
@@ -194,12 +194,11 @@ def _ld(t: torch.Tensor) -> int:
     return t.stride(-2) if t.dim() >= 2 else t.shape[-1]
 
 
-def _row_ld(t: torch.Tensor, rows: int, cols: int) -> int:
-    """Leading dimension of a 2-d tensor; one row (or none) has no use for it, and its stride may be anything."""
-    return t.stride(0) if rows > 1 else (cols + 15) // 16 * 16
-
-
-_UNIT = CScale(None, None, 2 ** 31 - 1, 31)
+# The call descriptions of include/ivit.h, packed in one go (a scale: two pointers, multiplier, shift).
+_RMSNORM = struct.Struct("=" + "Qq" * 4 + "Q" + "qq" + "QQii" * 3 + "iii4x")
+_ATTENTION = struct.Struct("=" + "Qq" * 2 + "QQ" + "Qq" * 2 + "q" * 5 + "QQii" * 2 + "iiii")
+_EVICT = struct.Struct("=" + "Qq" * 2 + "QQ" + "Qq" * 2 + "Q" + "q" * 5)
+_UNIT = (0, 0, 2 ** 31 - 1, 31)
 
 
 class DevScale:
@@ -215,7 +214,10 @@ class DevScale:
             self.c = CScale(self.mult_t.data_ptr(), self.shift_t.data_ptr(), 0, 0)
         else:
             self.c = CScale(None, None, int(scale.mult), int(scale.shift))
+        self._pack()
 
+    def _pack(self):
+        self.fields = (self.c.mult_c or 0, self.c.shift_c or 0, self.c.mult, self.c.shift)
 
     @classmethod
     def of(cls, mult, shift) -> "DevScale":
@@ -228,6 +230,7 @@ class DevScale:
             self.c = CScale(mult.data_ptr(), shift.data_ptr(), 0, 0)
         else:
             self.c = CScale(None, None, int(mult), int(shift))
+        self._pack()
         return self
 
 
@@ -249,8 +252,6 @@ class Kv4Cache:
 
 
 def _cexp(p) -> CExp:
-    if isinstance(p, CExp):
-        return p
     return CExp(int(p.I0), int(p.N), int(p.M), int(p.k_out))
 
 
@@ -429,47 +430,51 @@ class Context:
         return out
 
     def _want(self, what: str, dtype, dim: int, t: torch.Tensor):
-        """Refuses a tensor that the C side would read as something else; returns its shape."""
-        shape = t.shape
-        if t.dtype is not dtype or len(shape) != dim or t.get_device() != self.index or (shape[-1] > 1 and t.stride(-1) != 1):
+        """Refuses a tensor that the C side would read as something else; returns its shape and leading dimension."""
+        shape, strides = t.shape, t.stride()
+        if t.dtype is not dtype or len(shape) != dim or t.get_device() != self.index or (strides[-1] != 1 and shape[-1] > 1):
             raise ValueError(f"{what}: want a {dim}-d {dtype} tensor on {self.device} with contiguous rows, got {tuple(shape)} "
-                             f"{t.dtype} on {t.device}, strides {t.stride()}")
-        return shape
+                             f"{t.dtype} on {t.device}, strides {strides}")
+        # (one row, or none, has no use for a leading dimension, and its stride may be anything)
+        return shape, strides[0] if shape[0] > 1 else (shape[-1] + 15) // 16 * 16
 
     def rmsnorm(self, x, gamma_scale: DevScale, x_scale: DevScale = None, res=None, res_scale: DevScale = None, M_ln=20, sum_out=None,
                 out=None, row_max=None):
         """ivit_rmsnorm: x (int8 or int32) [rows, C], with res added first (its sum goes to sum_out, which may be res); returns int8 rows.
         row_max (int32 [rows]): every row gets a scale of its own, written there."""
         x8 = x.dtype is torch.int8
-        shape = self._want("x", torch.int8 if x8 else torch.int32, 2, x)
+        shape, ldx = self._want("x", torch.int8 if x8 else torch.int32, 2, x)
         rows, Cc = shape
         if out is None:
             out = torch.empty((rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
-        elif self._want("out", torch.int8, 2, out) != shape:
+        o_shape, ldo = self._want("out", torch.int8, 2, out)
+        if o_shape != shape:
             raise ValueError("out has the shape of x")
-        r8, ld_res, ld_sum, p_res, p_sum, p_max, xs, rs = 0, 0, 0, None, None, None, _UNIT, _UNIT
+        r8, ldr, lds, p_res, p_sum, p_max, xs, rs = False, 0, 0, 0, 0, 0, _UNIT, _UNIT
         if res is not None:
             r8 = res.dtype is torch.int8
             dt = torch.int8 if r8 else torch.int32
-            if x_scale is None or res_scale is None or self._want("res", dt, 2, res) != shape:
+            r_shape, ldr = self._want("res", dt, 2, res)
+            if x_scale is None or res_scale is None or r_shape != shape:
                 raise ValueError("res has the shape of x, and comes with x_scale and res_scale")
-            xs, rs, p_res, ld_res = x_scale.c, res_scale.c, res.data_ptr(), _row_ld(res, rows, Cc)
+            xs, rs, p_res = x_scale.fields, res_scale.fields, res.data_ptr()
             if x_scale.mult_t is not None and x_scale.mult_t.numel() != Cc:
                 raise ValueError("a per-channel scale has an entry for each channel")
             if sum_out is not None:
-                if self._want("sum_out", dt, 2, sum_out) != shape:
+                s_shape, lds = self._want("sum_out", dt, 2, sum_out)
+                if s_shape != shape:
                     raise ValueError("sum_out has the shape of x")
-                p_sum, ld_sum = sum_out.data_ptr(), _row_ld(sum_out, rows, Cc)
+                p_sum = sum_out.data_ptr()
         elif sum_out is not None:
             raise ValueError("sum_out comes with res")
         if gamma_scale.mult_t is not None and gamma_scale.mult_t.numel() != Cc:
             raise ValueError("a per-channel scale has an entry for each channel")
         if row_max is not None:
-            if self._want("row_max", torch.int32, 1, row_max)[0] != rows:
+            if self._want("row_max", torch.int32, 1, row_max)[0][0] != rows:
                 raise ValueError("row_max has an entry for each row")
             p_max = row_max.data_ptr()
-        rc = self.lib.ivit_rmsnorm(self.h, x.data_ptr(), I8 if x8 else I32, _row_ld(x, rows, Cc), xs, p_res, I8 if r8 else I32, ld_res, rs,
-                                   gamma_scale.c, M_ln, p_sum, ld_sum, out.data_ptr(), _row_ld(out, rows, Cc), p_max, rows, Cc)
+        rc = self.lib.ivit_rmsnorm(self.h, _RMSNORM.pack(x.data_ptr(), ldx, p_res, ldr, p_sum, lds, out.data_ptr(), ldo, p_max, rows, Cc, *xs, *rs,
+                                                         *gamma_scale.fields, I8 if x8 else I32, I8 if r8 else I32, M_ln))
         if rc:
             raise IvitError(rc, "ivit_rmsnorm")
         return out
@@ -478,12 +483,12 @@ class Context:
 
     def kv4_append(self, cache: Kv4Cache, k, v, slots):
         """ivit_kv4_append: int8 rows [tokens, heads d] into the rows of the pool that slots (int64) names; negative: left out."""
-        shape = self._want("k", torch.int8, 2, k)
+        shape, ldk = self._want("k", torch.int8, 2, k)
+        v_shape, ldv = self._want("v", torch.int8, 2, v)
         n, width = shape
-        if (self._want("v", torch.int8, 2, v) != shape or self._want("slots", torch.int64, 1, slots)[0] != n or width != cache.width or
-                cache.index != self.index):
+        if v_shape != shape or self._want("slots", torch.int64, 1, slots)[0][0] != n or width != cache.width or cache.index != self.index:
             raise ValueError("k and v are [tokens, heads d], slots [tokens], the pool is on the context's device")
-        rc = self.lib.ivit_kv4_append(self.h, cache.ref, k.data_ptr(), _row_ld(k, n, width), v.data_ptr(), _row_ld(v, n, width), slots.data_ptr(), n)
+        rc = self.lib.ivit_kv4_append(self.h, cache.ref, k.data_ptr(), ldk, v.data_ptr(), ldv, slots.data_ptr(), n)
         if rc:
             raise IvitError(rc, "ivit_kv4_append")
 
@@ -491,27 +496,26 @@ class Context:
                       out=None, weights=None):
         """ivit_kv4_attention: query rows [tokens, query heads d] of len(lens) sequences over the cache; returns int8 rows of the same
         shape (a new one starts as zeros, rows of no sequence keep what out held).  weights (int64 [seqs, heads, >= max_len]) is added to."""
-        shape = self._want("q", torch.int8, 2, q)
+        shape, ldq = self._want("q", torch.int8, 2, q)
         n, width = shape
         if out is None:
             out = torch.zeros((n, width), dtype=torch.int8, device=q.device)
-        elif self._want("out", torch.int8, 2, out) != shape:
-            raise ValueError("out has the shape of q")
-        seqs, = self._want("lens", torch.int32, 1, lens)
-        t_rows, t_cols = self._want("table", torch.int32, 2, table)
-        if (self._want("q_start", torch.int32, 1, q_start)[0] != seqs + 1 or t_rows != seqs or width % cache.d or t_cols * cache.page < max_len or
-                cache.index != self.index):
-            raise ValueError("q is [tokens, query heads d], q_start [seqs + 1], table [seqs, pages for max_len keys], the pool is on the context's device")
-        p_w, ldw = None, 0
+        o_shape, ldo = self._want("out", torch.int8, 2, out)
+        (seqs,), _ = self._want("lens", torch.int32, 1, lens)
+        (t_rows, t_cols), ldt = self._want("table", torch.int32, 2, table)
+        if (o_shape != shape or self._want("q_start", torch.int32, 1, q_start)[0][0] != seqs + 1 or t_rows != seqs or width % cache.d or
+                t_cols * cache.page < max_len or cache.index != self.index):
+            raise ValueError("q and out are [tokens, query heads d], q_start [seqs + 1], table [seqs, pages for max_len keys], the pool is on the "
+                             "context's device")
+        p_w, ldw = 0, 0
         if weights is not None:
-            w_seqs, w_heads, ldw = self._want("weights", torch.int64, 3, weights)
+            (w_seqs, w_heads, ldw), _ = self._want("weights", torch.int64, 3, weights)
             if w_seqs != seqs or w_heads != cache.heads or not weights.is_contiguous():
                 raise ValueError("weights is a contiguous [seqs, heads, keys]")
             p_w = weights.data_ptr()
-        rc = self.lib.ivit_kv4_attention(self.h, cache.ref, q.data_ptr(), _row_ld(q, n, width), width // cache.d, n, q_start.data_ptr(),
-                                         lens.data_ptr(), table.data_ptr(), _row_ld(table, seqs, t_cols), qk_scale.c,
-                                         smax if type(smax) is CExp else _cexp(smax), pv_scale.c, out.data_ptr(), _row_ld(out, n, width), p_w, ldw,
-                                         seqs, max_q, max_len)
+        rc = self.lib.ivit_kv4_attention(self.h, cache.ref, _ATTENTION.pack(
+            q.data_ptr(), ldq, out.data_ptr(), ldo, q_start.data_ptr(), lens.data_ptr(), table.data_ptr(), ldt, p_w, ldw, width // cache.d, n, seqs,
+            max_q, max_len, *qk_scale.fields, *pv_scale.fields, smax.I0, smax.N, smax.M, smax.k_out))
         if rc:
             raise IvitError(rc, "ivit_kv4_attention")
         return out
@@ -520,25 +524,25 @@ class Context:
                   weights_out=None, kept=None, new_lens=None):
         """ivit_kv4_evict: at most `keep` keys of each sequence and head stay; in place unless dst_table and weights_out are given.
         Returns (kept [seqs, heads, keep], new_lens [seqs])."""
-        seqs, = self._want("lens", torch.int32, 1, lens)
+        (seqs,), _ = self._want("lens", torch.int32, 1, lens)
         dst_table = table if dst_table is None else dst_table
         weights_out = weights if weights_out is None else weights_out
         kept = torch.empty((seqs, cache.heads, keep), dtype=torch.int32, device=self.device) if kept is None else kept
         new_lens = torch.empty_like(lens) if new_lens is None else new_lens
-        ws, wh, ldw = self._want("weights", torch.int64, 3, weights)
-        os_, oh, ldo = self._want("weights_out", torch.int64, 3, weights_out)
-        ks, kh, kk = self._want("kept", torch.int32, 3, kept)
-        ts, tc = self._want("table", torch.int32, 2, table)
-        ds, dc = self._want("dst_table", torch.int32, 2, dst_table)
-        if not (ws == os_ == ks == ts == ds == seqs == self._want("new_lens", torch.int32, 1, new_lens)[0] and wh == oh == kh == cache.heads and
+        (ws, wh, ldw), _ = self._want("weights", torch.int64, 3, weights)
+        (os_, oh, ldo), _ = self._want("weights_out", torch.int64, 3, weights_out)
+        (ks, kh, kk), _ = self._want("kept", torch.int32, 3, kept)
+        (ts, tc), ldt = self._want("table", torch.int32, 2, table)
+        (ds, dc), ldd = self._want("dst_table", torch.int32, 2, dst_table)
+        if not (ws == os_ == ks == ts == ds == seqs == self._want("new_lens", torch.int32, 1, new_lens)[0][0] and wh == oh == kh == cache.heads and
                 weights.is_contiguous() and weights_out.is_contiguous() and kept.is_contiguous() and kk == keep and cache.index == self.index):
             raise ValueError("lens and new_lens are [seqs], weights and weights_out contiguous [seqs, heads, keys], kept contiguous "
                              "[seqs, heads, keep], the tables [seqs, pages], the pool is on the context's device")
         if tc * cache.page < max_len or dc * cache.page < min(keep, max_len):
             raise ValueError("the tables name pages for max_len and keep keys of each sequence")
-        rc = self.lib.ivit_kv4_evict(self.h, cache.ref, weights.data_ptr(), ldw, lens.data_ptr(), table.data_ptr(), _row_ld(table, seqs, tc),
-                                     dst_table.data_ptr(), _row_ld(dst_table, seqs, dc), weights_out.data_ptr(), ldo, kept.data_ptr(),
-                                     new_lens.data_ptr(), seqs, max_len, keep, sinks, recent)
+        rc = self.lib.ivit_kv4_evict(self.h, cache.ref, _EVICT.pack(
+            weights.data_ptr(), ldw, weights_out.data_ptr(), ldo, lens.data_ptr(), new_lens.data_ptr(), table.data_ptr(), ldt, dst_table.data_ptr(), ldd,
+            kept.data_ptr(), seqs, max_len, keep, sinks, recent))
         if rc:
             raise IvitError(rc, "ivit_kv4_evict")
         return kept, new_lens

@@ -280,20 +280,13 @@ int launch_shiftgelu_static(ivit_ctx* ctx, const int8_t* in, int64_t ldin, ivit_
                             int8_t* out, int64_t ldout, int64_t rows, int64_t cols);
 int launch_shiftgelu(ivit_ctx* ctx, const int8_t* in, int64_t ldin, ivit_exp_params p, ivit_scale post,
                      int8_t* out, int64_t ldout, int64_t rows, int64_t cols);
-int launch_rmsnorm(ivit_ctx* ctx, const void* x, int x_dtype, int64_t ldx, ScaleDev xs, const void* res, int res_dtype, int64_t ldres,
-                   ScaleDev rs, ScaleDev gs, int M_ln, void* sum, int64_t ldsum, int8_t* out, int64_t ldout, int32_t* row_max,
-                   int64_t rows, int64_t C);
-// The cache in 4 bits (kv4.cu); kv4_prepare_device: shared-memory limits of its kernels, for the current device.
+int launch_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params& p);
+// The cache in 4 bits (kv4.cu, kv4_attention.cu); kv4_prepare_device: shared-memory limits of its kernels, for the current device.
 int kv4_prepare_device();
 int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
                       const int64_t* slots, int64_t tokens);
-int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
-                         const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable, ivit_scale qk_scale,
-                         ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo, int64_t* weights, int64_t ldw, int64_t seqs,
-                         int64_t max_q, int64_t max_len);
-int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens, const int32_t* table,
-                     int64_t ldtable, const int32_t* dst_table, int64_t ld_dst, int64_t* weights_out, int64_t ldw_out, int32_t* kept,
-                     int32_t* new_lens, int64_t seqs, int64_t max_len, int64_t keep, int64_t sinks, int64_t recent);
+int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_kv4_attention_params& p);
+int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_kv4_evict_params& p);
 int launch_patchify(ivit_ctx* ctx, const int8_t* img, int64_t B, int64_t C, int64_t Hi, int64_t Wi,
                     int64_t P, int64_t window, int8_t* out, int64_t ldout, const int8_t* fill_src = nullptr, int64_t fill_width = 0,
                     int8_t* fill_dst = nullptr, int64_t fill_stride = 0);   // fill_src: also this row to every image's fill_dst

@@ -1086,24 +1086,22 @@ const char* ivit_kernel_kind_name(int32_t kind) {
   }
 }
 
-int ivit_rmsnorm(ivit_ctx* ctx, const void* x, int32_t x_dtype, int64_t ldx, ivit_scale x_scale, const void* res, int32_t res_dtype,
-                 int64_t ldres, ivit_scale res_scale, ivit_scale gamma_scale, int32_t M_ln, void* sum, int64_t ldsum, int8_t* out,
-                 int64_t ldout, int32_t* row_max, int64_t rows, int64_t C) {
-  if (!ctx || rows < 0 || C < 1 || (rows > 0 && (!x || !out)) || (sum && !res)) return IVIT_ERR_INVALID_ARG;
-  if (x_dtype != IVIT_I8 && x_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
-  if (res && res_dtype != IVIT_I8 && res_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
-  if (C % 4 || C > 16384 || rows > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
-  if (M_ln < 8 || M_ln > 22) return IVIT_ERR_RANGE;
-  if (ldx < C || ldout < C || (res && ldres < C) || (sum && ldsum < C)) return IVIT_ERR_INVALID_ARG;
-  auto misaligned = [](const void* p, int64_t ld, int dtype) { return !aligned16(p) || ld % (dtype == IVIT_I8 ? 16 : 4); };
-  if (misaligned(x, ldx, x_dtype) || misaligned(out, ldout, IVIT_I8) || !aligned4(row_max)) return IVIT_ERR_ALIGNMENT;
-  if ((res && misaligned(res, ldres, res_dtype)) || (sum && misaligned(sum, ldsum, res_dtype))) return IVIT_ERR_ALIGNMENT;
-  if (!scale_ok(gamma_scale) || (res && (!scale_ok(x_scale) || !scale_ok(res_scale) || res_scale.mult_c))) return IVIT_ERR_RANGE;
-  if (!aligned4(gamma_scale.mult_c) || (res && !aligned4(x_scale.mult_c))) return IVIT_ERR_ALIGNMENT;
+int ivit_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params* p) {
+  if (!ctx || !p || p->rows < 0 || p->C < 1 || (p->rows > 0 && (!p->x || !p->out)) || (p->sum && !p->res)) return IVIT_ERR_INVALID_ARG;
+  if (p->x_dtype != IVIT_I8 && p->x_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
+  if (p->res && p->res_dtype != IVIT_I8 && p->res_dtype != IVIT_I32) return IVIT_ERR_INVALID_ARG;
+  if (p->C % 4 || p->C > 16384 || p->rows > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  if (p->M_ln < 8 || p->M_ln > 22) return IVIT_ERR_RANGE;
+  if (p->ldx < p->C || p->ldout < p->C || (p->res && p->ldres < p->C) || (p->sum && p->ldsum < p->C)) return IVIT_ERR_INVALID_ARG;
+  auto misaligned = [](const void* q, int64_t ld, int dtype) { return !aligned16(q) || ld % (dtype == IVIT_I8 ? 16 : 4); };
+  if (misaligned(p->x, p->ldx, p->x_dtype) || misaligned(p->out, p->ldout, IVIT_I8) || !aligned4(p->row_max)) return IVIT_ERR_ALIGNMENT;
+  if ((p->res && misaligned(p->res, p->ldres, p->res_dtype)) || (p->sum && misaligned(p->sum, p->ldsum, p->res_dtype))) return IVIT_ERR_ALIGNMENT;
+  if (!scale_ok(p->gamma_scale) || (p->res && (!scale_ok(p->x_scale) || !scale_ok(p->res_scale) || p->res_scale.mult_c))) return IVIT_ERR_RANGE;
+  if (!aligned4(p->gamma_scale.mult_c) || (p->res && !aligned4(p->x_scale.mult_c))) return IVIT_ERR_ALIGNMENT;
+  if (p->rows == 0) return IVIT_OK;
   DeviceGuard guard(ctx);
   if (!guard.ok) return IVIT_ERR_CUDA;
-  return launch_rmsnorm(ctx, x, x_dtype, ldx, to_dev(x_scale), res, res_dtype, ldres, to_dev(res_scale), to_dev(gamma_scale), M_ln, sum, ldsum,
-                        out, ldout, row_max, rows, C);
+  return launch_rmsnorm(ctx, *p);
 }
 
 static int check_kv4(const ivit_kv4_cache* c, bool data) {
@@ -1131,52 +1129,51 @@ int ivit_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K,
   return launch_kv4_append(ctx, cache, K, ldk, V, ldv, slots, tokens);
 }
 
-int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
-                       const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable, ivit_scale qk_scale,
-                       ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo, int64_t* weights, int64_t ldw, int64_t seqs,
-                       int64_t max_q, int64_t max_len) {
-  if (!ctx || tokens < 0 || seqs < 0 || max_q < 0 || max_len < 0) return IVIT_ERR_INVALID_ARG;
-  const bool any = tokens > 0 && seqs > 0 && max_q > 0;   // (nothing to do: pointers may be null)
-  if (any && (!Q || !O || Q == O || !q_start || !lens || (!table && max_len > 0))) return IVIT_ERR_INVALID_ARG;
-  int rc = check_kv4(cache, true);
+int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_attention_params* p) {
+  if (!ctx || !p || p->tokens < 0 || p->seqs < 0 || p->max_q < 0 || p->max_len < 0) return IVIT_ERR_INVALID_ARG;
+  const bool any = p->tokens > 0 && p->seqs > 0 && p->max_q > 0;   // (nothing to do: pointers may be null)
+  if (any && (!p->Q || !p->O || p->Q == p->O || !p->q_start || !p->lens || (!p->table && p->max_len > 0))) return IVIT_ERR_INVALID_ARG;
+  const int rc = check_kv4(cache, true);
   if (rc) return rc;
-  if (q_heads < cache->heads || q_heads % cache->heads) return IVIT_ERR_INVALID_ARG;
-  if (ldq < q_heads * cache->d || ldo < q_heads * cache->d || ldtable < (max_len + cache->page - 1) / cache->page || (weights && ldw < max_len))
+  if (p->q_heads < cache->heads || p->q_heads % cache->heads) return IVIT_ERR_INVALID_ARG;
+  if (p->max_len > IVIT_KV4_MAX_LEN || p->seqs > 65535 || p->q_heads > 65535 || p->max_q > 0xffffff ||
+      p->max_q * (p->q_heads / cache->heads) > 0x7fffff00ll || p->tokens > 0x7fffffffll)
+    return IVIT_ERR_UNSUPPORTED;
+  if (p->ldq < p->q_heads * cache->d || p->ldo < p->q_heads * cache->d || p->ldtable < (p->max_len + cache->page - 1) / cache->page ||
+      (p->weights && p->ldw < p->max_len))
     return IVIT_ERR_INVALID_ARG;
-  if (max_len > IVIT_KV4_MAX_LEN || seqs > 65535 || q_heads > 65535 || max_q > 0xffffff || max_q * (q_heads / cache->heads) > 0x7fffff00ll || tokens > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
-  if (!aligned16(Q) || !aligned16(O) || ldq % 16 || ldo % 16 || !aligned4(q_start) || !aligned4(lens) || !aligned4(table) ||
-      (reinterpret_cast<uintptr_t>(weights) & 7))
+  if (!aligned16(p->Q) || !aligned16(p->O) || p->ldq % 16 || p->ldo % 16 || !aligned4(p->q_start) || !aligned4(p->lens) || !aligned4(p->table) ||
+      (reinterpret_cast<uintptr_t>(p->weights) & 7))
     return IVIT_ERR_ALIGNMENT;
-  if (!scale_ok(qk_scale) || !scale_ok(pv_scale) || qk_scale.mult_c || pv_scale.mult_c) return IVIT_ERR_RANGE;
-  if (smax.I0 < 1 || smax.I0 > (1 << 15) || smax.N < 0 || smax.N > 24 || smax.M != 45) return IVIT_ERR_RANGE;
-  const int64_t top = (int64_t)smax.I0 << smax.N;
+  if (!scale_ok(p->qk_scale) || !scale_ok(p->pv_scale) || p->qk_scale.mult_c || p->pv_scale.mult_c) return IVIT_ERR_RANGE;
+  if (p->smax.I0 < 1 || p->smax.I0 > (1 << 15) || p->smax.N < 0 || p->smax.N > 24 || p->smax.M != 45) return IVIT_ERR_RANGE;
+  const int64_t top = (int64_t)p->smax.I0 << p->smax.N;
   if (top < (1 << 14) || top >= (1 << 24)) return IVIT_ERR_RANGE;
   if (!any) return IVIT_OK;
   DeviceGuard guard(ctx);
   if (!guard.ok) return IVIT_ERR_CUDA;
-  return launch_kv4_attention(ctx, cache, Q, ldq, q_heads, tokens, q_start, lens, table, ldtable, qk_scale, smax, pv_scale, O, ldo, weights, ldw,
-                              seqs, max_q, max_len);
+  return launch_kv4_attention(ctx, *cache, *p);
 }
 
-int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens, const int32_t* table,
-                   int64_t ldtable, const int32_t* dst_table, int64_t ld_dst, int64_t* weights_out, int64_t ldw_out, int32_t* kept,
-                   int32_t* new_lens, int64_t seqs, int64_t max_len, int64_t keep, int64_t sinks, int64_t recent) {
-  if (!ctx || seqs < 0 || max_len < 0) return IVIT_ERR_INVALID_ARG;
-  if (seqs > 0 && (!weights || !lens || !table || !dst_table || !weights_out || !kept || !new_lens)) return IVIT_ERR_INVALID_ARG;
-  int rc = check_kv4(cache, true);
+int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_evict_params* p) {
+  if (!ctx || !p || p->seqs < 0 || p->max_len < 0) return IVIT_ERR_INVALID_ARG;
+  if (p->seqs > 0 && (!p->weights || !p->lens || !p->table || !p->dst_table || !p->weights_out || !p->kept || !p->new_lens)) return IVIT_ERR_INVALID_ARG;
+  const int rc = check_kv4(cache, true);
   if (rc) return rc;
-  if (keep < 1 || sinks < 0 || recent < 0 || sinks > keep || recent > keep - sinks) return IVIT_ERR_INVALID_ARG;
-  if (seqs > 65535 || max_len > 0x7fffffffll || keep > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
-  const int64_t rows = keep < max_len ? keep : max_len;
-  if (ldw < max_len || ldw_out < keep || ldtable < (max_len + cache->page - 1) / cache->page || ld_dst < (rows + cache->page - 1) / cache->page)
+  if (p->keep < 1 || p->sinks < 0 || p->recent < 0 || p->sinks > p->keep || p->recent > p->keep - p->sinks) return IVIT_ERR_INVALID_ARG;
+  if (p->seqs > 65535 || p->max_len > 0x7fffffffll || p->keep > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  const int64_t rows = p->keep < p->max_len ? p->keep : p->max_len;
+  if (p->ldw < p->max_len || p->ldw_out < p->keep || p->ldtable < (p->max_len + cache->page - 1) / cache->page ||
+      p->ld_dst < (rows + cache->page - 1) / cache->page)
     return IVIT_ERR_INVALID_ARG;
-  if ((dst_table == table && ld_dst != ldtable) || (weights_out == weights && ldw_out != ldw)) return IVIT_ERR_INVALID_ARG;
-  const uintptr_t al8 = reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(weights_out);
-  if ((al8 & 7) || !aligned4(lens) || !aligned4(table) || !aligned4(dst_table) || !aligned4(kept) || !aligned4(new_lens)) return IVIT_ERR_ALIGNMENT;
+  if ((p->dst_table == p->table && p->ld_dst != p->ldtable) || (p->weights_out == p->weights && p->ldw_out != p->ldw)) return IVIT_ERR_INVALID_ARG;
+  const uintptr_t al8 = reinterpret_cast<uintptr_t>(p->weights) | reinterpret_cast<uintptr_t>(p->weights_out);
+  if ((al8 & 7) || !aligned4(p->lens) || !aligned4(p->table) || !aligned4(p->dst_table) || !aligned4(p->kept) || !aligned4(p->new_lens))
+    return IVIT_ERR_ALIGNMENT;
+  if (p->seqs == 0) return IVIT_OK;
   DeviceGuard guard(ctx);
   if (!guard.ok) return IVIT_ERR_CUDA;
-  return launch_kv4_evict(ctx, cache, weights, ldw, lens, table, ldtable, dst_table, ld_dst, weights_out, ldw_out, kept, new_lens, seqs, max_len,
-                          keep, sinks, recent);
+  return launch_kv4_evict(ctx, *cache, *p);
 }
 
 int ivit_patchify(ivit_ctx* ctx, const int8_t* img, int64_t B, int64_t C, int64_t Hi, int64_t Wi,

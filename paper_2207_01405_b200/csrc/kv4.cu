@@ -1,5 +1,6 @@
 // A key/value cache held in 4 bits: append to it, eviction from it (sm_100a).  Layout: ivit_kv4_cache in ivit.h.
 #include "common.cuh"
+#include "kv4_layout.cuh"
 
 namespace ivit {
 
@@ -51,22 +52,12 @@ __device__ __forceinline__ uint32_t codes_of(uint32_t w, int step, unsigned r) {
   return step ? c : 0x08080808u;
 }
 
-struct HeadDiv {   // quotient of n < 2^31 by the number of heads: the product's upper word, shifted (multiplier of 32 bits, rounded up)
-  unsigned d, m;
-  int s;
-};
-static HeadDiv head_div(unsigned d) {
-  int l = 0;
-  while ((1u << l) < d) ++l;
-  return HeadDiv{d, d > 1 ? (unsigned)(((1ull << (31 + l)) + d - 1) / d) : 0u, l - 1};
-}
-
 // D / 8 lanes take a row of one token and head: eight channels each of K and of V, so that loads and stores of codes are runs of double
 // words; the lanes with a word's low and high halves are 2 apart in K, D / 16 apart in V.  U rows at a time keep loads in flight.  What
 // bounds it is the issue of instructions; with four channels a lane, and a division for each step and for the head, it took twice the time.
 template <int D, int U>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const int8_t* __restrict__ K, int64_t ldk, const int8_t* __restrict__ V,
-                                                         int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, HeadDiv by_heads, int* status) {
+                                                         int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, Kv4Div by_heads, int* status) {
   constexpr int L = D / 8, kPer = 256 / L;       // lanes of a row, rows of a CTA
   __shared__ unsigned recip[256];
   if (threadIdx.x < 148) recip[threadIdx.x] = threadIdx.x ? (1u << 23) / threadIdx.x + 1u : 0u;
@@ -79,7 +70,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const in
   int h[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const unsigned r = min(r0 + u * kPer, rows - 1), t = by_heads.d == 1 ? r : __umulhi(r, by_heads.m) >> by_heads.s;
+    const unsigned r = min(r0 + u * kPer, rows - 1), t = (unsigned)by_heads.div((int)r);
     h[u] = (int)(r - t * by_heads.d);
     k[u] = *reinterpret_cast<const uint2*>(K + t * ldk + (h[u] * D + 8 * l));
     v[u] = *reinterpret_cast<const uint2*>(V + t * ldv + (h[u] * D + 8 * l));
@@ -128,7 +119,7 @@ int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* 
   const bool many = rows >= 64u * (unsigned)ctx->sm_count;    // (below, the rows are better spread over the SMs)
   const unsigned grid = (rows + (many ? 4 * per : per) - 1) / (many ? 4 * per : per);
   auto go = [&](auto k) {
-    launch_k(k, grid, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, head_div((unsigned)cache->heads), ctx->status_dev);
+    launch_k(k, grid, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, kv4_div((unsigned)cache->heads), ctx->status_dev);
   };
   if (cache->d == 128) many ? go(kv4_append_kernel<128, 4>) : go(kv4_append_kernel<128, 1>);
   else many ? go(kv4_append_kernel<64, 4>) : go(kv4_append_kernel<64, 1>);
@@ -394,26 +385,23 @@ __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const
   if (h == 0 && blockIdx.x == 0 && tid == 0) a.new_lens[b] = n;
 }
 
-int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int64_t* weights, int64_t ldw, const int32_t* lens, const int32_t* table,
-                     int64_t ldtable, const int32_t* dst_table, int64_t ld_dst, int64_t* weights_out, int64_t ldw_out, int32_t* kept,
-                     int32_t* new_lens, int64_t seqs, int64_t max_len, int64_t keep, int64_t sinks, int64_t recent) {
-  if (seqs == 0) return IVIT_OK;
-  const EvictArgs a{to_dev(cache), weights, ldw, lens, table, ldtable, dst_table, ld_dst, weights_out, ldw_out, kept, new_lens, (int)max_len,
-                    (int)keep, (int)sinks, (int)recent, ctx->status_dev};
+int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_kv4_evict_params& p) {
+  const EvictArgs a{to_dev(&cache), p.weights, p.ldw, p.lens, p.table, p.ldtable, p.dst_table, p.ld_dst, p.weights_out, p.ldw_out, p.kept, p.new_lens,
+                    (int)p.max_len, (int)p.keep, (int)p.sinks, (int)p.recent, ctx->status_dev};
   int rc;
   {
-    LaunchScope ls(ctx, KIND_MOVE, 8.0 * seqs * cache->heads * max_len);
-    const dim3 grid((unsigned)cache->heads, (unsigned)seqs);
-    if (max_len <= 16384) launch_k(kv4_select_kernel<true>, grid, 1024, 0, ctx->stream, a);
+    LaunchScope ls(ctx, KIND_MOVE, 8.0 * p.seqs * cache.heads * p.max_len);
+    const dim3 grid((unsigned)cache.heads, (unsigned)p.seqs);
+    if (p.max_len <= 16384) launch_k(kv4_select_kernel<true>, grid, 1024, 0, ctx->stream, a);
     else launch_k(kv4_select_kernel<false>, grid, 1024, 0, ctx->stream, a);
     if ((rc = ls.done())) return rc;
   }
-  LaunchScope ls(ctx, KIND_MOVE, 2.0 * seqs * cache->heads * keep * (cache->d + cache->d / 32 + 9));
   // in place (of the pages, or of the weights): in order
-  const bool ordered = dst_table == table || weights_out == weights;
-  const int64_t rows = keep < max_len ? keep : max_len, per = 4 * 256 / (cache->d / 16);
-  const dim3 grid(ordered ? 1u : (unsigned)(rows > per ? (rows + per - 1) / per : 1), (unsigned)cache->heads, (unsigned)seqs);
-  if (cache->d == 128) ordered ? launch_k(kv4_compact_kernel<128, true>, grid, 512, 0, ctx->stream, a) : launch_k(kv4_compact_kernel<128, false>, grid, 256, 0, ctx->stream, a);
+  const bool ordered = p.dst_table == p.table || p.weights_out == p.weights;
+  const int64_t rows = p.keep < p.max_len ? p.keep : p.max_len, per = 4 * 256 / (cache.d / 16);
+  const dim3 grid(ordered ? 1u : (unsigned)(rows > per ? (rows + per - 1) / per : 1), (unsigned)cache.heads, (unsigned)p.seqs);
+  LaunchScope ls(ctx, KIND_MOVE, 2.0 * p.seqs * cache.heads * rows * (cache.d + cache.d / 32 + 9));
+  if (cache.d == 128) ordered ? launch_k(kv4_compact_kernel<128, true>, grid, 512, 0, ctx->stream, a) : launch_k(kv4_compact_kernel<128, false>, grid, 256, 0, ctx->stream, a);
   else ordered ? launch_k(kv4_compact_kernel<64, true>, grid, 512, 0, ctx->stream, a) : launch_k(kv4_compact_kernel<64, false>, grid, 256, 0, ctx->stream, a);
   return ls.done();
 }

@@ -11,7 +11,7 @@ struct AttendArgs {
   int64_t pages, block_bytes;
   int heads, page, page_log;
   const int8_t* Q; int64_t ldq;
-  int group;                       // query heads per key/value head
+  Kv4Div group;                    // query heads per key/value head
   int64_t tokens;
   const int32_t *q_start, *lens, *table;
   int64_t ldtable;
@@ -93,20 +93,6 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
   return e;
 }
 
-__device__ __forceinline__ int cut_of(unsigned long long den) { return max(0, 32 - __clzll((long long)den)); }
-__device__ __forceinline__ unsigned long long recip_of(unsigned long long den) { return den ? ~0ull / (den >> cut_of(den)) : 0; }
-
-// floor(w / den) for |w| <= 2^24 den, den < 2^43 (0 for den = w = 0): both are cut to a divisor of at most 32 bits, whose quotient is off by at most one (the
-// cut moves it by less than 2^24 2^-31), and multiplied back.  cut = cut_of(den), r = recip_of(den).
-__device__ __forceinline__ int small_quotient(long long w, unsigned long long den, int cut, unsigned long long r) {
-  const unsigned long long a = w < 0 ? 0ull - (unsigned long long)w : (unsigned long long)w;
-  int q = (int)__umul64hi(a >> cut, r);
-  long long left = (long long)(a - (unsigned long long)(unsigned)q * den);
-  if (left < 0) { --q; left += (long long)den; }
-  if (left >= (long long)den && den) { ++q; left -= (long long)den; }
-  return w < 0 ? -q - (left != 0) : q;
-}
-
 // ---------------------------------------------------------------- the kernel
 //
 // A cluster of `split` CTAs takes up to 8 RN query rows (of one sequence, all of them readers of one key/value head) and shares the
@@ -175,26 +161,28 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   int q_at[RN], q_head[RN];                            // query token and head (of the group's) of the lane's rows
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
-    q_at[j] = (row0 + 8 * j + n8) / a.group;
-    q_head[j] = row0 + 8 * j + n8 - q_at[j] * a.group;
+    q_at[j] = a.group.div(row0 + 8 * j + n8);
+    q_head[j] = row0 + 8 * j + n8 - q_at[j] * (int)a.group.d;
   }
   pdl_wait();
   pdl_trigger();
+  // (not split: the first pages are known without the lengths, and fetched beside them)
+  const int early = a.split == 1 && (tid << a.page_log) < a.max_len ? a.table[b * a.ldtable + tid] : 0;
   const Kv4Seq seq = kv4_sequence(a.q_start[b], a.q_start[b + 1], a.lens[b], a.tokens, a.max_q, a.max_len);
   if (seq.bad && tid == 0) *(volatile int*)a.status = IVIT_ERR_RANGE;
-  const int nrows = min(kRows, seq.n * a.group - row0);
+  const int nrows = min(kRows, seq.n * (int)a.group.d - row0);
   if (nrows <= 0) {                        // (the whole cluster)
     if (a.split > 1) cluster_wait();
     return;
   }
   // keys that some row of the tile sees, and this CTA's run of them
-  const int seen_all = kv4_seen(seq, (row0 + nrows - 1) / a.group), seen_min = kv4_seen(seq, row0 / a.group);
+  const int seen_all = kv4_seen(seq, a.group.div(row0 + nrows - 1)), seen_min = kv4_seen(seq, a.group.div(row0));
   const int blks = (seen_all + kKv4Block - 1) / kKv4Block, run = (blks + a.split - 1) / a.split;
   const int blk0 = rank * run, nblk = max(0, min(run, blks - blk0));
   const int page0 = blk0 * kKv4Block >> a.page_log;
   bool bad = false;
   for (int i = tid; i < (nblk > 0 ? ((blk0 + nblk) * kKv4Block - 1 >> a.page_log) - page0 + 1 : 0); i += 256) {
-    const int pg = a.table[b * a.ldtable + page0 + i];
+    const int pg = a.split == 1 && i < 256 ? early : a.table[b * a.ldtable + page0 + i];
     const bool there = pg >= 0 && pg < a.pages;
     if (!there) {
       bad = true;
@@ -206,14 +194,14 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
     for (int j = 0; j < RN; ++j) {
       lim[8 * j + n8] = 8 * j + n8 < nrows ? kv4_seen(seq, q_at[j]) : 0;
-      row_out[8 * j + n8] = (unsigned long long)((seq.q0 + q_at[j]) * a.ldo + (int64_t)(h * a.group + q_head[j]) * D);
+      row_out[8 * j + n8] = (unsigned long long)((seq.q0 + q_at[j]) * a.ldo + (int64_t)(h * (int)a.group.d + q_head[j]) * D);
     }
   // B operand of the scores: the lane's query row of each tile of eight, bytes 32 g + 4 t.. and 32 g + 16 + 4 t..
   uint32_t q[RN][kG][2];
 #pragma unroll
   for (int j = 0; j < RN; ++j) {
     const bool there = 8 * j + n8 < nrows;
-    const int8_t* src = a.Q + (there ? (seq.q0 + q_at[j]) * a.ldq + (int64_t)(h * a.group + q_head[j]) * D : 0) + 4 * t4;
+    const int8_t* src = a.Q + (there ? (seq.q0 + q_at[j]) * a.ldq + (int64_t)(h * (int)a.group.d + q_head[j]) * D : 0) + 4 * t4;
 #pragma unroll
     for (int g = 0; g < kG; ++g) {
       q[j][g][0] = there ? *reinterpret_cast<const uint32_t*>(src + 32 * g) : 0;
@@ -524,8 +512,12 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
     for (int i = 0; i < kTurns; ++i)
       if (tid + 256 * i < own) {
+        long long v[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = k < a.split ? part_in[k * own + tid + 256 * i] : 0;
         part[i] = 0;
-        for (int k = 0; k < a.split; ++k) part[i] += part_in[k * own + tid + 256 * i];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) part[i] += v[k];
       }
   }
   __syncthreads();
@@ -538,7 +530,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     const unsigned long long den_row = row_den[row];
     // (codes came in as code + 8, the upper half's sixteenfold; a row that sees nothing: every number is zero)
     const long long num = (part[i] >> (ch < D / 2 ? 0 : 4)) - 8 * (long long)row_u[row];
-    const int t = small_quotient(num * (1ll << (a.z + 5)), den_row, cut_of(den_row), row_recip[row]);
+    const int t = small_quotient(num * (1ll << (a.z + 5)), den_row, row_recip[row]);
     if (tid + 256 * i < own && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
   }
 
@@ -548,7 +540,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
     for (int i = tid; i < nrows * 256; i += 256) {
       const unsigned long long den_row = row_den[i >> 8];
       const unsigned e = *reinterpret_cast<const unsigned*>(sm + at.table + (i & 255) * (4 * kKv4Copies)) >> (16 - a.z);
-      share[i] = den_row ? (unsigned)small_quotient((long long)e << 24, den_row, cut_of(den_row), row_recip[i >> 8]) : 0;
+      share[i] = den_row ? (unsigned)small_quotient((long long)e << 24, den_row, row_recip[i >> 8]) : 0;
     }
     __syncthreads();
     unsigned long long* w = reinterpret_cast<unsigned long long*>(a.weights) + ((int64_t)b * a.heads + h) * a.ldw;
@@ -591,36 +583,33 @@ int kv4_prepare_device() {
   });
 }
 
-int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* Q, int64_t ldq, int64_t q_heads, int64_t tokens,
-                         const int32_t* q_start, const int32_t* lens, const int32_t* table, int64_t ldtable, ivit_scale qk_scale,
-                         ivit_exp_params smax, ivit_scale pv_scale, int8_t* O, int64_t ldo, int64_t* weights, int64_t ldw, int64_t seqs,
-                         int64_t max_q, int64_t max_len) {
-  const int d = (int)cache->d, page = (int)cache->page;
-  const int64_t group = q_heads / cache->heads;
-  const Kv4Plan p = kv4_plan(d, page, group, cache->heads, seqs, max_q, max_len, ctx->sm_count);
+int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_kv4_attention_params& c) {
+  const int d = (int)cache.d, page = (int)cache.page;
+  const int64_t group = c.q_heads / cache.heads;
+  const Kv4Plan p = kv4_plan(d, page, group, cache.heads, c.seqs, c.max_q, c.max_len, ctx->sm_count);
   if (p.smem > kKv4SmemMax || (int64_t)p.tiles * p.split > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
   AttendArgs a{};
-  a.data = cache->data; a.pages = cache->pages; a.block_bytes = kv4_block_bytes(d, page);
-  a.heads = (int)cache->heads; a.page = page;
+  a.data = cache.data; a.pages = cache.pages; a.block_bytes = kv4_block_bytes(d, page);
+  a.heads = (int)cache.heads; a.page = page;
   while ((1 << a.page_log) < page) ++a.page_log;
-  a.Q = Q; a.ldq = ldq; a.group = (int)group; a.tokens = tokens;
-  a.q_start = q_start; a.lens = lens; a.table = table; a.ldtable = ldtable;
+  a.Q = c.Q; a.ldq = c.ldq; a.group = kv4_div((unsigned)group); a.tokens = c.tokens;
+  a.q_start = c.q_start; a.lens = c.lens; a.table = c.table; a.ldtable = c.ldtable;
   // rq(x; m, s) = rq(16 x; m, s + 4), whose shift is beyond 32: the rounding constant is a whole number in the product's upper word.  Beyond a
   // shift of 59 every value rounds to zero (|16 x| < 2^30, m < 2^31).
-  const int s16 = qk_scale.shift + 4;
-  a.qk_mult = s16 <= 63 ? qk_scale.mult : 0;
+  const int s16 = c.qk_scale.shift + 4;
+  a.qk_mult = s16 <= 63 ? c.qk_scale.mult : 0;
   a.qk_add = s16 <= 63 ? 1 << (s16 - 33) : 0;
   a.qk_sh = s16 <= 63 ? s16 - 32 : 0;
-  a.pv_mult = pv_scale.mult; a.pv_shift = pv_scale.shift; a.I0 = smax.I0; a.N = smax.N;
-  const int64_t top = (int64_t)smax.I0 << smax.N;
-  while (top >> (a.z + 8)) ++a.z;
-  a.O = O; a.ldo = ldo; a.weights = weights; a.ldw = ldw;
-  a.max_q = (int)max_q; a.max_len = (int)max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept; a.stages = p.stages;
   a.sixteen = 16;
+  a.pv_mult = c.pv_scale.mult; a.pv_shift = c.pv_scale.shift; a.I0 = c.smax.I0; a.N = c.smax.N;
+  const int64_t top = (int64_t)c.smax.I0 << c.smax.N;
+  while (top >> (a.z + 8)) ++a.z;
+  a.O = c.O; a.ldo = c.ldo; a.weights = c.weights; a.ldw = c.ldw;
+  a.max_q = (int)c.max_q; a.max_len = (int)c.max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept; a.stages = p.stages;
   a.status = ctx->status_dev;
-  LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * seqs * q_heads * max_q * max_len * d);
+  LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * c.seqs * c.q_heads * c.max_q * c.max_len * d);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(p.tiles * p.split), (unsigned)cache->heads, (unsigned)seqs);
+  cfg.gridDim = dim3((unsigned)(p.tiles * p.split), (unsigned)cache.heads, (unsigned)c.seqs);
   cfg.blockDim = 256;
   cfg.dynamicSmemBytes = (size_t)p.smem;
   cfg.stream = ctx->stream;
@@ -633,7 +622,7 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_
   cfg.attrs = attr;
   cfg.numAttrs = p.split > 1 ? 2 : 1;
   each_kernel([&](auto k, int kd, int rn, bool w) {
-    if (kd == d && rn * 8 == p.rows && w == (weights != nullptr)) cudaLaunchKernelEx(&cfg, k, a);
+    if (kd == d && rn * 8 == p.rows && w == (c.weights != nullptr)) cudaLaunchKernelEx(&cfg, k, a);
     return (int)IVIT_OK;
   });
   return ls.done();

@@ -47,6 +47,59 @@ IVIT_KV4_FN int kv4_seen(const Kv4Seq& s, int t) {
   return v < 0 ? 0 : (v > s.len ? s.len : v);
 }
 
+// ---- quotients of the attention ----
+
+IVIT_KV4_FN int kv4_clz(unsigned long long n) {
+#ifdef __CUDA_ARCH__
+  return __clzll((long long)n);
+#else
+  return n ? __builtin_clzll(n) : 64;
+#endif
+}
+IVIT_KV4_FN unsigned long long kv4_mul_hi(unsigned long long a, unsigned long long b) {
+#ifdef __CUDA_ARCH__
+  return __umul64hi(a, b);
+#else
+  return (unsigned long long)(((unsigned __int128)a * b) >> 64);
+#endif
+}
+// About 2^64 / (den 2^up), up = leading zeros of den less 32 (den scaled to 32 bits with the upper one set; negative: cut): the reciprocal of
+// its upper 16 bits by a 32-bit division (off by 2^-15), then one step of Newton's iteration (2^-29).  den < 2^43; 0 for den = 0.
+// (A 64-bit division took 400 clocks more, with nothing beside it.)
+IVIT_KV4_FN int up_of(unsigned long long den) { return kv4_clz(den) - 32; }
+IVIT_KV4_FN unsigned long long recip_of(unsigned long long den) {
+  if (!den) return 0;
+  const int up = up_of(den);
+  const unsigned d = (unsigned)(up >= 0 ? den << up : den >> -up);
+  const unsigned v = 0xffffffffu / (d >> 16);                                       // about 2^48 / d, 17 bits
+  const long long e = (long long)((1ull << 48) - (unsigned long long)v * d);        // of 2^48, at most 2^33 or so
+  return ((unsigned long long)v << 16) + (unsigned long long)((e * (long long)v) >> 32);   // v 2^16 (1 + e / 2^48)
+}
+
+// floor(w / den) for |w| <= 2^24 den, den < 2^43 (0 for den = w = 0): the product with the reciprocal is off by less than 2^24 2^-28 and a
+// unit, so by one at most, and multiplied back.  r = recip_of(den).
+IVIT_KV4_FN int small_quotient(long long w, unsigned long long den, unsigned long long r) {
+  const unsigned long long a = w < 0 ? 0ull - (unsigned long long)w : (unsigned long long)w;
+  const int up = up_of(den);
+  int q = (int)kv4_mul_hi(up >= 0 ? a << up : a >> -up, r);
+  long long left = (long long)(a - (unsigned long long)(unsigned)q * den);
+  if (left < 0) { --q; left += (long long)den; }
+  if (left >= (long long)den && den) { ++q; left -= (long long)den; }
+  return w < 0 ? -q - (left != 0) : q;
+}
+
+// Quotient of 0 <= n < 2^31 by a divisor that the host knows: the product's upper word, shifted (a multiplier of 32 bits, rounded up).
+struct Kv4Div {
+  unsigned d, m;
+  int s;
+  IVIT_KV4_FN int div(int n) const { return d == 1 ? n : (int)((unsigned)(((unsigned long long)(unsigned)n * m) >> 32) >> s); }
+};
+inline Kv4Div kv4_div(unsigned d) {
+  int l = 0;
+  while ((1u << l) < d) ++l;
+  return Kv4Div{d, d > 1 ? (unsigned)(((1ull << (31 + l)) + d - 1) / d) : 0u, l - 1};
+}
+
 // ---- launch of the attention ----
 
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time

@@ -276,25 +276,23 @@ static void launch_rows(ivit_ctx* ctx, const RmsArgs& a) {
     launch_k(rmsnorm_kernel<XI, HI, 4, 1, kDyn, false>, (unsigned)a.rows, threads(4), 0, ctx->stream, a);
 }
 
-int launch_rmsnorm(ivit_ctx* ctx, const void* x, int x_dtype, int64_t ldx, ScaleDev xs, const void* res, int res_dtype, int64_t ldres,
-                   ScaleDev rs, ScaleDev gs, int M_ln, void* sum, int64_t ldsum, int8_t* out, int64_t ldout, int32_t* row_max,
-                   int64_t rows, int64_t C) {
-  if (rows == 0) return IVIT_OK;
-  auto vec = [](const ScaleDev& s) { return s.mult_c && aligned16(s.mult_c) && aligned4(s.shift_c) ? 1 : 0; };
-  const RmsArgs a{x, ldx, xs, res, ldres, rs, gs, M_ln, sum, ldsum, out, ldout, row_max, rows, (int)C, vec(xs), vec(gs)};
-  const int xb = x_dtype == IVIT_I8 ? 1 : 4, hb = res_dtype == IVIT_I8 ? 1 : 4;
-  LaunchScope ls(ctx, KIND_LAYERNORM, (double)rows * C * (xb + 1 + (res ? hb : 0) + (sum ? hb : 0)));
+int launch_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params& p) {
+  auto vec = [](const ivit_scale& s) { return s.mult_c && aligned16(s.mult_c) && aligned4(s.shift_c) ? 1 : 0; };
+  const RmsArgs a{p.x, p.ldx, to_dev(p.x_scale), p.res, p.ldres, to_dev(p.res_scale), to_dev(p.gamma_scale), p.M_ln, p.sum, p.ldsum,
+                  p.out, p.ldout, p.row_max, p.rows, (int)p.C, vec(p.x_scale), vec(p.gamma_scale)};
+  const int xb = p.x_dtype == IVIT_I8 ? 1 : 4, hb = p.res_dtype == IVIT_I8 ? 1 : 4;
+  LaunchScope ls(ctx, KIND_LAYERNORM, (double)p.rows * p.C * (xb + 1 + (p.res ? hb : 0) + (p.sum ? hb : 0)));
   auto go = [&](auto xi, auto hi) {
-    if (row_max) launch_rows<decltype(xi)::value, decltype(hi)::value, true>(ctx, a);
+    if (p.row_max) launch_rows<decltype(xi)::value, decltype(hi)::value, true>(ctx, a);
     else launch_rows<decltype(xi)::value, decltype(hi)::value, false>(ctx, a);
   };
   using std::integral_constant;
   const integral_constant<int, -1> none;
   const integral_constant<int, 0> i8;
   const integral_constant<int, 1> i32;
-  if (!res) x_dtype == IVIT_I8 ? go(i8, none) : go(i32, none);
-  else if (x_dtype == IVIT_I8) res_dtype == IVIT_I8 ? go(i8, i8) : go(i8, i32);
-  else res_dtype == IVIT_I8 ? go(i32, i8) : go(i32, i32);
+  if (!p.res) p.x_dtype == IVIT_I8 ? go(i8, none) : go(i32, none);
+  else if (p.x_dtype == IVIT_I8) p.res_dtype == IVIT_I8 ? go(i8, i8) : go(i8, i32);
+  else p.res_dtype == IVIT_I8 ? go(i32, i8) : go(i32, i32);
   return ls.done();
 }
 

@@ -138,7 +138,8 @@ def layout(tmp_path_factory):
                    '  Kv4Seq s = kv4_sequence(q0, q1, len, tok, mq, ml); o[0] = s.q0; o[1] = s.n; o[2] = s.nq; o[3] = s.len; o[4] = s.bad; }\n'
                    'int seen(int q0, int q1, int len, int64_t tok, int64_t mq, int64_t ml, int t) { return kv4_seen(kv4_sequence(q0, q1, len, tok, mq, ml), t); }\n'
                    'void places(int d, int page, int o, int64_t* v) { v[0] = kv4_kcode(d, page, o); v[1] = kv4_kstep(d, page, o); v[2] = kv4_vcode(d, page, o);\n'
-                   '  v[3] = kv4_vstep(d, page, o); v[4] = kv4_block_bytes(d, page); }\n}\n')
+                   '  v[3] = kv4_vstep(d, page, o); v[4] = kv4_block_bytes(d, page); }\n'
+                   'int quotient(int64_t w, uint64_t den) { return small_quotient(w, den, recip_of(den)); }\n}\n')
     so = src.with_suffix(".so")
     subprocess.run(["g++", "-O2", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2207_01405_b200", "csrc"), "-o", str(so), str(src)], check=True)
     L = C.CDLL(str(so))
@@ -146,6 +147,7 @@ def layout(tmp_path_factory):
     L.plan.argtypes = [C.c_int, C.c_int, i64, i64, i64, i64, i64, C.c_int, C.POINTER(C.c_int)]
     L.seq.argtypes = [C.c_int, C.c_int, C.c_int, i64, i64, i64, C.POINTER(i64)]
     L.seen.argtypes = [C.c_int, C.c_int, C.c_int, i64, i64, i64, C.c_int]
+    L.quotient.argtypes = [i64, C.c_uint64]
     L.places.argtypes = [C.c_int, C.c_int, C.c_int, C.POINTER(i64)]
     return L
 
@@ -176,6 +178,19 @@ def test_every_launch_fits(layout):
                     assert len({(2 * t * sum_ld + n) % 32 for t in range(4) for n in range(8)}) == 32
                     # sums of a CTA stay below 2^31: a byte of codes times a byte of a weight
                     assert 255 * 255 * 32 * blocks < 2 ** 31
+
+
+def test_quotients(layout):
+    """floor(w / den) at and around every multiple that matters, over the whole range of denominators."""
+    rng = np.random.default_rng(7)
+    assert layout.quotient(0, 0) == 0
+    for n in range(60000):
+        b = int(rng.integers(1, 43))
+        den = max(1, [int(rng.integers(1 << (b - 1), 1 << b)), (1 << b) - 1, (1 << b) - 2, 1 << (b - 1), (1 << (b - 1)) + 1][n % 5])
+        q = int(rng.integers(0, 1 << int(rng.integers(1, 25))))
+        for w in (q * den, q * den + den - 1, q * den + int(rng.integers(0, den))):
+            if w < 1 << 62 and w <= den << 24:
+                assert layout.quotient(w, den) == w // den and layout.quotient(-w, den) == -w // den, (w, den)
 
 
 def test_what_a_sequence_may_touch(layout):
@@ -222,6 +237,30 @@ def lib():
     return binding
 
 
+def test_call_descriptions_have_the_header_s_layout(lib, tmp_path):
+    """Every field of the structures of ivit.h lies where the binding packs it."""
+    src = tmp_path / "t.c"
+    fields = {"rmsnorm": "x ldx res ldres sum ldsum out ldout row_max rows C x_scale res_scale gamma_scale x_dtype res_dtype M_ln",
+              "kv4_attention": "Q ldq O ldo q_start lens table ldtable weights ldw q_heads tokens seqs max_q max_len qk_scale pv_scale smax",
+              "kv4_evict": "weights ldw weights_out ldw_out lens new_lens table ldtable dst_table ld_dst kept seqs max_len keep sinks recent"}
+    body = "".join(f'  printf("%zu ", sizeof(ivit_{n}_params));\n' + "".join(f'  printf("%zu ", offsetof(ivit_{n}_params, {f}));\n' for f in fs.split()) +
+                   '  printf("\\n");\n' for n, fs in fields.items())
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "ivit.h"\nint main(void) {\n' + body + "  return 0;\n}\n")
+    exe = tmp_path / "t"
+    subprocess.run(["gcc", "-I", os.path.join(ROOT, "include"), "-o", str(exe), str(src)], check=True)
+    got = [[int(v) for v in line.split()] for line in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines()]
+    scale, eight = 24, 8
+    want = []
+    for n, fs in fields.items():
+        at, offs = 0, []
+        for f in fs.split():
+            offs.append(at)
+            at += scale if f.endswith("_scale") else 16 if f == "smax" else 4 if f in ("x_dtype", "res_dtype", "M_ln") else eight
+        want.append([-(-at // 8) * 8] + offs)
+    assert got == want
+    assert [lib._RMSNORM.size, lib._ATTENTION.size, lib._EVICT.size] == [w[0] for w in want]
+
+
 CTX = C.create_string_buffer(8192)          # never looked at: every call here is refused, or has nothing to do
 AT = 1 << 20                                # an aligned address that is never read
 
@@ -230,8 +269,11 @@ def rms(b, **k):
     v = dict(ctx=C.addressof(CTX), x=AT, xd=0, ldx=64, xs=b.CScale(None, None, 2 ** 30, 33), res=None, rd=0, ldr=0, rs=b.CScale(None, None, 2 ** 30, 31),
              gs=b.CScale(None, None, 2 ** 30, 35), M=20, sum=None, lds=0, out=AT, ldo=64, rm=None, rows=1, C=64)
     v.update(k)
-    return b.load_library().ivit_rmsnorm(v["ctx"], v["x"], v["xd"], v["ldx"], v["xs"], v["res"], v["rd"], v["ldr"], v["rs"], v["gs"], v["M"], v["sum"],
-                                         v["lds"], v["out"], v["ldo"], v["rm"], v["rows"], v["C"])
+    f = lambda s: (s.mult_c or 0, s.shift_c or 0, s.mult, s.shift)  # noqa: E731
+    z = lambda n: v[n] or 0  # noqa: E731
+    d = b._RMSNORM.pack(z("x"), v["ldx"], z("res"), v["ldr"], z("sum"), v["lds"], z("out"), v["ldo"], z("rm"), v["rows"], v["C"], *f(v["xs"]), *f(v["rs"]),
+                        *f(v["gs"]), v["xd"], v["rd"], v["M"])
+    return b.load_library().ivit_rmsnorm(v["ctx"], d)
 
 
 def test_rmsnorm_refusals(lib):
@@ -291,8 +333,11 @@ def attend(b, c=None, **k):
     v = dict(ctx=C.addressof(CTX), Q=AT, ldq=256, qh=4, tokens=3, qs=AT, lens=AT, table=AT, ldt=4, qk=one, p=b.CExp(17, 15, 45, 8), pv=one, O=2 * AT,
              ldo=256, w=None, ldw=0, seqs=2, mq=2, ml=100)
     v.update(k)
-    return b.load_library().ivit_kv4_attention(v["ctx"], C.byref(c or cache(b)), v["Q"], v["ldq"], v["qh"], v["tokens"], v["qs"], v["lens"], v["table"],
-                                               v["ldt"], v["qk"], v["p"], v["pv"], v["O"], v["ldo"], v["w"], v["ldw"], v["seqs"], v["mq"], v["ml"])
+    f = lambda s: (s.mult_c or 0, s.shift_c or 0, s.mult, s.shift)  # noqa: E731
+    z = lambda n: v[n] or 0  # noqa: E731
+    d = b._ATTENTION.pack(z("Q"), v["ldq"], z("O"), v["ldo"], z("qs"), z("lens"), z("table"), v["ldt"], z("w"), v["ldw"], v["qh"], v["tokens"], v["seqs"],
+                          v["mq"], v["ml"], *f(v["qk"]), *f(v["pv"]), v["p"].I0, v["p"].N, v["p"].M, v["p"].k_out)
+    return b.load_library().ivit_kv4_attention(v["ctx"], C.byref(c or cache(b)), d)
 
 
 def test_attention_refusals(lib):
@@ -319,8 +364,10 @@ def evict(b, c=None, **k):
     v = dict(ctx=C.addressof(CTX), w=AT, ldw=100, lens=AT, table=AT, ldt=4, dst=2 * AT, ldd=2, wo=2 * AT, ldwo=64, kept=AT, new=AT, seqs=1, ml=100,
              keep=50, sinks=4, recent=20)
     v.update(k)
-    return b.load_library().ivit_kv4_evict(v["ctx"], C.byref(c or cache(b)), v["w"], v["ldw"], v["lens"], v["table"], v["ldt"], v["dst"], v["ldd"],
-                                           v["wo"], v["ldwo"], v["kept"], v["new"], v["seqs"], v["ml"], v["keep"], v["sinks"], v["recent"])
+    z = lambda n: v[n] or 0  # noqa: E731
+    d = b._EVICT.pack(z("w"), v["ldw"], z("wo"), v["ldwo"], z("lens"), z("new"), z("table"), v["ldt"], z("dst"), v["ldd"], z("kept"), v["seqs"], v["ml"],
+                      v["keep"], v["sinks"], v["recent"])
+    return b.load_library().ivit_kv4_evict(v["ctx"], C.byref(c or cache(b)), d)
 
 
 def test_evict_refusals(lib):
