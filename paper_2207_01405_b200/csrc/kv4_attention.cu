@@ -20,7 +20,7 @@ struct AttendArgs {
   int pv_mult, pv_shift, I0, N, z;
   int8_t* O; int64_t ldo;
   int64_t* weights; int64_t ldw;
-  int max_q, max_len, split, blocks, kept, stages;
+  int max_q, max_len, split, blocks, kept, stages, sorted;   // sorted: the number of sequences, which go longest first (0: in their order)
   int* status;
 };
 
@@ -96,7 +96,7 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
 // ---------------------------------------------------------------- the kernel
 //
 // A cluster of `split` CTAs takes up to 8 RN query rows (of one sequence, all of them readers of one key/value head) and shares the
-// keys out in runs of blocks of 32; the eight warps of a CTA take its blocks in turn.  Two passes, because ShiftExp needs the row's
+// keys out in runs of blocks of 32; the warps of a CTA take its blocks in turn.  Two passes, because ShiftExp needs the row's
 // maximum before the first weight (its floors do not commute with a change of the maximum, so nothing can be corrected afterwards):
 //   scores:  S^T = K Q^T on m16n8k32 products, keys along M, the query rows along N (a decoder has 1 to 16 of them: none is padding of 16).
 //            One product of 32 channels is one group of a key, whose step multiplies it in 32 bits; the int8 scores stay in shared memory.
@@ -105,29 +105,31 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
 // maxima), and unpacks them in registers: three instructions for eight codes of K, and a transpose of bytes more for V, whose products
 // run along the keys.  Maxima, sums and outputs of the cluster's CTAs meet in distributed shared memory: one launch, no workspace, and
 // integer sums, so that the order changes nothing.
-template <int D, int RN, bool kWeights>
-__global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(const AttendArgs a) {
+template <int D, int RN, int W, bool kWeights>
+__global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attention_kernel(const AttendArgs a) {
   constexpr int kG = D / 32;               // groups of a key
   constexpr int kLaneWords = D / 32;       // words of a K row that a lane takes
   constexpr int kMu = D / 16;              // tiles of 16 channels
+  constexpr int T = 32 * W;                // threads
   constexpr int kRows = 8 * RN, kStage = kKv4Block * (D / 2 + D / 32);
   extern __shared__ __align__(128) uint8_t sm[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n8 = lane >> 2, t4 = lane & 3;
-  const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split, h = blockIdx.y, b = blockIdx.z;
-  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks, a.split, a.stages);
+  const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split, h = blockIdx.y;
+  int b = blockIdx.z;
+  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks, a.split, W, a.stages);
   const uint8_t** const pages = reinterpret_cast<const uint8_t**>(sm + at.pages);   // this head's block of each page of the run
   int* const small = reinterpret_cast<int*>(sm + at.small);
   int* const lim = small;                                                            // [16] keys that a row sees
   int* const top = small + 16;                                                       // [16] maxima of the rows
-  const uint32_t bar0 = smem_u32(small + 544), bar1 = bar0 + 8;                      // what peers send: maxima; sums
-  int* const warp_top = small + 32;                                                  // [8][16]
-  int* const cta_u = small + 160;                                                    // [2][16] sums of the weights' planes
-  unsigned long long* const row_den = reinterpret_cast<unsigned long long*>(small + 192);   // [16]
+  int* const warp_top = small + 32;                                                  // [16][16]
+  int* const cta_u = small + 288;                                                    // [2][16] sums of the weights' planes
+  unsigned long long* const row_den = reinterpret_cast<unsigned long long*>(small + 320);   // [16]
   unsigned long long* const row_u = row_den + 16;                                    // [16]
   unsigned long long* const row_recip = row_u + 16;                                  // [16]
-  unsigned long long* const warp_den = row_recip + 16;                               // [8][16]
-  unsigned long long* const row_out = reinterpret_cast<unsigned long long*>(small + 560);   // [16] where a row of O starts
-  static_assert(4 * 560 + 8 * 16 <= kKv4Small && 4 * 192 + 8 * (3 * 16 + kKv4Warps * 16) <= 4 * 544, "room for the rows' numbers");
+  unsigned long long* const row_out = row_recip + 16;                                // [16] where a row of O starts
+  unsigned long long* const warp_den = row_out + 16;                                 // [16][16]
+  const uint32_t bar0 = smem_u32(warp_den + 256), bar1 = bar0 + 8;                   // what peers send: maxima; sums
+  static_assert(4 * 320 + 8 * (4 * 16 + 256 + 2) <= kKv4Small, "room for the rows' numbers");
   int* const sums = reinterpret_cast<int*>(sm + at.sums);                            // [plane][row][channel]
   // what the CTAs of the cluster send: [rank][row] maxima, [denominator, weights][rank][row], [rank][this CTA's share of the sums]
   int* const top_in = reinterpret_cast<int*>(sm + at.peers);
@@ -137,20 +139,17 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   int8_t* const score = reinterpret_cast<int8_t*>(sm + at.score);
   constexpr int kLd = D + 4;
   // what needs nothing that a kernel in front may still be writing
-  for (int i = tid; i < 2 * kRows * kLd / 4; i += 256) reinterpret_cast<int4*>(sums)[i] = make_int4(0, 0, 0, 0);
+  for (int i = tid; i < 2 * kRows * kLd / 4; i += T) reinterpret_cast<int4*>(sums)[i] = make_int4(0, 0, 0, 0);
   if (tid < 32) cta_u[tid] = 0;
-  const int own = kRows * D / a.split;     // sums that this CTA finishes, in the order [row][channel]
   if (a.split > 1) {
     if (tid == 0) {
       mbar_init(bar0, 1);
       mbar_init(bar1, 1);
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-      expect_bytes(bar0, 4 * a.split * kRows);
-      expect_bytes(bar1, 16 * a.split * kRows + 8 * kRows * D);
     }
     cluster_arrive();
   }
-  {  // the exponentials, shifted so that a weight's 16 bits are the upper half of its product with a step
+  if (tid < 256) {  // the exponentials, shifted so that a weight's 16 bits are the upper half of its product with a step
     const unsigned e = shiftexp(-tid, a.I0, a.N) << (16 - a.z);
     uint4* dst = reinterpret_cast<uint4*>(sm + at.table) + tid * (kKv4Copies / 4);
     static_assert(kKv4Copies % 4 == 0, "whole vectors");
@@ -166,6 +165,21 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   pdl_wait();
   pdl_trigger();
+  if (a.sorted) {
+    // The z-th longest sequence (of equal ones the one in front): a long one that starts behind the others would end long after them.
+    int* const order = reinterpret_cast<int*>(score);
+    if (tid < a.sorted) order[tid] = a.lens[tid];
+    __syncthreads();
+    if (tid < a.sorted) {
+      const int mine = order[tid];
+      int before = 0;
+      for (int i = 0; i < a.sorted; ++i) before += order[i] > mine || (order[i] == mine && i < tid);
+      if (before == b) top[0] = tid;
+    }
+    __syncthreads();
+    b = top[0];
+    __syncthreads();
+  }
   // (not split: the first pages are known without the lengths, and fetched beside them)
   const int early = a.split == 1 && (tid << a.page_log) < a.max_len ? a.table[b * a.ldtable + tid] : 0;
   const Kv4Seq seq = kv4_sequence(a.q_start[b], a.q_start[b + 1], a.lens[b], a.tokens, a.max_q, a.max_len);
@@ -177,12 +191,26 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   // keys that some row of the tile sees, and this CTA's run of them
   const int seen_all = kv4_seen(seq, a.group.div(row0 + nrows - 1)), seen_min = kv4_seen(seq, a.group.div(row0));
-  const int blks = (seen_all + kKv4Block - 1) / kKv4Block, run = (blks + a.split - 1) / a.split;
+  const int blks = (seen_all + kKv4Block - 1) / kKv4Block;
+  // A sequence takes as many of the cluster's CTAs (1, 2, 4, ...) as leave each no more than the launch was sized for: short ones among long
+  // ones pay for no exchange, and their CTAs make room.
+  int split = 1;
+  while (split < a.split && split * a.blocks < blks) split *= 2;
+  if (rank >= split) {
+    cluster_wait();
+    return;
+  }
+  const int run = (blks + split - 1) / split;
+  const int own = kRows * D / split;       // sums that this CTA finishes, in the order [row][channel]
+  if (split > 1 && tid == 0) {
+    expect_bytes(bar0, 4 * split * kRows);
+    expect_bytes(bar1, 16 * split * kRows + 8 * kRows * D);
+  }
   const int blk0 = rank * run, nblk = max(0, min(run, blks - blk0));
   const int page0 = blk0 * kKv4Block >> a.page_log;
   bool bad = false;
-  for (int i = tid; i < (nblk > 0 ? ((blk0 + nblk) * kKv4Block - 1 >> a.page_log) - page0 + 1 : 0); i += 256) {
-    const int pg = a.split == 1 && i < 256 ? early : a.table[b * a.ldtable + page0 + i];
+  for (int i = tid; i < (nblk > 0 ? ((blk0 + nblk) * kKv4Block - 1 >> a.page_log) - page0 + 1 : 0); i += T) {
+    const int pg = a.split == 1 && i < T ? early : a.table[b * a.ldtable + page0 + i];
     const bool there = pg >= 0 && pg < a.pages;
     if (!there) {
       bad = true;
@@ -241,15 +269,15 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   for (int c = 0; c < D / 32; ++c) v_at[c] = place(lane, c);
 
   // ---- scores
-  for (int s = 0; s < a.stages - 1; ++s) request_k(warp + 8 * s, page_of(warp + 8 * s), s * kStage);
+  for (int s = 0; s < a.stages - 1; ++s) request_k(warp + W * s, page_of(warp + W * s), s * kStage);
   int best[RN][2];
 #pragma unroll
   for (int j = 0; j < RN; ++j) best[j][0] = best[j][1] = -128;
-  const int ahead = 8 * (a.stages - 1);
+  const int ahead = W * (a.stages - 1);
   const uint32_t last = (a.stages - 1) * kStage;
   uint32_t stage = 0, behind = last;                        // the block at hand; where the one requested now goes
   const uint8_t* next = page_of(warp + ahead);             // (looked up a turn before it is needed)
-  for (int lb = warp; lb < nblk; lb += 8) {
+  for (int lb = warp; lb < nblk; lb += W) {
     cp_wait_stages(a.stages);
     __syncwarp();
     const uint8_t* buf = ring + stage;
@@ -269,7 +297,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       for (int g = 0; g < kG; ++g) step[i][g] = buf[kKv4Block * (D / 2) + (4 * n8 + i) * kG + g];
     }
     request_k(lb + ahead, next, behind);
-    next = page_of(lb + ahead + 8);
+    next = page_of(lb + ahead + W);
     behind = stage;
     stage = stage == last ? 0 : stage + kStage;
     const int key0 = (blk0 + lb) * kKv4Block;
@@ -318,7 +346,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   cp_wait<0>();
   __syncwarp();
-  for (int s = 0; s < a.stages - 1; ++s) request_v(warp + 8 * s, page_of(warp + 8 * s), s * kStage);
+  for (int s = 0; s < a.stages - 1; ++s) request_v(warp + W * s, page_of(warp + W * s), s * kStage);
   next = page_of(warp + ahead);
 #pragma unroll
   for (int j = 0; j < RN; ++j)
@@ -334,17 +362,17 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   const int pr = tid >> 4, pk = tid & 15;
   if (a.split > 1) cluster_wait();         // (the peers' barriers are set up)
   if (pr < kRows) {
-    int v = pk < kKv4Warps ? warp_top[pk * 16 + pr] : -128;
+    int v = pk < W ? warp_top[pk * 16 + pr] : -128;
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
-    if (a.split == 1) {
+    if (split == 1) {
       if (pk == 0) top[pr] = v;
-    } else if (pk < a.split) {
+    } else if (pk < split) {
       send_i32(peer_addr(smem_u32(top_in + rank * kRows + pr), pk), v, peer_addr(bar0, pk));
     }
-    if (a.split > 1) {
+    if (split > 1) {
       mbar_wait(bar0, 0, a.status);
-      v = pk < a.split ? top_in[pk * kRows + pr] : -128;
+      v = pk < split ? top_in[pk * kRows + pr] : -128;
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
       if (pk == 0) top[pr] = v;
@@ -372,7 +400,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   constexpr uint32_t kSel = (uint32_t)(-4 * kKv4Copies) & 255u;
   stage = 0, behind = last;
-  for (int lb = warp; lb < nblk; lb += 8) {
+  for (int lb = warp; lb < nblk; lb += W) {
     cp_wait_stages(a.stages);
     __syncwarp();
     const uint8_t* buf = ring + stage;
@@ -387,7 +415,7 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) load_transposed(smem_u32(buf) + v_at[c], y[c][0], y[c][1], y[c][2], y[c][3]);
     request_v(lb + ahead, next, behind);
-    next = page_of(lb + ahead + 8);
+    next = page_of(lb + ahead + W);
     behind = stage;
     stage = stage == last ? 0 : stage + kStage;
     const int key0 = (blk0 + lb) * kKv4Block;
@@ -467,32 +495,32 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   }
   __syncthreads();
   // ---- the rows' sums and the cluster's
-  constexpr int kTurns = kRows * D / 256;
+  constexpr int kTurns = kRows * D / T;
   long long part[kTurns];
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
-    const int item = tid + 256 * i;
+    const int item = tid + T * i;
     const int* src = sums + item / D * kLd + item % D;
     part[i] = src[0] + 256ll * src[kRows * kLd];
     if (item % D < D / 2) part[i] -= src[D / 2] + 256ll * src[kRows * kLd + D / 2];
-    if (a.split > 1) {
+    if (split > 1) {
       const int to = item / own;
       send_u64(peer_addr(smem_u32(part_in + rank * own + (item - to * own)), to), (unsigned long long)part[i], peer_addr(bar1, to));
     }
   }
   if (pr < kRows) {
-    unsigned long long row_d = pk < kKv4Warps ? warp_den[pk * 16 + pr] : 0;   // denominator and sum of the weights, of this CTA
+    unsigned long long row_d = pk < W ? warp_den[pk * 16 + pr] : 0;   // denominator and sum of the weights, of this CTA
     unsigned long long row_s = (unsigned)cta_u[pr] + 256ull * (unsigned)cta_u[16 + pr];
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) row_d += __shfl_xor_sync(~0u, row_d, o);
-    if (a.split > 1) {
-      if (pk < a.split) {
+    if (split > 1) {
+      if (pk < split) {
         send_u64(peer_addr(smem_u32(row_in + rank * kRows + pr), pk), row_d, peer_addr(bar1, pk));
         send_u64(peer_addr(smem_u32(row_in + (16 + rank) * kRows + pr), pk), row_s, peer_addr(bar1, pk));
       }
       mbar_wait(bar1, 0, a.status);
-      row_d = pk < a.split ? row_in[pk * kRows + pr] : 0;
-      row_s = pk < a.split ? row_in[(16 + pk) * kRows + pr] : 0;
+      row_d = pk < split ? row_in[pk * kRows + pr] : 0;
+      row_s = pk < split ? row_in[(16 + pk) * kRows + pr] : 0;
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) {
         row_d += __shfl_xor_sync(~0u, row_d, o);
@@ -506,15 +534,15 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
       row_recip[pr] = recip_of(row_d);
     }
   }
-  if (a.split > 1) {
+  if (split > 1) {
     mbar_wait(bar1, 0, a.status);
     cluster_arrive();                      // (waited for at the end: no CTA leaves while a peer may still send to it, not even when a wait gave up)
 #pragma unroll
     for (int i = 0; i < kTurns; ++i)
-      if (tid + 256 * i < own) {
+      if (tid + T * i < own) {
         long long v[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = k < a.split ? part_in[k * own + tid + 256 * i] : 0;
+        for (int k = 0; k < 16; ++k) v[k] = k < split ? part_in[k * own + tid + T * i] : 0;
         part[i] = 0;
 #pragma unroll
         for (int k = 0; k < 16; ++k) part[i] += v[k];
@@ -525,26 +553,26 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
   // ---- outputs
 #pragma unroll
   for (int i = 0; i < kTurns; ++i) {
-    const int item = min(rank * own + tid + 256 * i, kRows * D - 1), row = item / D;
+    const int item = min(rank * own + tid + T * i, kRows * D - 1), row = item / D;
     const int ch = item % D;
     const unsigned long long den_row = row_den[row];
     // (codes came in as code + 8, the upper half's sixteenfold; a row that sees nothing: every number is zero)
     const long long num = (part[i] >> (ch < D / 2 ? 0 : 4)) - 8 * (long long)row_u[row];
     const int t = small_quotient(num * (1ll << (a.z + 5)), den_row, row_recip[row]);
-    if (tid + 256 * i < own && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
+    if (tid + T * i < own && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
   }
 
   // ---- accumulated weights: floor(e 2^24 / den) of every difference of scores, row by row, then the sum over the rows of each key
   if (kWeights) {
     unsigned* share = reinterpret_cast<unsigned*>(sm + at.ring);
-    for (int i = tid; i < nrows * 256; i += 256) {
+    for (int i = tid; i < nrows * 256; i += T) {
       const unsigned long long den_row = row_den[i >> 8];
       const unsigned e = *reinterpret_cast<const unsigned*>(sm + at.table + (i & 255) * (4 * kKv4Copies)) >> (16 - a.z);
       share[i] = den_row ? (unsigned)small_quotient((long long)e << 24, den_row, row_recip[i >> 8]) : 0;
     }
     __syncthreads();
     unsigned long long* w = reinterpret_cast<unsigned long long*>(a.weights) + ((int64_t)b * a.heads + h) * a.ldw;
-    for (int i = tid; i < nblk * 8; i += 256) {
+    for (int i = tid; i < nblk * 8; i += T) {
       const int key0 = (blk0 + (i >> 3)) * kKv4Block, n = i & 7;
       if (holes && !page_of(i >> 3)) continue;
       unsigned long long v[4] = {0, 0, 0, 0};
@@ -560,22 +588,31 @@ __global__ void __launch_bounds__(256, RN == 1 ? 2 : 1) kv4_attention_kernel(con
         if (v[k]) atomicAdd(w + key0 + 4 * n + k, v[k]);
     }
   }
-  if (a.split > 1) cluster_wait();
+  if (split > 1) cluster_wait();
 }
 
+// f(kernel, head dimension, query rows, warps, weights) for each of the kernels.
 template <class F>
 static int each_kernel(F f) {
-  int rc;
-  if ((rc = f(kv4_attention_kernel<64, 1, false>, 64, 1, false)) || (rc = f(kv4_attention_kernel<64, 2, false>, 64, 2, false)) ||
-      (rc = f(kv4_attention_kernel<64, 1, true>, 64, 1, true)) || (rc = f(kv4_attention_kernel<64, 2, true>, 64, 2, true)) ||
-      (rc = f(kv4_attention_kernel<128, 1, false>, 128, 1, false)) || (rc = f(kv4_attention_kernel<128, 2, false>, 128, 2, false)) ||
-      (rc = f(kv4_attention_kernel<128, 1, true>, 128, 1, true)) || (rc = f(kv4_attention_kernel<128, 2, true>, 128, 2, true)))
-    return rc;
-  return IVIT_OK;
+  int rc = IVIT_OK;
+  auto both = [&](auto d, auto rn, auto w) {
+    constexpr int D = decltype(d)::value, RN = decltype(rn)::value, W = decltype(w)::value;
+    if (rc == IVIT_OK) rc = f(kv4_attention_kernel<D, RN, W, false>, D, 8 * RN, W, false);
+    if (rc == IVIT_OK) rc = f(kv4_attention_kernel<D, RN, W, true>, D, 8 * RN, W, true);
+  };
+  const std::integral_constant<int, 1> one;
+  const std::integral_constant<int, 2> two;
+  const std::integral_constant<int, 8> w8;
+  const std::integral_constant<int, 16> w16;
+  const std::integral_constant<int, 64> d64;
+  const std::integral_constant<int, 128> d128;
+  both(d64, one, w8); both(d64, one, w16); both(d64, two, w8);
+  both(d128, one, w8); both(d128, one, w16); both(d128, two, w8);
+  return rc;
 }
 
 int kv4_prepare_device() {
-  return each_kernel([](auto k, int, int, bool) {
+  return each_kernel([](auto k, int, int, int, bool) {
     if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kKv4SmemMax) != cudaSuccess ||
         cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
       return (int)IVIT_ERR_CUDA;
@@ -606,11 +643,14 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_
   while (top >> (a.z + 8)) ++a.z;
   a.O = c.O; a.ldo = c.ldo; a.weights = c.weights; a.ldw = c.ldw;
   a.max_q = (int)c.max_q; a.max_len = (int)c.max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept; a.stages = p.stages;
+  // (few waves of long CTAs: worth the 0.2 us that finding one's sequence takes; the numbers wait where the scores will be)
+  const int64_t ctas = cache.heads * c.seqs;
+  a.sorted = p.warps == 16 && p.split == 1 && p.tiles == 1 && ctas > ctx->sm_count && c.seqs <= 128 ? (int)c.seqs : 0;
   a.status = ctx->status_dev;
   LaunchScope ls(ctx, KIND_ATTENTION, 4.0 * c.seqs * c.q_heads * c.max_q * c.max_len * d);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(p.tiles * p.split), (unsigned)cache.heads, (unsigned)c.seqs);
-  cfg.blockDim = 256;
+  cfg.blockDim = 32 * p.warps;
   cfg.dynamicSmemBytes = (size_t)p.smem;
   cfg.stream = ctx->stream;
   cudaLaunchAttribute attr[2];
@@ -621,8 +661,8 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_
   attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = p.split > 1 ? 2 : 1;
-  each_kernel([&](auto k, int kd, int rn, bool w) {
-    if (kd == d && rn * 8 == p.rows && w == (c.weights != nullptr)) cudaLaunchKernelEx(&cfg, k, a);
+  each_kernel([&](auto k, int kd, int rows, int warps, bool w) {
+    if (kd == d && rows == p.rows && warps == p.warps && w == (c.weights != nullptr)) cudaLaunchKernelEx(&cfg, k, a);
     return (int)IVIT_OK;
   });
   return ls.done();

@@ -103,11 +103,10 @@ inline Kv4Div kv4_div(unsigned d) {
 // ---- launch of the attention ----
 
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time
-constexpr int kKv4Warps = 8;
 constexpr int kKv4Copies = 8;      // copies of the exponentials
 constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: a byte of codes times a byte of a weight, over 32768 keys, stays below 2^31
-constexpr int kKv4Split = 32;      // blocks of a CTA below which it is not halved once more: the exchange costs what four of a warp's blocks do
-constexpr int kKv4Small = 2560;    // bytes of the rows' numbers
+constexpr int kKv4Split = 48;      // blocks of a CTA below which it is not halved once more: an exchange costs what three of a warp's blocks do
+constexpr int kKv4Small = 3968;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
 constexpr int kKv4SmemHalf = 113 * 1024;   // two CTAs on an SM
 
@@ -121,8 +120,8 @@ struct Kv4Smem {
   int table, small, sums, peers, pages, ring, score, total;
 };
 // rows: query rows of a CTA (8 or 16); kept: those of them that some sequence can have, whose scores are kept; blocks: blocks of keys of a CTA;
-// split: CTAs of a cluster; stages: blocks that a warp holds, one it works on and the others on their way.
-IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, int split, int stages) {
+// split: CTAs of a cluster; warps: of a CTA; stages: blocks that a warp holds, one it works on and the others on their way.
+IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, int split, int warps, int stages) {
   Kv4Smem m;
   m.table = 0;
   m.small = m.table + 256 * kKv4Copies * 4;
@@ -131,15 +130,15 @@ IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, in
   m.pages = m.peers + (split > 1 ? 16 * rows * (4 + 2 * 8) + rows * d * 8 : 0);   // (see the kernel)
   m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 8 + 127) / 128 * 128;
   // behind the passes the ring holds the shares of the weights
-  const int ring = kKv4Warps * stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
+  const int ring = warps * stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
   m.score = m.ring + (ring > shares ? ring : shares);
   m.total = m.score + kept * kv4_score_ld(blocks);
   return m;
 }
 
 struct Kv4Plan {
-  // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, blocks a warp holds, row tiles, bytes
-  int rows, kept, split, blocks, stages, tiles, smem;
+  // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, warps, blocks a warp holds, row tiles, bytes
+  int rows, kept, split, blocks, warps, stages, tiles, smem;
 };
 inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms) {
   Kv4Plan p;
@@ -148,20 +147,27 @@ inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t s
     p.tiles = (int)((q_rows + p.rows - 1) / p.rows);
     p.kept = (int)(q_rows < p.rows ? q_rows : p.rows);
     const int64_t ctas = (int64_t)p.tiles * heads * seqs;
-    // three blocks under way for each warp where there is room, else two; bytes within the limit for the rows' form
+    // Three blocks under way for each warp where there is room, else two.  A CTA of 8 warps shares its SM with another (eight query rows),
+    // one of 16 has it alone.  Clusters of 16 CTAs with an SM each find room seven times on the GPU.
     auto fits = [&]() {
       p.blocks = (int)((all + p.split - 1) / p.split);
       if (p.blocks < 1) p.blocks = 1;
-      const int limit = p.rows == 8 && (ctas * p.split > sms || p.split == 16) ? kKv4SmemHalf : kKv4SmemMax;
-      for (p.stages = 4; p.stages >= 3; --p.stages) {
-        p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.stages).total;
-        if (p.smem <= limit) return p.blocks <= kKv4Blocks;
+      const int64_t n = ctas * p.split;
+      // 16 warps: few CTAs, or few waves of them (sequences of uneven lengths, whose longest ends last); not many, which overlap one another
+      const bool wide = p.rows == 8 && p.blocks >= 16 && n < 4 * sms && (p.split == 1 || (p.split == 16 ? n <= 112 : n <= sms));
+      for (p.warps = wide ? 16 : 8; p.warps >= 8; p.warps -= 8) {
+        const int limit = p.rows == 8 && p.warps == 8 && (n > sms || p.split == 16) ? kKv4SmemHalf : kKv4SmemMax;
+        for (p.stages = 4; p.stages >= 3; --p.stages) {
+          p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps, p.stages).total;
+          if (p.smem <= limit) return p.blocks <= kKv4Blocks;
+        }
       }
+      p.warps = 8;
       p.stages = 3;
       return false;
     };
     p.split = 1;
-    while (p.split < 16 && ctas * p.split < sms && all > (int64_t)p.split * kKv4Split) p.split *= 2;
+    while (p.split < 16 && 2 * ctas * p.split <= sms && all > (int64_t)p.split * kKv4Split) p.split *= 2;
     while (!fits() && p.split < 16) p.split *= 2;
     if ((p.smem <= kKv4SmemMax && p.blocks <= kKv4Blocks) || p.rows == 8) return p;
   }

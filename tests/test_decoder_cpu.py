@@ -131,9 +131,9 @@ def layout(tmp_path_factory):
     src = tmp_path_factory.mktemp("layout") / "t.cpp"
     src.write_text('#include "kv4_layout.cuh"\nusing namespace ivit;\nextern "C" {\n'
                    'void plan(int d, int page, int64_t g, int64_t h, int64_t s, int64_t q, int64_t l, int sms, int* o) {\n'
-                   '  Kv4Plan p = kv4_plan(d, page, g, h, s, q, l, sms); Kv4Smem m = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.stages);\n'
-                   '  int v[] = {p.rows, p.split, p.blocks, p.tiles, p.smem, m.table, m.small, m.sums, m.peers, m.pages, m.ring, m.score, kv4_score_ld(p.blocks), kv4_sum_ld(d), p.kept, p.stages};\n'
-                   '  for (int i = 0; i < 16; ++i) o[i] = v[i]; }\n'
+                   '  Kv4Plan p = kv4_plan(d, page, g, h, s, q, l, sms); Kv4Smem m = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps, p.stages);\n'
+                   '  int v[] = {p.rows, p.split, p.blocks, p.tiles, p.smem, m.table, m.small, m.sums, m.peers, m.pages, m.ring, m.score, kv4_score_ld(p.blocks), kv4_sum_ld(d), p.kept, p.stages, p.warps};\n'
+                   '  for (int i = 0; i < 17; ++i) o[i] = v[i]; }\n'
                    'void seq(int q0, int q1, int len, int64_t tok, int64_t mq, int64_t ml, int64_t* o) {\n'
                    '  Kv4Seq s = kv4_sequence(q0, q1, len, tok, mq, ml); o[0] = s.q0; o[1] = s.n; o[2] = s.nq; o[3] = s.len; o[4] = s.bad; }\n'
                    'int seen(int q0, int q1, int len, int64_t tok, int64_t mq, int64_t ml, int t) { return kv4_seen(kv4_sequence(q0, q1, len, tok, mq, ml), t); }\n'
@@ -155,7 +155,7 @@ def layout(tmp_path_factory):
 def test_every_launch_fits(layout):
     """The plan of a launch covers every key and query row, and the parts of shared memory follow one another inside the limit."""
     rng = np.random.default_rng(6)
-    o = (C.c_int * 16)()
+    o = (C.c_int * 17)()
     lens = [0, 1, 31, 32, 33, 256, 257, 1000, 4096, 12288, 12289, 24577, 65536, 100003, 131073, 196607, 196608]
     for d in (64, 128):
         for page in (32, 256):
@@ -163,12 +163,12 @@ def test_every_launch_fits(layout):
                 for g, h, s, q in ((1, 1, 1, 1), (4, 8, 1, 1), (8, 8, 64, 1), (9, 2, 3, 1), (16, 1, 1, 1), (17, 1, 1, 1), (4, 8, 5, 300), (1, 65535, 65535, 1),
                                    (7, 3, 2, 1 << 24)):
                     layout.plan(d, page, g, h, s, q, L, 148, o)
-                    rows, split, blocks, tiles, smem, table, small, sums, peers, pages, ring, score, ld, sum_ld, kept, stages = list(o)
+                    rows, split, blocks, tiles, smem, table, small, sums, peers, pages, ring, score, ld, sum_ld, kept, stages, warps = list(o)
                     assert rows in (8, 16) and split in (1, 2, 4, 8, 16) and smem <= 227 * 1024
                     assert tiles * rows >= q * g > (tiles - 1) * rows
                     assert split * blocks * 32 >= L and blocks >= 1
-                    assert small - table >= 256 * 8 * 4 and sums - small >= 4 * 560 + 8 * 16 and peers - sums >= 2 * rows * sum_ld * 4 and pages >= peers and ring - pages >= 8 * (blocks * 32 // page + 2)
-                    assert stages in (3, 4) and score - ring >= max(8 * stages * 32 * (d // 2 + d // 32), rows * 1024) and sum_ld >= d
+                    assert small - table >= 256 * 8 * 4 and sums - small >= 4 * 320 + 8 * 322 and peers - sums >= 2 * rows * sum_ld * 4 and pages >= peers and ring - pages >= 8 * (blocks * 32 // page + 2)
+                    assert stages in (3, 4) and (warps == 8 or (warps == 16 and rows == 8)) and score - ring >= max(warps * stages * 32 * (d // 2 + d // 32), rows * 1024) and sum_ld >= d
                     assert split == 1 or (pages - peers >= 16 * rows * 20 + 8 * rows * d and peers % 8 == 0 and rows * d % split == 0)
                     assert ld >= blocks * 32 and ld % 128 == 16 and smem >= score + kept * ld and 1 <= kept == min(rows, q * g)
                     assert ring % 128 == 0 and score % 16 == 0 and pages % 16 == 0 and small % 16 == 0
