@@ -463,7 +463,7 @@ int ivit_ctx_create(ivit_ctx** out, int device, void* cuda_stream) {
     fn = nullptr;
   c->tmap_encode = fn;
   if (gemm_tc_prepare_device() != IVIT_OK || gemm_small_prepare_device() != IVIT_OK || attention_prepare_device() != IVIT_OK ||
-      kv4_prepare_device() != IVIT_OK) {
+      kv4_prepare_device(c) != IVIT_OK) {
     cudaGetLastError();
     cudaFree(c->gelu_tables);
     cudaFreeHost(c->status_host);

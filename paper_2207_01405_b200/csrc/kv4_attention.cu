@@ -192,19 +192,19 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   // keys that some row of the tile sees, and this CTA's run of them
   const int seen_all = kv4_seen(seq, a.group.div(row0 + nrows - 1)), seen_min = kv4_seen(seq, a.group.div(row0));
   const int blks = (seen_all + kKv4Block - 1) / kKv4Block;
-  // A sequence takes as many of the cluster's CTAs (1, 2, 4, ...) as leave each no more than the launch was sized for: short ones among long
-  // ones pay for no exchange, and their CTAs make room.
-  int split = 1;
-  while (split < a.split && split * a.blocks < blks) split *= 2;
+  // A sequence takes as many of the cluster's CTAs as leave each no more than the launch was sized for: short ones among long ones pay for
+  // no exchange, and their CTAs make room.
+  const int split = max(1, min(a.split, (blks + a.blocks - 1) / a.blocks));
   if (rank >= split) {
     cluster_wait();
     return;
   }
   const int run = (blks + split - 1) / split;
-  const int own = kRows * D / split;       // sums that this CTA finishes, in the order [row][channel]
+  // sums that a CTA finishes, in the order [row][channel], and those that are left for this one
+  const int own = (kRows * D + split - 1) / split, mine_n = max(0, min(own, kRows * D - rank * own));
   if (split > 1 && tid == 0) {
     expect_bytes(bar0, 4 * split * kRows);
-    expect_bytes(bar1, 16 * split * kRows + 8 * kRows * D);
+    expect_bytes(bar1, 16 * split * kRows + 8 * split * mine_n);
   }
   const int blk0 = rank * run, nblk = max(0, min(run, blks - blk0));
   const int page0 = blk0 * kKv4Block >> a.page_log;
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
     cluster_arrive();                      // (waited for at the end: no CTA leaves while a peer may still send to it, not even when a wait gave up)
 #pragma unroll
     for (int i = 0; i < kTurns; ++i)
-      if (tid + T * i < own) {
+      if (tid + T * i < mine_n) {
         long long v[16];
 #pragma unroll
         for (int k = 0; k < 16; ++k) v[k] = k < split ? part_in[k * own + tid + T * i] : 0;
@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
     // (codes came in as code + 8, the upper half's sixteenfold; a row that sees nothing: every number is zero)
     const long long num = (part[i] >> (ch < D / 2 ? 0 : 4)) - 8 * (long long)row_u[row];
     const int t = small_quotient(num * (1ll << (a.z + 5)), den_row, row_recip[row]);
-    if (tid + T * i < own && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
+    if (tid + T * i < mine_n && row < nrows) a.O[row_out[row] + ch] = (int8_t)sat8(rq(t, a.pv_mult, a.pv_shift));
   }
 
   // ---- accumulated weights: floor(e 2^24 / den) of every difference of scores, row by row, then the sum over the rows of each key
@@ -611,19 +611,38 @@ static int each_kernel(F f) {
   return rc;
 }
 
-int kv4_prepare_device() {
-  return each_kernel([](auto k, int, int, int, bool) {
+int kv4_prepare_device(ivit_ctx* ctx) {
+  const int rc = each_kernel([](auto k, int, int, int, bool) {
     if (cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kKv4SmemMax) != cudaSuccess ||
         cudaFuncSetAttribute(k, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess)
       return (int)IVIT_ERR_CUDA;
     return (int)IVIT_OK;
   });
+  if (rc) return rc;
+  // how many clusters of each size run at once, an SM for each CTA
+  for (int c = 1; c <= 16; ++c) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = (unsigned)(c * ctx->sm_count);
+    cfg.blockDim = 512;
+    cfg.dynamicSmemBytes = kKv4SmemMax;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)c;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&ctx->cluster_room[c], kv4_attention_kernel<128, 1, 16, false>, &cfg) != cudaSuccess) {
+      cudaGetLastError();
+      ctx->cluster_room[c] = c == 1 ? ctx->sm_count : 0;
+    }
+  }
+  return IVIT_OK;
 }
 
 int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_kv4_attention_params& c) {
   const int d = (int)cache.d, page = (int)cache.page;
   const int64_t group = c.q_heads / cache.heads;
-  const Kv4Plan p = kv4_plan(d, page, group, cache.heads, c.seqs, c.max_q, c.max_len, ctx->sm_count);
+  const Kv4Plan p = kv4_plan(d, page, group, cache.heads, c.seqs, c.max_q, c.max_len, ctx->sm_count, ctx->cluster_room);
   if (p.smem > kKv4SmemMax || (int64_t)p.tiles * p.split > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
   AttendArgs a{};
   a.data = cache.data; a.pages = cache.pages; a.block_bytes = kv4_block_bytes(d, page);

@@ -105,7 +105,7 @@ inline Kv4Div kv4_div(unsigned d) {
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time
 constexpr int kKv4Copies = 8;      // copies of the exponentials
 constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: a byte of codes times a byte of a weight, over 32768 keys, stays below 2^31
-constexpr int kKv4Split = 48;      // blocks of a CTA below which it is not halved once more: an exchange costs what three of a warp's blocks do
+constexpr int kKv4Split = 32;      // fewest blocks of a CTA in a cluster: an exchange costs what two or three of a warp's blocks do
 constexpr int kKv4Small = 3968;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
 constexpr int kKv4SmemHalf = 113 * 1024;   // two CTAs on an SM
@@ -127,7 +127,7 @@ IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, in
   m.small = m.table + 256 * kKv4Copies * 4;
   m.sums = m.small + kKv4Small;
   m.peers = m.sums + 2 * rows * kv4_sum_ld(d) * 4;
-  m.pages = m.peers + (split > 1 ? 16 * rows * (4 + 2 * 8) + rows * d * 8 : 0);   // (see the kernel)
+  m.pages = m.peers + (split > 1 ? 16 * rows * (4 + 2 * 8) + (rows * d + 16) * 8 : 0);   // (see the kernel)
   m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 8 + 127) / 128 * 128;
   // behind the passes the ring holds the shares of the weights
   const int ring = warps * stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
@@ -140,36 +140,38 @@ struct Kv4Plan {
   // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, warps, blocks a warp holds, row tiles, bytes
   int rows, kept, split, blocks, warps, stages, tiles, smem;
 };
-inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms) {
+// room[c]: clusters of c CTAs, an SM for each, that the GPU runs at the same time (c <= 16).
+inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms, const int* room) {
   Kv4Plan p;
   const int64_t all = (max_len + kKv4Block - 1) / kKv4Block, q_rows = max_q * group;
   for (p.rows = q_rows <= 8 ? 8 : 16;; p.rows = 8) {
     p.tiles = (int)((q_rows + p.rows - 1) / p.rows);
     p.kept = (int)(q_rows < p.rows ? q_rows : p.rows);
     const int64_t ctas = (int64_t)p.tiles * heads * seqs;
-    // Three blocks under way for each warp where there is room, else two.  A CTA of 8 warps shares its SM with another (eight query rows),
-    // one of 16 has it alone.  Clusters of 16 CTAs with an SM each find room seven times on the GPU.
     auto fits = [&]() {
       p.blocks = (int)((all + p.split - 1) / p.split);
       if (p.blocks < 1) p.blocks = 1;
       const int64_t n = ctas * p.split;
-      // 16 warps: few CTAs, or few waves of them (sequences of uneven lengths, whose longest ends last); not many, which overlap one another
-      const bool wide = p.rows == 8 && p.blocks >= 16 && n < 4 * sms && (p.split == 1 || (p.split == 16 ? n <= 112 : n <= sms));
-      for (p.warps = wide ? 16 : 8; p.warps >= 8; p.warps -= 8) {
-        const int limit = p.rows == 8 && p.warps == 8 && (n > sms || p.split == 16) ? kKv4SmemHalf : kKv4SmemMax;
+      // 16 warps, an SM to themselves: few CTAs, or few waves of them (sequences of uneven lengths, whose longest ends last); not many, which
+      // overlap one another, two of 8 warps on an SM.  Three blocks under way for each warp where there is room, else two.
+      const bool wide = p.rows == 8 && p.blocks >= 16 && n < 4 * sms, pairs = p.rows == 8 && p.split == 1 && n > sms;
+      for (int form = wide ? 0 : (pairs ? 1 : 2); form < 3; ++form)
         for (p.stages = 4; p.stages >= 3; --p.stages) {
+          p.warps = form == 0 ? 16 : 8;
           p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps, p.stages).total;
-          if (p.smem <= limit) return p.blocks <= kKv4Blocks;
+          if (p.smem <= (form == 1 ? kKv4SmemHalf : kKv4SmemMax) && p.blocks <= kKv4Blocks) return true;
         }
-      }
-      p.warps = 8;
-      p.stages = 3;
       return false;
     };
-    p.split = 1;
-    while (p.split < 16 && 2 * ctas * p.split <= sms && all > (int64_t)p.split * kKv4Split) p.split *= 2;
-    while (!fits() && p.split < 16) p.split *= 2;
-    if ((p.smem <= kKv4SmemMax && p.blocks <= kKv4Blocks) || p.rows == 8) return p;
+    // the largest clusters that all run at once and leave their CTAs work enough; larger ones only where the scores need the room
+    p.split = 16;
+    while (p.split > 1 && (room[p.split] < ctas || all < (int64_t)p.split * kKv4Split)) --p.split;
+    bool ok = fits();
+    while (!ok && p.split < 16) {
+      ++p.split;
+      ok = fits();
+    }
+    if (ok || p.rows == 8) return p;
   }
 }
 

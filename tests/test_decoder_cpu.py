@@ -130,8 +130,8 @@ def test_row_scalars_on_the_host(tmp_path):
 def layout(tmp_path_factory):
     src = tmp_path_factory.mktemp("layout") / "t.cpp"
     src.write_text('#include "kv4_layout.cuh"\nusing namespace ivit;\nextern "C" {\n'
-                   'void plan(int d, int page, int64_t g, int64_t h, int64_t s, int64_t q, int64_t l, int sms, int* o) {\n'
-                   '  Kv4Plan p = kv4_plan(d, page, g, h, s, q, l, sms); Kv4Smem m = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps, p.stages);\n'
+                   'void plan(int d, int page, int64_t g, int64_t h, int64_t s, int64_t q, int64_t l, int sms, const int* room, int* o) {\n'
+                   '  Kv4Plan p = kv4_plan(d, page, g, h, s, q, l, sms, room); Kv4Smem m = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps, p.stages);\n'
                    '  int v[] = {p.rows, p.split, p.blocks, p.tiles, p.smem, m.table, m.small, m.sums, m.peers, m.pages, m.ring, m.score, kv4_score_ld(p.blocks), kv4_sum_ld(d), p.kept, p.stages, p.warps};\n'
                    '  for (int i = 0; i < 17; ++i) o[i] = v[i]; }\n'
                    'void seq(int q0, int q1, int len, int64_t tok, int64_t mq, int64_t ml, int64_t* o) {\n'
@@ -144,7 +144,7 @@ def layout(tmp_path_factory):
     subprocess.run(["g++", "-O2", "-shared", "-fPIC", "-I", os.path.join(ROOT, "paper_2207_01405_b200", "csrc"), "-o", str(so), str(src)], check=True)
     L = C.CDLL(str(so))
     i64 = C.c_int64
-    L.plan.argtypes = [C.c_int, C.c_int, i64, i64, i64, i64, i64, C.c_int, C.POINTER(C.c_int)]
+    L.plan.argtypes = [C.c_int, C.c_int, i64, i64, i64, i64, i64, C.c_int, C.POINTER(C.c_int), C.POINTER(C.c_int)]
     L.seq.argtypes = [C.c_int, C.c_int, C.c_int, i64, i64, i64, C.POINTER(i64)]
     L.seen.argtypes = [C.c_int, C.c_int, C.c_int, i64, i64, i64, C.c_int]
     L.quotient.argtypes = [i64, C.c_uint64]
@@ -156,20 +156,23 @@ def test_every_launch_fits(layout):
     """The plan of a launch covers every key and query row, and the parts of shared memory follow one another inside the limit."""
     rng = np.random.default_rng(6)
     o = (C.c_int * 17)()
+    rooms = [[0, 148, 74, 45, 33, 26, 22, 15, 15, 15, 11, 7, 7, 7, 7, 7, 7], [0, 148] + [0] * 15, [148] * 17]
+    room = (C.c_int * 17)()
     lens = [0, 1, 31, 32, 33, 256, 257, 1000, 4096, 12288, 12289, 24577, 65536, 100003, 131073, 196607, 196608]
     for d in (64, 128):
         for page in (32, 256):
             for L in lens + rng.integers(1, 196609, 30).tolist():
                 for g, h, s, q in ((1, 1, 1, 1), (4, 8, 1, 1), (8, 8, 64, 1), (9, 2, 3, 1), (16, 1, 1, 1), (17, 1, 1, 1), (4, 8, 5, 300), (1, 65535, 65535, 1),
                                    (7, 3, 2, 1 << 24)):
-                    layout.plan(d, page, g, h, s, q, L, 148, o)
+                    room[:] = rooms[(L + g) % 3]
+                    layout.plan(d, page, g, h, s, q, L, 148, room, o)
                     rows, split, blocks, tiles, smem, table, small, sums, peers, pages, ring, score, ld, sum_ld, kept, stages, warps = list(o)
-                    assert rows in (8, 16) and split in (1, 2, 4, 8, 16) and smem <= 227 * 1024
+                    assert rows in (8, 16) and 1 <= split <= 16 and smem <= 227 * 1024
                     assert tiles * rows >= q * g > (tiles - 1) * rows
                     assert split * blocks * 32 >= L and blocks >= 1
                     assert small - table >= 256 * 8 * 4 and sums - small >= 4 * 320 + 8 * 322 and peers - sums >= 2 * rows * sum_ld * 4 and pages >= peers and ring - pages >= 8 * (blocks * 32 // page + 2)
                     assert stages in (3, 4) and (warps == 8 or (warps == 16 and rows == 8)) and score - ring >= max(warps * stages * 32 * (d // 2 + d // 32), rows * 1024) and sum_ld >= d
-                    assert split == 1 or (pages - peers >= 16 * rows * 20 + 8 * rows * d and peers % 8 == 0 and rows * d % split == 0)
+                    assert split == 1 or (pages - peers >= 16 * rows * 20 + 8 * (rows * d + 16) and peers % 8 == 0 and -(-rows * d // split) * split <= rows * d + 16)
                     assert ld >= blocks * 32 and ld % 128 == 16 and smem >= score + kept * ld and 1 <= kept == min(rows, q * g)
                     assert ring % 128 == 0 and score % 16 == 0 and pages % 16 == 0 and small % 16 == 0
                     # eight rows, four words each, at the same keys: 32 banks
