@@ -295,19 +295,32 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
     }
   }
   // ---- weights above `prefix` stay, and the first `need` of those equal to it
-  unsigned above = 0, ties = 0;
+  unsigned above = 0, ties = 0, up_bits = 0, tie_bits = 0;   // (of this lane's keys, in order: one bit of each word for each turn)
+  int turn = 0;
   each([&](int j, unsigned long long k, bool there) {
-    const bool up = there && (j < lo || j >= hi || k > prefix);
-    above += __popc(__ballot_sync(~0u, up));
-    ties += __popc(__ballot_sync(~0u, there && !up && k == prefix));
+    const bool up = there && (j < lo || j >= hi || k > prefix), tie = there && !up && k == prefix;
+    if (kRegs) up_bits |= (unsigned)up << turn, tie_bits |= (unsigned)tie << turn, ++turn;
+    above += up;
+    ties += tie;
   });
+  above = __reduce_add_sync(~0u, above);
+  ties = __reduce_add_sync(~0u, ties);
   __syncthreads();   // (sums was read above)
   if (lane == 0) { sums[warp] = above; ties_s[warp] = ties; }
   __syncthreads();
   unsigned at_above = __reduce_add_sync(~0u, lane < warp ? sums[lane] : 0), at_ties = __reduce_add_sync(~0u, lane < warp ? ties_s[lane] : 0);
   const unsigned below = (1u << lane) - 1;
+  turn = 0;
   each([&](int j, unsigned long long k, bool there) {
-    const bool up = there && (j < lo || j >= hi || k > prefix), tie = there && !up && k == prefix;
+    bool up, tie;
+    if (kRegs) {
+      up = up_bits >> turn & 1;
+      tie = tie_bits >> turn & 1;
+      ++turn;
+    } else {
+      up = there && (j < lo || j >= hi || k > prefix);
+      tie = there && !up && k == prefix;
+    }
     const unsigned mu = __ballot_sync(~0u, up), mt = __ballot_sync(~0u, tie);
     const unsigned t = at_ties + __popc(mt & below);
     if (up || (tie && t < need)) kept[at_above + __popc(mu & below) + min(t, need)] = j;
@@ -316,72 +329,78 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
   });
 }
 
-// Moves the rows that stay, 16 bytes of codes to a thread.  kOrdered (in place): one CTA for each (sequence, head), group of rows behind
-// group of rows, each loaded before any of it is stored; rows that are read later lie behind those that are written.  Else the groups of rows are shared out.
+// Moves the rows that stay, 16 bytes of K and of V to a thread.  kOrdered (in place): one CTA for each (sequence, head), group of rows behind
+// group of rows, each loaded before any of it is stored; rows that are read later lie behind those that are written.  Else the groups of rows are
+// shared out.  Bound by the latency of three dependent loads (index, page, row), hence the rows that a thread has under way.
 template <int D, bool kOrdered>
 __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const EvictArgs a) {
-  constexpr int kParts = D / 32, kLanes = 2 * kParts, U = 4;       // chunks of a row of K or V; threads of a row; rows of a thread
-  constexpr int kThreads = kOrdered ? 512 : 256, kRows = kThreads / kLanes;
+  constexpr int kParts = D / 32, U = 4;                            // threads of a row; rows of a thread
+  constexpr int kThreads = kOrdered ? 512 : 256, kRows = kThreads / kParts;
   pdl_wait();
   pdl_trigger();
-  const int tid = threadIdx.x, sub = tid % kLanes, part = sub % kParts;
+  const int tid = threadIdx.x, part = tid % kParts;
   const int h = blockIdx.y, b = blockIdx.z;
-  const bool value = sub >= kParts;
   const int n = min(evict_len(a, b), a.keep);
   const int64_t bh = (int64_t)b * a.c.heads + h;
+  const int32_t* kept = a.kept + bh * a.keep;
+  const int32_t *from = a.table + b * a.ldtable, *to = a.dst + b * a.ld_dst;
+  const int64_t *w_in = a.w + bh * a.ldw;
+  int64_t* w_out = a.w_out + bh * a.ldw_out;
+  const int kstep = a.c.page * (D / 2), vcode = a.c.page * (D / 2 + D / 32), vstep = a.c.page * (D + D / 32);
   for (int i0 = blockIdx.x * (kRows * U); i0 < n; i0 += gridDim.x * (kRows * U)) {
-    uint4 x[U];
+    uint4 k[U], v[U];
     uint32_t st[U];
     int64_t w[U];
-    uint8_t *to[U];
     int j[U], sp[U], dp[U];
-    // (index, pages, rows: three loads behind one another, each of them for all U rows at once)
+    // (each of the three loads for all U rows at once)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = min(i0 + u * kRows + tid / kLanes, n - 1);
-      j[u] = a.kept[bh * a.keep + i];
-      dp[u] = a.dst[b * a.ld_dst + (i >> a.c.page_log)];
+      const int i = min(i0 + u * kRows + tid / kParts, n - 1);
+      j[u] = kept[i];
+      dp[u] = to[i >> a.c.page_log];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u) sp[u] = a.table[b * a.ldtable + (j[u] >> a.c.page_log)];
+    for (int u = 0; u < U; ++u) sp[u] = from[j[u] >> a.c.page_log];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kRows + tid / kLanes, o = j[u] & (a.c.page - 1);
+      const int i = i0 + u * kRows + tid / kParts, o = j[u] & (a.c.page - 1);
       const bool there = i < n && sp[u] >= 0 && sp[u] < a.c.pages && dp[u] >= 0 && dp[u] < a.c.pages;
-      const Block s = a.c.block(there ? sp[u] : 0, h);
-      to[u] = there ? a.c.block(dp[u], h).p : nullptr;
-      x[u] = make_uint4(0, 0, 0, 0);
+      const uint8_t* s = a.c.block(there ? sp[u] : 0, h).p;
+      if (!there) dp[u] = -1;
+      k[u] = v[u] = make_uint4(0, 0, 0, 0);
       st[u] = 0;
       w[u] = 0;
       if (there) {
-        x[u] = reinterpret_cast<const uint4*>(value ? s.vcode(o) : s.kcode(o))[part];
-        if (sub == 0) st[u] = D == 128 ? *reinterpret_cast<const uint32_t*>(s.kstep(o)) : *reinterpret_cast<const uint16_t*>(s.kstep(o));
-        if (sub == kParts) st[u] = *s.vstep(o);
+        k[u] = *reinterpret_cast<const uint4*>(s + o * (D / 2) + 16 * part);
+        v[u] = *reinterpret_cast<const uint4*>(s + vcode + o * (D / 2) + 16 * part);
+        if (part == 0) st[u] = D == 128 ? *reinterpret_cast<const uint32_t*>(s + kstep + o * 4) : *reinterpret_cast<const uint16_t*>(s + kstep + o * 2);
+        if (part == 1) st[u] = s[vstep + o];
       }
-      if (sub == 0 && i < n) {
-        w[u] = a.w[bh * a.ldw + j[u]];
+      if (part == 0 && i < n) {
+        w[u] = w_in[j[u]];
         if (!there) report(a.status, IVIT_ERR_RANGE);
       }
     }
     if (kOrdered) __syncthreads();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kRows + tid / kLanes;
-      if (i < n && sub == 0) a.w_out[bh * a.ldw_out + i] = w[u];
-      if (to[u]) {
-        const Block t{to[u], D, a.c.page};
+      const int i = i0 + u * kRows + tid / kParts;
+      if (i < n && part == 0) w_out[i] = w[u];
+      if (dp[u] >= 0) {
+        uint8_t* t = a.c.block(dp[u], h).p;
         const int o = i & (a.c.page - 1);
-        reinterpret_cast<uint4*>(value ? t.vcode(o) : t.kcode(o))[part] = x[u];
-        if (sub == 0) {
-          if (D == 128) *reinterpret_cast<uint32_t*>(t.kstep(o)) = st[u];
-          else *reinterpret_cast<uint16_t*>(t.kstep(o)) = (uint16_t)st[u];
+        *reinterpret_cast<uint4*>(t + o * (D / 2) + 16 * part) = k[u];
+        *reinterpret_cast<uint4*>(t + vcode + o * (D / 2) + 16 * part) = v[u];
+        if (part == 0) {
+          if (D == 128) *reinterpret_cast<uint32_t*>(t + kstep + o * 4) = st[u];
+          else *reinterpret_cast<uint16_t*>(t + kstep + o * 2) = (uint16_t)st[u];
         }
-        if (sub == kParts) *t.vstep(o) = (uint8_t)st[u];
+        if (part == 1) t[vstep + o] = (uint8_t)st[u];
       }
     }
     if (kOrdered) __syncthreads();
   }
-  for (int64_t i = n + (int64_t)blockIdx.x * kThreads + tid; i < a.ldw_out; i += (int64_t)gridDim.x * kThreads) a.w_out[bh * a.ldw_out + i] = 0;
+  for (int64_t i = n + (int64_t)blockIdx.x * kThreads + tid; i < a.ldw_out; i += (int64_t)gridDim.x * kThreads) w_out[i] = 0;
   if (h == 0 && blockIdx.x == 0 && tid == 0) a.new_lens[b] = n;
 }
 
@@ -398,7 +417,7 @@ int launch_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_kv4_
   }
   // in place (of the pages, or of the weights): in order
   const bool ordered = p.dst_table == p.table || p.weights_out == p.weights;
-  const int64_t rows = p.keep < p.max_len ? p.keep : p.max_len, per = 4 * 256 / (cache.d / 16);
+  const int64_t rows = p.keep < p.max_len ? p.keep : p.max_len, per = 4 * 256 / (cache.d / 32);
   const dim3 grid(ordered ? 1u : (unsigned)(rows > per ? (rows + per - 1) / per : 1), (unsigned)cache.heads, (unsigned)p.seqs);
   LaunchScope ls(ctx, KIND_MOVE, 2.0 * p.seqs * cache.heads * rows * (cache.d + cache.d / 32 + 9));
   if (cache.d == 128) ordered ? launch_k(kv4_compact_kernel<128, true>, grid, 512, 0, ctx->stream, a) : launch_k(kv4_compact_kernel<128, false>, grid, 256, 0, ctx->stream, a);

@@ -273,6 +273,40 @@ def test_attention_long_rows(d, page, hq, hk, L):
     attend(c, g, ref, q, hq, [2], [L], table, weights=True, pv=dyadic(1 / 400))
 
 
+@pytest.mark.parametrize("B,hk,G,d,L", [(1, 8, 4, 64, 11000), (2, 5, 1, 128, 12100), (3, 5, 2, 64, 9001), (4, 6, 3, 128, 6400), (11, 3, 5, 64, 4500),
+                                        (15, 3, 8, 128, 3300), (37, 2, 4, 64, 2500), (1, 7, 2, 128, 30001), (1, 1, 7, 64, 33000)])
+def test_attention_clusters(B, hk, G, d, L):
+    """Clusters of every size, sequences that use all of their cluster, some of it, or one CTA of it, and none at all."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(B * 100 + hk)
+    page = 64
+    lens = [L] + [int(v) for v in rng.integers(0, L + 1, B - 1)]
+    if B > 2:
+        lens[1], lens[2] = 0, 33
+    np_ = -(-L // page)
+    pages = min(B * np_, 900)
+    ref = filled(rng, pages, hk, d, page)
+    table = rng.integers(0, pages, (B, np_))                      # (sequences may share pages)
+    attend(c, g, ref, rand_i8(rng, (B, hk * G * d)), hk * G, [1] * B, lens, table, weights=True)
+    attend(c, g, ref, rand_i8(rng, (B, hk * G * d)), hk * G, [1] * B, lens, table)
+    assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("B", [40, 128, 129])
+def test_attention_uneven_batches(B):
+    """Batches whose sequences are taken longest first (up to 128 of them), with equal lengths among them, and one too large for that."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(B)
+    d, page, hk = 64, 32, 4
+    lens = rng.integers(0, 1500, B)
+    lens[::3] = 600
+    lens[5] = 0
+    np_ = 47
+    ref = filled(rng, 400, hk, d, page)
+    attend(c, g, ref, rand_i8(rng, (B, 2 * hk * d)), 2 * hk, [1] * B, lens, rng.integers(0, 400, (B, np_)), weights=True, max_len=1500)
+    assert c.poll_status() == 0
+
+
 def test_attention_longest():
     """The longest sequence that the entry point takes."""
     g, c = _g(), _g().ctx()
