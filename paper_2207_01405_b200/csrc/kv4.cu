@@ -36,8 +36,27 @@ __device__ __forceinline__ int signed_byte(uint32_t w, int b) {
   asm("prmt.b32 %0, %1, %1, %2;" : "=r"(d) : "r"(w), "r"(0x8880 + 0x1111 * b));
   return d;
 }
-__device__ __forceinline__ int top_of(uint32_t w) {   // largest magnitude of four int8
-  return max(max(abs(signed_byte(w, 0)), abs(signed_byte(w, 1))), max(abs(signed_byte(w, 2)), abs(signed_byte(w, 3))));
+__device__ __forceinline__ unsigned max_s16x2(unsigned a, unsigned b) {
+  unsigned d;
+  asm("max.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ unsigned min_s16x2(unsigned a, unsigned b) {
+  unsigned d;
+  asm("min.s16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ unsigned two_bytes(uint32_t w, int from) {   // bytes from, from + 1, sign-extended to 16 bits
+  unsigned d;
+  asm("prmt.b32 %0, %1, %1, %2;" : "=r"(d) : "r"(w), "r"(from ? 0xb3a2 : 0x9180));
+  return d;
+}
+// Largest magnitude of eight int8, two 16-bit values at a time: the larger of the maximum and of the minimum turned round.
+__device__ __forceinline__ int top_of(uint2 w) {
+  const unsigned a = two_bytes(w.x, 0), b = two_bytes(w.x, 2), c = two_bytes(w.y, 0), d = two_bytes(w.y, 2);
+  const unsigned hi = max_s16x2(max_s16x2(a, b), max_s16x2(c, d)), lo = min_s16x2(min_s16x2(a, b), min_s16x2(c, d));
+  const int h = max((int)(short)hi, (int)hi >> 16), l = min((int)(short)lo, (int)lo >> 16);
+  return max(h, -l);
 }
 // ceil(8 top / 7), top <= 128.
 __device__ __forceinline__ int step_of(int top) { return (8 * top + 6) / 7; }
@@ -45,9 +64,10 @@ __device__ __forceinline__ int step_of(int top) { return (8 * top + 6) / 7; }
 // product with r = floor(2^23 / step) + 1 (off by less than 4548 / 2^24 < 1 / (2 step)), whose upper byte is the quotient.  r = 0 and
 // eight in the end where the step is 0.
 __device__ __forceinline__ uint32_t codes_of(uint32_t w, int step, unsigned r) {
+  const unsigned m = 16u * r, c0 = 17u * (unsigned)step * r;   // (the sum is below 2^29, whatever its parts are modulo 2^32)
   unsigned p[4];
 #pragma unroll
-  for (int b = 0; b < 4; ++b) p[b] = (unsigned)(16 * signed_byte(w, b) + 17 * step) * r;
+  for (int b = 0; b < 4; ++b) p[b] = (unsigned)signed_byte(w, b) * m + c0;
   const uint32_t c = __byte_perm(__byte_perm(p[0], p[1], 0x0073), __byte_perm(p[2], p[3], 0x0073), 0x5410);
   return step ? c : 0x08080808u;
 }
@@ -80,7 +100,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const in
   const int vcode = c.page * (D / 2 + D / 32), kstep = c.page * (D / 2), vstep = c.page * (D + D / 32);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    int kt = max(top_of(k[u].x), top_of(k[u].y)), vt = max(top_of(v[u].x), top_of(v[u].y));
+    int kt = top_of(k[u]), vt = top_of(v[u]);
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) kt = max(kt, __shfl_xor_sync(~0u, kt, o));
 #pragma unroll
