@@ -499,7 +499,8 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv
  *   row i of dst_table's pages = that key's codes and steps;  weights_out[b, h, i] = its weight, 0 from new_lens[b] to ldw_out
  * In place: dst_table == table and weights_out == weights (with the same leading dimensions).  Else the pages of dst_table hold no
  * source row, and weights_out does not overlap weights.  new_lens may be lens.  sinks + recent <= keep; ldw >= max_len, ldw_out >= keep, ldtable >=
- * ceil(max_len / page), ld_dst >= ceil(min(keep, max_len) / page); max_len < 2^31.  lens above max_len and pages outside the pool are reported as above (such rows are not moved). */
+ * ceil(max_len / page), ld_dst >= ceil(min(keep, max_len) / page); max_len and keep <= 2^30.
+ * lens above max_len and pages outside the pool are reported as above (such rows are not moved). */
 typedef struct {
   const int64_t* weights; int64_t ldw;     /* [seqs, heads, ldw] */
   int64_t* weights_out; int64_t ldw_out;   /* [seqs, heads, ldw_out] */

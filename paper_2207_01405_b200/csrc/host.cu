@@ -1161,7 +1161,7 @@ int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_ev
   const int rc = check_kv4(cache, true);
   if (rc) return rc;
   if (p->keep < 1 || p->sinks < 0 || p->recent < 0 || p->sinks > p->keep || p->recent > p->keep - p->sinks) return IVIT_ERR_INVALID_ARG;
-  if (p->seqs > 65535 || p->max_len > 0x7fffffffll || p->keep > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
+  if (p->seqs > 65535 || p->max_len > (1ll << 30) || p->keep > (1ll << 30)) return IVIT_ERR_UNSUPPORTED;   // (indices run a turn past the end, in 32 bits)
   const int64_t rows = p->keep < p->max_len ? p->keep : p->max_len;
   if (p->ldw < p->max_len || p->ldw_out < p->keep || p->ldtable < (p->max_len + cache->page - 1) / cache->page ||
       p->ld_dst < (rows + cache->page - 1) / cache->page)

@@ -384,3 +384,10 @@ def test_evict_refusals(lib):
                     (-2, dict(w=AT + 4)), (-2, dict(wo=AT + 4)), (-2, dict(lens=AT + 2)), (-2, dict(table=AT + 2)), (-2, dict(dst=AT + 2)),
                     (-2, dict(kept=AT + 2)), (-2, dict(new=AT + 2))):
         assert evict(b, **k) == code, k
+
+
+def test_evict_refuses_what_its_indices_do_not_hold(lib):
+    """Indices are 32 bits and run up to a turn of all threads past the last key: 2^30 keys are the limit, of max_len and of keep."""
+    for k in (dict(ml=(1 << 30) + 1), dict(ml=(1 << 31) - 1), dict(keep=(1 << 30) + 1, ml=100), dict(keep=(1 << 31) - 1)):
+        assert evict(lib, **{**dict(ldw=1 << 31, ldt=1 << 30, ldwo=1 << 31, ldd=1 << 30), **k}) == -4, k
+    assert evict(lib, ml=1 << 30, keep=1 << 30, ldw=1 << 31, ldt=1 << 30, ldwo=1 << 31, ldd=1 << 30, seqs=0) == 0
