@@ -391,3 +391,10 @@ def test_evict_refuses_what_its_indices_do_not_hold(lib):
     for k in (dict(ml=(1 << 30) + 1), dict(ml=(1 << 31) - 1), dict(keep=(1 << 30) + 1, ml=100), dict(keep=(1 << 31) - 1)):
         assert evict(lib, **{**dict(ldw=1 << 31, ldt=1 << 30, ldwo=1 << 31, ldd=1 << 30), **k}) == -4, k
     assert evict(lib, ml=1 << 30, keep=1 << 30, ldw=1 << 31, ldt=1 << 30, ldwo=1 << 31, ldd=1 << 30, seqs=0) == 0
+
+
+def test_rmsnorm_refuses_a_sum_that_runs_over_its_own_stream(lib):
+    """sum == res with other leading dimensions: a row of the sum would lie on rows of res that are still to be read."""
+    for lds, ldr in ((64, 80), (80, 64)):
+        assert rms(lib, res=AT, ldr=ldr, sum=AT, lds=lds, rows=4) == -1
+    assert rms(lib, res=AT, ldr=80, sum=AT, lds=80, rows=0) == 0
