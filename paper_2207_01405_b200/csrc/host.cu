@@ -1093,10 +1093,10 @@ int ivit_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params* p) {
   if (p->C % 4 || p->C > 16384 || p->rows > 0x7fffffffll) return IVIT_ERR_UNSUPPORTED;
   if (p->M_ln < 8 || p->M_ln > 22) return IVIT_ERR_RANGE;
   if (p->ldx < p->C || p->ldout < p->C || (p->res && p->ldres < p->C) || (p->sum && p->ldsum < p->C)) return IVIT_ERR_INVALID_ARG;
-  if (p->sum && p->sum == p->res && p->ldsum != p->ldres) return IVIT_ERR_INVALID_ARG;
   auto misaligned = [](const void* q, int64_t ld, int dtype) { return !aligned16(q) || ld % (dtype == IVIT_I8 ? 16 : 4); };
   if (misaligned(p->x, p->ldx, p->x_dtype) || misaligned(p->out, p->ldout, IVIT_I8) || !aligned4(p->row_max)) return IVIT_ERR_ALIGNMENT;
   if ((p->res && misaligned(p->res, p->ldres, p->res_dtype)) || (p->sum && misaligned(p->sum, p->ldsum, p->res_dtype))) return IVIT_ERR_ALIGNMENT;
+  if (p->sum && p->sum == p->res && p->ldsum != p->ldres) return IVIT_ERR_INVALID_ARG;
   if (!scale_ok(p->gamma_scale) || (p->res && (!scale_ok(p->x_scale) || !scale_ok(p->res_scale) || p->res_scale.mult_c))) return IVIT_ERR_RANGE;
   if (!aligned4(p->gamma_scale.mult_c) || (p->res && !aligned4(p->x_scale.mult_c))) return IVIT_ERR_ALIGNMENT;
   if (p->rows == 0) return IVIT_OK;
