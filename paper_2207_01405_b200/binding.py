@@ -224,8 +224,9 @@ class DevScale:
         """From what is on the device already (int32 multipliers and uint8 shifts, one per channel), or from one pair of numbers."""
         self = cls(None, None)
         if torch.is_tensor(mult):
-            if mult.dtype != torch.int32 or shift.dtype != torch.uint8 or mult.shape != shift.shape or not (mult.is_contiguous() and shift.is_contiguous()):
-                raise ValueError("a per-channel scale is a contiguous int32 tensor and a uint8 tensor of the same length")
+            if (mult.dtype != torch.int32 or not torch.is_tensor(shift) or shift.dtype != torch.uint8 or mult.shape != shift.shape or
+                    not (mult.is_contiguous() and shift.is_contiguous()) or not mult.is_cuda or shift.device != mult.device):
+                raise ValueError("a per-channel scale is a contiguous int32 tensor and a uint8 tensor of the same length, on the same CUDA device")
             self.mult_t, self.shift_t = mult, shift
             self.c = CScale(mult.data_ptr(), shift.data_ptr(), 0, 0)
         else:
@@ -438,6 +439,12 @@ class Context:
         # (one row, or none, has no use for a leading dimension, and its stride may be anything)
         return shape, strides[0] if shape[0] > 1 else (shape[-1] + 15) // 16 * 16
 
+    def _fields(self, scale: DevScale, channels: int):
+        """A scale as the call descriptions hold it; its arrays have an entry for each channel, on the context's device."""
+        if scale.mult_t is not None and (scale.mult_t.numel() != channels or scale.mult_t.get_device() != self.index):
+            raise ValueError(f"a per-channel scale has an entry for each channel, on {self.device}")
+        return scale.fields
+
     def rmsnorm(self, x, gamma_scale: DevScale, x_scale: DevScale = None, res=None, res_scale: DevScale = None, M_ln=20, sum_out=None,
                 out=None, row_max=None):
         """ivit_rmsnorm: x (int8 or int32) [rows, C], with res added first (its sum goes to sum_out, which may be res); returns int8 rows.
@@ -457,9 +464,7 @@ class Context:
             r_shape, ldr = self._want("res", dt, 2, res)
             if x_scale is None or res_scale is None or r_shape != shape:
                 raise ValueError("res has the shape of x, and comes with x_scale and res_scale")
-            xs, rs, p_res = x_scale.fields, res_scale.fields, res.data_ptr()
-            if x_scale.mult_t is not None and x_scale.mult_t.numel() != Cc:
-                raise ValueError("a per-channel scale has an entry for each channel")
+            xs, rs, p_res = self._fields(x_scale, Cc), res_scale.fields, res.data_ptr()
             if sum_out is not None:
                 s_shape, lds = self._want("sum_out", dt, 2, sum_out)
                 if s_shape != shape:
@@ -467,14 +472,13 @@ class Context:
                 p_sum = sum_out.data_ptr()
         elif sum_out is not None:
             raise ValueError("sum_out comes with res")
-        if gamma_scale.mult_t is not None and gamma_scale.mult_t.numel() != Cc:
-            raise ValueError("a per-channel scale has an entry for each channel")
+        gs = self._fields(gamma_scale, Cc)
         if row_max is not None:
             if self._want("row_max", torch.int32, 1, row_max)[0][0] != rows:
                 raise ValueError("row_max has an entry for each row")
             p_max = row_max.data_ptr()
         rc = self.lib.ivit_rmsnorm(self.h, _RMSNORM.pack(x.data_ptr(), ldx, p_res, ldr, p_sum, lds, out.data_ptr(), ldo, p_max, rows, Cc, *xs, *rs,
-                                                         *gamma_scale.fields, I8 if x8 else I32, I8 if r8 else I32, M_ln))
+                                                         *gs, I8 if x8 else I32, I8 if r8 else I32, M_ln))
         if rc:
             raise IvitError(rc, "ivit_rmsnorm")
         return out

@@ -7,7 +7,9 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
 
+from ivit_inputs import Scale
 from ivit_inputs.gen import dyadic
 from oracle import api as O
 from oracle import decoder as D
@@ -398,3 +400,20 @@ def test_rmsnorm_refuses_a_sum_that_runs_over_its_own_stream(lib):
     for lds, ldr in ((64, 80), (80, 64)):
         assert rms(lib, res=AT, ldr=ldr, sum=AT, lds=lds, rows=4) == -1
     assert rms(lib, res=AT, ldr=80, sum=AT, lds=80, rows=0) == 0
+
+
+def test_scales_that_are_not_on_the_device_are_refused(lib):
+    """An array of multipliers in host memory would be read by the GPU as an address of its own."""
+    mult, shift = torch.full((64,), 2 ** 30, dtype=torch.int32), torch.full((64,), 35, dtype=torch.uint8)
+    for m, s in ((mult, shift), (mult, 35), (mult.long(), shift), (mult, shift[:32])):
+        with pytest.raises(ValueError):
+            lib.DevScale.of(m, s)
+    c = object.__new__(lib.Context)          # (no device, no library call: only the check)
+    c.index, c.device = 0, "cuda:0"
+    scale = lib.DevScale(Scale(mult.numpy(), shift.numpy()), "cpu")
+    for n in (64, 32):
+        with pytest.raises(ValueError):
+            c._fields(scale, n)
+    c.index = -1
+    assert c._fields(scale, 64) == scale.fields and c._fields(lib.DevScale.of(2 ** 30, 35), 7) == (0, 0, 2 ** 30, 35)
+    c.h = None
