@@ -552,3 +552,139 @@ def test_a_decoder_step_and_a_graph_of_it():
             g.assert_equal(g.host(weights), w_ref, f"weights, replay {i}")
         assert c.poll_status() == 0
         c.close()
+
+
+# ---- what the calls allow and the tests above do not make ----
+
+def test_two_contexts_at_once():
+    """Clusters of two streams on the GPU at the same time, each with a context of its own."""
+    g = _g()
+    rng = np.random.default_rng(31)
+    d, page, hk, hq, L = 128, 64, 4, 8, 20000
+    np_ = -(-L // page)
+    ref = filled(rng, np_, hk, d, page)
+    table = rng.permutation(np_)[None]
+    pool = cuda(ref.to_bytes())
+    qk, pv = dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40)), dyadic(1 / 128)
+    runs = []
+    for i in range(2):
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            q, length = rand_i8(rng, (1, hq * d)), L - 777 * i
+            runs.append(dict(s=s, c=g.binding.Context(0, s), q=q, length=length, dq=cuda(q), qs=cuda(np.array([0, 1], np.int32)),
+                             lens=cuda(np.array([length], np.int32)), table=cuda(table.astype(np.int32)),
+                             out=torch.zeros((1, hq * d), dtype=torch.int8, device="cuda"), w=torch.zeros((1, hk, L), dtype=torch.int64, device="cuda")))
+        s.synchronize()
+    for _ in range(10):
+        for r in runs:
+            with torch.cuda.stream(r["s"]):
+                r["c"].kv4_attention(g.binding.Kv4Cache(pool, d, page), r["dq"], r["qs"], r["lens"], r["table"], g.binding.DevScale.of(*qk),
+                                     ExpParams(17, 15), g.binding.DevScale.of(*pv), 1, L, out=r["out"], weights=r["w"])
+    torch.cuda.synchronize()
+    for r in runs:
+        want, w = D.attention(ref, r["q"], hq, [0, 1], [r["length"]], table, qk, 17, 15, pv, np.zeros((1, hq * d)), np.zeros((1, hk, L), np.int64))
+        g.assert_equal(g.host(r["out"]), want.astype(np.int8), "out")
+        g.assert_equal(g.host(r["w"]), 10 * w, "weights")
+        assert r["c"].poll_status() == 0
+        r["c"].close()
+
+
+def test_graph_of_a_split_sequence_and_its_eviction():
+    """Attention by clusters, then eviction in place, captured once and replayed while the length on the device changes."""
+    g = _g()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        c = g.binding.Context(0, stream)
+        rng = np.random.default_rng(32)
+        d, page, hk, hq, L, keep = 64, 64, 2, 8, 17000, 9000
+        np_ = -(-L // page)
+        ref = filled(rng, np_, hk, d, page)
+        table = rng.permutation(np_)[None].astype(np.int32)
+        cache = g.binding.Kv4Cache(cuda(ref.to_bytes()), d, page)
+        qk, pv = dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40)), dyadic(1 / 128)
+        dqk, dpv, dtable = g.binding.DevScale.of(*qk), g.binding.DevScale.of(*pv), cuda(table)
+        q = rand_i8(rng, (1, hq * d))
+        dq, qs, lens = cuda(q), cuda(np.array([0, 1], np.int32)), cuda(np.array([L], np.int32))
+        out, w = torch.zeros((1, hq * d), dtype=torch.int8, device="cuda"), torch.zeros((1, hk, L), dtype=torch.int64, device="cuda")
+        kept, new = torch.zeros((1, hk, keep), dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            c.kv4_attention(cache, dq, qs, lens, dtable, dqk, ExpParams(17, 15), dpv, 1, L, out=out, weights=w)
+            c.kv4_evict(cache, w, lens, dtable, keep, 4, 100, L, kept=kept, new_lens=new)
+        ww = np.zeros((1, hk, L), np.int64)
+        for length in (L, 9000, 8999, 9500, 40, 0):
+            lens.copy_(cuda(np.array([length], np.int32)))
+            graph.replay()
+            stream.synchronize()
+            want, ww = D.attention(ref, q, hq, [0, 1], [length], table, qk, 17, 15, pv, np.zeros((1, hq * d)), ww)
+            wk, wn, ww, pool = D.evict(ref, ww, [length], table, table, L, keep, 4, 100)
+            g.assert_equal(g.host(out), want.astype(np.int8), f"out, {length}")
+            g.assert_equal(g.host(kept), wk.astype(np.int32), f"kept, {length}")
+            g.assert_equal(g.host(w), ww, f"weights, {length}")
+            g.assert_equal(g.host(cache.pool), pool, f"pool, {length}")
+            assert int(new) == wn[0]
+        assert c.poll_status() == 0
+        c.close()
+
+
+@pytest.mark.parametrize("pages_in_place,weights_in_place", [(True, False), (False, True)])
+def test_evict_with_only_one_of_two_in_place(pages_in_place, weights_in_place):
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(33)
+    L, keep, page, hk, B = 1100, 300, 32, 3, 2
+    ps, pd = -(-L // page), -(-keep // page)
+    ref = filled(rng, B * (ps + pd), hk, 128, page)
+    order = rng.permutation(B * (ps + pd)).astype(np.int32)
+    table, dst = order[:B * ps].reshape(B, ps), order[B * ps:].reshape(B, pd)
+    w = rng.integers(0, 10 ** 6, (B, hk, L))
+    cache, dw, dt = g.binding.Kv4Cache(cuda(ref.to_bytes()), 128, page), cuda(w), cuda(table)
+    wo = dw if weights_in_place else torch.full((B, hk, keep + 1), -1, dtype=torch.int64, device="cuda")
+    kept, _ = c.kv4_evict(cache, dw, cuda(np.array([L, 299], np.int32)), dt, keep, 3, 7, L, dst_table=dt if pages_in_place else cuda(dst), weights_out=wo)
+    wk, _, ww, pool = D.evict(ref, w, [L, 299], table, table if pages_in_place else dst, wo.shape[2], keep, 3, 7)
+    g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+    g.assert_equal(g.host(wo), ww, "weights")
+    g.assert_equal(g.host(cache.pool), pool, "pool")
+
+
+def test_the_binding_refuses_what_the_library_would_misread():
+    """Types, shapes, strides and devices: refused before anything is launched."""
+    g, c = _g(), _g().ctx()
+    B = g.binding
+    z = lambda *s, t=torch.int8: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    one = B.DevScale.of(2 ** 30, 40)
+    host_scale = B.DevScale(Scale(np.full(64, 2 ** 30, np.int32), np.full(64, 40, np.uint8)), "cpu")
+    x, cache = z(4, 64), B.Kv4Cache.empty(4, 2, 64, 32, "cuda")
+    lens, qs, table, w = z(2, t=torch.int32), z(3, t=torch.int32), z(2, 2, t=torch.int32), z(2, 2, 64, t=torch.int64)
+    q, smax = z(2, 256), ExpParams(17, 15)
+    att = lambda **k: c.kv4_attention(**{**dict(cache=cache, q=q, q_start=qs, lens=lens, table=table, qk_scale=one, smax=smax, pv_scale=one, max_q=1, max_len=64), **k})  # noqa: E731
+    evi = lambda **k: c.kv4_evict(**{**dict(cache=cache, weights=w, lens=lens, table=table, keep=40, sinks=1, recent=1, max_len=64), **k})  # noqa: E731
+    app = lambda **k: c.kv4_append(**{**dict(cache=cache, k=z(4, 128), v=z(4, 128), slots=z(4, t=torch.int64)), **k})  # noqa: E731
+    nrm = lambda **k: c.rmsnorm(**{**dict(x=x, gamma_scale=one), **k})  # noqa: E731
+    before = c.launch_count()
+    for f, bad in ((nrm, [dict(x=x.cpu()), dict(x=x.half()), dict(x=z(64)), dict(x=z(64, 64).t()[:4]), dict(out=z(4, 48)), dict(out=z(4, 64, t=torch.int32)),
+                          dict(res=x), dict(res=z(3, 64), x_scale=one, res_scale=one), dict(sum_out=x), dict(row_max=z(3, t=torch.int32)),
+                          dict(row_max=z(4, t=torch.int64)), dict(gamma_scale=host_scale), dict(res=x, x_scale=host_scale, res_scale=one),
+                          dict(res=x, x_scale=one, res_scale=one, sum_out=z(4, 64, t=torch.int32))]),
+                   (app, [dict(k=z(4, 64), v=z(4, 64)), dict(v=z(3, 128)), dict(slots=z(3, t=torch.int64)), dict(slots=z(4, t=torch.int32)),
+                          dict(slots=z(4, t=torch.int64).cpu()), dict(k=z(4, 256)[:, ::2]), dict(slots=z(8, t=torch.int64)[::2])]),
+                   (att, [dict(q=q.cpu()), dict(q=z(2, 100)), dict(out=z(3, 256)), dict(q_start=z(2, t=torch.int32)), dict(q_start=z(3, t=torch.int64)),
+                          dict(lens=lens.cpu()), dict(table=z(3, 2, t=torch.int32)), dict(table=z(2, 1, t=torch.int32)), dict(max_len=65),
+                          dict(table=z(2, 2, t=torch.int64)), dict(weights=z(2, 1, 64, t=torch.int64)), dict(weights=z(2, 2, 64, t=torch.int32)),
+                          dict(weights=z(2, 2, 128, t=torch.int64)[:, :, :64])]),
+                   (evi, [dict(weights=z(1, 2, 64, t=torch.int64)), dict(weights=w[:, :, ::2]), dict(table=table.t()), dict(max_len=65),
+                          dict(dst_table=z(2, 1, t=torch.int32)), dict(weights_out=z(2, 3, 64, t=torch.int64)), dict(kept=z(2, 2, 39, t=torch.int32)),
+                          dict(new_lens=z(3, t=torch.int32)), dict(lens=lens.cpu())])):
+        for k in bad:
+            with pytest.raises(ValueError):
+                f(**k)
+    for make in (lambda: B.Kv4Cache(z(4, 2, 32 * 67), 64, 32), lambda: B.Kv4Cache(z(4, 2, 32 * 67 + 1, t=torch.uint8), 64, 32),
+                 lambda: B.Kv4Cache(z(4, 2, 48 * 67, t=torch.uint8), 64, 48)):
+        with pytest.raises(ValueError):
+            make()
+    with pytest.raises(B.IvitError):
+        evi(weights_out=z(2, 2, 39, t=torch.int64))
+    assert c.launch_count() == before
+    torch.cuda.synchronize()
+    assert c.poll_status() == 0
