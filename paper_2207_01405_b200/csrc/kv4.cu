@@ -6,27 +6,17 @@ namespace ivit {
 
 __device__ __forceinline__ void report(int* status, int code) { *(volatile int*)status = code; }
 
-// One (page, head) block.
-struct Block {
-  uint8_t* p;
-  int d, page;
-  __device__ __forceinline__ uint8_t* kcode(int o) const { return p + o * (d / 2); }
-  __device__ __forceinline__ uint8_t* kstep(int o) const { return p + page * (d / 2) + o * (d / 32); }
-  __device__ __forceinline__ uint8_t* vcode(int o) const { return p + page * (d / 2 + d / 32) + o * (d / 2); }
-  __device__ __forceinline__ uint8_t* vstep(int o) const { return p + page * (d + d / 32) + o; }
-};
-
 struct Cache {
   uint8_t* data;
   int64_t pages;
-  int heads, d, page, page_log, block_bytes;
-  __device__ __forceinline__ Block block(int pg, int h) const { return Block{data + ((int64_t)pg * heads + h) * block_bytes, d, page}; }
+  int heads, page, page_log, block_bytes;
+  __device__ __forceinline__ uint8_t* block(int pg, int h) const { return data + ((int64_t)pg * heads + h) * block_bytes; }
 };
 
 static Cache to_dev(const ivit_kv4_cache* c) {
   int lg = 0;
   while ((1 << lg) < c->page) ++lg;
-  return Cache{c->data, c->pages, (int)c->heads, (int)c->d, (int)c->page, lg, (int)(c->page * (c->d + c->d / 32 + 1))};
+  return Cache{c->data, c->pages, (int)c->heads, (int)c->page, lg, (int)kv4_block_bytes((int)c->d, (int)c->page)};
 }
 
 // ---------------------------------------------------------------- append
@@ -74,7 +64,8 @@ __device__ __forceinline__ uint32_t codes_of(uint32_t w, int step, unsigned r) {
 
 // D / 8 lanes take a row of one token and head: eight channels each of K and of V, so that loads and stores of codes are runs of double
 // words; the lanes with a word's low and high halves are 2 apart in K, D / 16 apart in V.  U rows at a time keep loads in flight.  What
-// bounds it is the issue of instructions; with four channels a lane, and a division for each step and for the head, it took twice the time.
+// bounds it is the issue of instructions (20 011 tokens x 8 heads of 64 12.5 us, with four rows at a time 13.0, of those 11.6 without the stores; 31 MB would
+// take 4.8); with four channels a lane, and a division for each step and for the head, it took twice the time.
 template <int D, int U>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const int8_t* __restrict__ K, int64_t ldk, const int8_t* __restrict__ V,
                                                          int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, Kv4Div by_heads, int* status) {
@@ -97,7 +88,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const in
     slot[u] = r0 + u * kPer < rows ? slots[t] : -1;
   }
   __syncthreads();
-  const int vcode = c.page * (D / 2 + D / 32), kstep = c.page * (D / 2), vstep = c.page * (D + D / 32);
+  const int kstep = kv4_kstep(D, c.page, 0), vcode = kv4_vcode(D, c.page, 0), vstep = kv4_vstep(D, c.page, 0);
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     int kt = top_of(k[u]), vt = top_of(v[u]);
@@ -117,7 +108,7 @@ __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const in
       if (l == 0) report(status, IVIT_ERR_RANGE);
       continue;
     }
-    uint8_t* p = c.block((int)(slot[u] >> c.page_log), h[u]).p;
+    uint8_t* p = c.block((int)(slot[u] >> c.page_log), h[u]);
     const int o = (int)slot[u] & (c.page - 1), g = l >> 2;
     if ((l & 2) == 0) {                          // words 2 (l & 1) and the next one of group g
       uint32_t* dst = reinterpret_cast<uint32_t*>(p + o * (D / 2)) + D / 32 * (2 * (l & 1)) + g;
@@ -135,14 +126,14 @@ int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* 
   if (tokens == 0) return IVIT_OK;
   LaunchScope ls(ctx, KIND_MOVE, (double)tokens * cache->heads * (3 * cache->d + cache->d / 32 + 1));
   const unsigned rows = (unsigned)(tokens * cache->heads);
-  const int per = cache->d == 128 ? 16 : 32;
-  const bool many = rows >= 64u * (unsigned)ctx->sm_count;    // (below, the rows are better spread over the SMs)
-  const unsigned grid = (rows + (many ? 4 * per : per) - 1) / (many ? 4 * per : per);
-  auto go = [&](auto k) {
-    launch_k(k, grid, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, kv4_div((unsigned)cache->heads), ctx->status_dev);
+  // One row at a time up to 400 for each SM, then several, whose loads are all under way (us, one / several): 5000 tokens x 8 heads of 64 4.4 / 5.8, of 128
+  // 7.4 / 7.8; 20011 tokens 13.2 / 12.5 and 24.9 / 22.9 (of 64 with four 13.0, of 128 with two 24.0).
+  const bool many = rows >= 400u * (unsigned)ctx->sm_count;
+  auto go = [&](auto k, unsigned per) {
+    launch_k(k, (rows + per - 1) / per, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, kv4_div((unsigned)cache->heads), ctx->status_dev);
   };
-  if (cache->d == 128) many ? go(kv4_append_kernel<128, 4>) : go(kv4_append_kernel<128, 1>);
-  else many ? go(kv4_append_kernel<64, 4>) : go(kv4_append_kernel<64, 1>);
+  if (cache->d == 128) many ? go(kv4_append_kernel<128, 4>, 64) : go(kv4_append_kernel<128, 1>, 16);
+  else many ? go(kv4_append_kernel<64, 2>, 64) : go(kv4_append_kernel<64, 1>, 32);
   return ls.done();
 }
 
@@ -183,6 +174,8 @@ __device__ __forceinline__ int first_digit(unsigned long long k) {
 //   1. counts of the first digits, and the digit in which `need` of the largest are reached;
 //   2. the keys of that digit: one value (small weights; all equal) needs no more, up to 1024 are ranked against one another, more are told apart byte by byte;
 //   3. each warp counts what stays of its run, and writes it behind what stays of the runs in front.
+// 12 sequences x 8 heads of 16 001 keys: 19 us, of which the weights' 12.3 MB would be 2; with 96 CTAs it is their passes, one behind the other, that
+// count.  Reading the keys again in each pass takes 19 us more (41.3 / 60.0 for the whole call); for 4000 keys it is all the same (11.8 / 11.3).
 template <bool kRegs>
 __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
   constexpr int kKeys = 16;
@@ -351,7 +344,8 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
 
 // Moves the rows that stay, 16 bytes of K and of V to a thread.  kOrdered (in place): one CTA for each (sequence, head), group of rows behind
 // group of rows, each loaded before any of it is stored; rows that are read later lie behind those that are written.  Else the groups of rows are
-// shared out.  Bound by the latency of three dependent loads (index, page, row), hence the rows that a thread has under way.
+// shared out.  Bound by the latency of three dependent loads (index, page, row), hence the rows that a thread has
+// under way: 12 sequences x 8 heads, 4001 rows of 16 001, 102 MB in 25 us, 0.48 of the DRAM's peak.
 template <int D, bool kOrdered>
 __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const EvictArgs a) {
   constexpr int kParts = D / 32, U = 4;                            // threads of a row; rows of a thread
@@ -366,7 +360,7 @@ __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const
   const int32_t *from = a.table + b * a.ldtable, *to = a.dst + b * a.ld_dst;
   const int64_t *w_in = a.w + bh * a.ldw;
   int64_t* w_out = a.w_out + bh * a.ldw_out;
-  const int kstep = a.c.page * (D / 2), vcode = a.c.page * (D / 2 + D / 32), vstep = a.c.page * (D + D / 32);
+  const int kstep = kv4_kstep(D, a.c.page, 0), vcode = kv4_vcode(D, a.c.page, 0), vstep = kv4_vstep(D, a.c.page, 0);
   for (int i0 = blockIdx.x * (kRows * U); i0 < n; i0 += gridDim.x * (kRows * U)) {
     uint4 k[U], v[U];
     uint32_t st[U];
@@ -385,7 +379,7 @@ __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * kRows + tid / kParts, o = j[u] & (a.c.page - 1);
       const bool there = i < n && sp[u] >= 0 && sp[u] < a.c.pages && dp[u] >= 0 && dp[u] < a.c.pages;
-      const uint8_t* s = a.c.block(there ? sp[u] : 0, h).p;
+      const uint8_t* s = a.c.block(there ? sp[u] : 0, h);
       if (!there) dp[u] = -1;
       k[u] = v[u] = make_uint4(0, 0, 0, 0);
       st[u] = 0;
@@ -407,7 +401,7 @@ __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const
       const int i = i0 + u * kRows + tid / kParts;
       if (i < n && part == 0) w_out[i] = w[u];
       if (dp[u] >= 0) {
-        uint8_t* t = a.c.block(dp[u], h).p;
+        uint8_t* t = a.c.block(dp[u], h);
         const int o = i & (a.c.page - 1);
         *reinterpret_cast<uint4*>(t + o * (D / 2) + 16 * part) = k[u];
         *reinterpret_cast<uint4*>(t + vcode + o * (D / 2) + 16 * part) = v[u];

@@ -20,7 +20,7 @@ struct AttendArgs {
   int pv_mult, pv_shift, I0, N, z;
   int8_t* O; int64_t ldo;
   int64_t* weights; int64_t ldw;
-  int max_q, max_len, split, blocks, kept, stages, sorted;   // sorted: the number of sequences, which go longest first (0: in their order)
+  int max_q, max_len, split, blocks, kept, sorted;   // sorted: the number of sequences, which go longest first (0: in their order)
   int* status;
 };
 
@@ -33,11 +33,6 @@ __device__ __forceinline__ void cp16_if(bool ok, uint32_t dst, const void* src) 
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-// All but the last `stages` - 2 groups (3 or 4 stages).
-__device__ __forceinline__ void cp_wait_stages(int stages) {
-  if (stages == 4) cp_wait<2>();
-  else cp_wait<1>();
-}
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 __device__ __forceinline__ uint32_t peer_addr(uint32_t a, int rank) {
@@ -101,10 +96,15 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
 //   scores:  S^T = K Q^T on m16n8k32 products, keys along M, the query rows along N (a decoder has 1 to 16 of them: none is padding of 16).
 //            One product of 32 channels is one group of a key, whose step multiplies it in 32 bits; the int8 scores stay in shared memory.
 //   values:  O^T = V^T U, channels along M, the weights u (16 bits) as two planes of unsigned bytes.
-// A warp brings its codes in with cp.async, kKv4Stages blocks ahead (the first blocks of V are under way across the exchange of the
-// maxima), and unpacks them in registers: three instructions for eight codes of K, and a transpose of bytes more for V, whose products
-// run along the keys.  Maxima, sums and outputs of the cluster's CTAs meet in distributed shared memory: one launch, no workspace, and
-// integer sums, so that the order changes nothing.
+// A warp brings its codes in with cp.async, kKv4Stages - 1 blocks ahead (the first blocks of V are under way across the exchange of the
+// maxima).  K is unpacked in registers, three instructions for eight codes; V's rows are transposed by the loads, and a byte goes into the
+// products as it is, or with its lower half cleared: the difference of the two sums is the lower code's.  Maxima, sums and outputs of the
+// cluster's CTAs meet in distributed shared memory: one launch, no workspace, and integer sums, so that the order changes nothing.
+//
+// What bounds it, decoding: 37 sequences of up to 7000 keys, 32 / 8 heads of 128, 139 MB, 33 us (4.2 TB/s, 0.64 of the copy rate): about
+// 160 clocks of an SM for 32 keys, in which no unit is busy half of the time (issue 48 % of all cycles, shared memory 37 %, ALU 35 %), and 8000 clocks
+// around a CTA's keys (set-up, exponentials, exchange, sums, quotients).  Many query rows (16 a CTA): registers hold the sums, two warps
+// for a scheduler do not cover one another's latencies: issue 42 %.
 template <int D, int RN, int W, bool kWeights>
 __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attention_kernel(const AttendArgs a) {
   constexpr int kG = D / 32;               // groups of a key
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n8 = lane >> 2, t4 = lane & 3;
   const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split, h = blockIdx.y;
   int b = blockIdx.z;
-  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks, a.split, W, a.stages);
+  const Kv4Smem at = kv4_smem(D, kRows, a.kept, a.page, a.blocks, a.split, W);
   const uint8_t** const pages = reinterpret_cast<const uint8_t**>(sm + at.pages);   // this head's block of each page of the run
   int* const small = reinterpret_cast<int*>(sm + at.small);
   int* const lim = small;                                                            // [16] keys that a row sees
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   }
   const bool holes = __syncthreads_or(bad) != 0;   // a page of the run points nowhere: its keys are not seen
 
-  uint8_t* const ring = sm + at.ring + warp * (a.stages * kStage);
+  uint8_t* const ring = sm + at.ring + warp * (kKv4Stages * kStage);
   // A block's codes lie in the ring as rows of 16-byte chunks, at a place of their own for each (row, chunk) that keeps three kinds of
   // access off the same banks: eight rows one behind the other (V, transposed), every fourth row (K), and the rows as they come in.
   auto place = [](int row, int chunk) {
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   const int in_page = a.page / kKv4Block - 1, per_page = a.page_log - 5;
   // page and place in it of the run's block lb: pages[(lb + first) >> per_page], (lb + first) & in_page
   const int first = blk0 & in_page;
-  const int kstep = kv4_kstep(D, a.page, 0), vcode = kv4_vcode(D, a.page, 0), vstep = kv4_vstep(D, a.page, 0);
+  const int kcode = kv4_kcode(D, a.page, 0), kstep = kv4_kstep(D, a.page, 0), vcode = kv4_vcode(D, a.page, 0), vstep = kv4_vstep(D, a.page, 0);
   auto page_of = [&](int lb) { return lb < nblk ? pages[(lb + first) >> per_page] : nullptr; };
   auto request = [&](int lb, const uint8_t* src, uint32_t stage, int code, int step, int step_bytes) {
     const int o = (lb + first) & in_page;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
     cp16_if(src != nullptr && lane < step_bytes / 16, put_step + stage, src + (step + o * step_bytes + 16 * lane));
     cp_commit();
   };
-  auto request_k = [&](int lb, const uint8_t* src, uint32_t stage) { request(lb, src, stage, 0, kstep, kKv4Block * kG); };
+  auto request_k = [&](int lb, const uint8_t* src, uint32_t stage) { request(lb, src, stage, kcode, kstep, kKv4Block * kG); };
   auto request_v = [&](int lb, const uint8_t* src, uint32_t stage) { request(lb, src, stage, vcode, vstep, kKv4Block); };
 
   // where the lane's parts of K rows 4 n8 + i lie, and its row of V, chunk by chunk
@@ -269,16 +269,16 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   for (int c = 0; c < D / 32; ++c) v_at[c] = place(lane, c);
 
   // ---- scores
-  for (int s = 0; s < a.stages - 1; ++s) request_k(warp + W * s, page_of(warp + W * s), s * kStage);
+  for (int s = 0; s < kKv4Stages - 1; ++s) request_k(warp + W * s, page_of(warp + W * s), s * kStage);
   int best[RN][2];
 #pragma unroll
   for (int j = 0; j < RN; ++j) best[j][0] = best[j][1] = -128;
-  const int ahead = W * (a.stages - 1);
-  const uint32_t last = (a.stages - 1) * kStage;
+  constexpr int ahead = W * (kKv4Stages - 1);
+  constexpr uint32_t last = (kKv4Stages - 1) * kStage;
   uint32_t stage = 0, behind = last;                        // the block at hand; where the one requested now goes
   const uint8_t* next = page_of(warp + ahead);             // (looked up a turn before it is needed)
   for (int lb = warp; lb < nblk; lb += W) {
-    cp_wait_stages(a.stages);
+    cp_wait<kKv4Stages - 2>();
     __syncwarp();
     const uint8_t* buf = ring + stage;
     // what the turn reads, then the request, then the arithmetic: the first is on its way while the second is issued
@@ -346,7 +346,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   }
   cp_wait<0>();
   __syncwarp();
-  for (int s = 0; s < a.stages - 1; ++s) request_v(warp + W * s, page_of(warp + W * s), s * kStage);
+  for (int s = 0; s < kKv4Stages - 1; ++s) request_v(warp + W * s, page_of(warp + W * s), s * kStage);
   next = page_of(warp + ahead);
 #pragma unroll
   for (int j = 0; j < RN; ++j)
@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
   constexpr uint32_t kSel = (uint32_t)(-4 * kKv4Copies) & 255u;
   stage = 0, behind = last;
   for (int lb = warp; lb < nblk; lb += W) {
-    cp_wait_stages(a.stages);
+    cp_wait<kKv4Stages - 2>();
     __syncwarp();
     const uint8_t* buf = ring + stage;
     uint32_t sc[RN][2], vs[2][4], y[D / 32][4];
@@ -661,8 +661,9 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_
   const int64_t top = (int64_t)c.smax.I0 << c.smax.N;
   while (top >> (a.z + 8)) ++a.z;
   a.O = c.O; a.ldo = c.ldo; a.weights = c.weights; a.ldw = c.ldw;
-  a.max_q = (int)c.max_q; a.max_len = (int)c.max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept; a.stages = p.stages;
-  // (few waves of long CTAs: worth the 0.2 us that finding one's sequence takes; the numbers wait where the scores will be)
+  a.max_q = (int)c.max_q; a.max_len = (int)c.max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept;
+  // Few waves of long CTAs go longest first: 37 sequences of up to 7000 keys 33.6 us / 41.3 in their order; it takes 0.2 us to find a CTA's sequence (the
+  // lengths wait where the scores will be).
   const int64_t ctas = cache.heads * c.seqs;
   a.sorted = p.warps == 16 && p.split == 1 && p.tiles == 1 && ctas > ctx->sm_count && c.seqs <= 128 ? (int)c.seqs : 0;
   a.status = ctx->status_dev;

@@ -105,10 +105,10 @@ inline Kv4Div kv4_div(unsigned d) {
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time
 constexpr int kKv4Copies = 8;      // copies of the exponentials
 constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: a byte of codes times a byte of a weight, over 32768 keys, stays below 2^31
-constexpr int kKv4Split = 32;      // fewest blocks of a CTA in a cluster: an exchange costs what two or three of a warp's blocks do
+constexpr int kKv4Stages = 3;      // blocks that a warp holds: one that it works on, two on their way (with a fourth 0 to 3 % slower: 34.2 / 33.3 us for
+                                   // 37 sequences of up to 7000 keys, 65.6 / 64.5 for pieces of prompts)
 constexpr int kKv4Small = 3968;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
-constexpr int kKv4SmemHalf = 113 * 1024;   // two CTAs on an SM
 
 // Bytes of a row of scores in shared memory: 16 modulo 128, so that eight rows at the same keys lie in different banks.
 IVIT_KV4_FN int kv4_score_ld(int blocks) { return (blocks * kKv4Block + 127) / 128 * 128 + 16; }
@@ -120,8 +120,8 @@ struct Kv4Smem {
   int table, small, sums, peers, pages, ring, score, total;
 };
 // rows: query rows of a CTA (8 or 16); kept: those of them that some sequence can have, whose scores are kept; blocks: blocks of keys of a CTA;
-// split: CTAs of a cluster; warps: of a CTA; stages: blocks that a warp holds, one it works on and the others on their way.
-IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, int split, int warps, int stages) {
+// split: CTAs of a cluster; warps: of a CTA.
+IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, int split, int warps) {
   Kv4Smem m;
   m.table = 0;
   m.small = m.table + 256 * kKv4Copies * 4;
@@ -130,42 +130,43 @@ IVIT_KV4_FN Kv4Smem kv4_smem(int d, int rows, int kept, int page, int blocks, in
   m.pages = m.peers + (split > 1 ? 16 * rows * (4 + 2 * 8) + (rows * d + 16) * 8 : 0);   // (see the kernel)
   m.ring = (m.pages + (blocks * kKv4Block / page + 2) * 8 + 127) / 128 * 128;
   // behind the passes the ring holds the shares of the weights
-  const int ring = warps * stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
+  const int ring = warps * kKv4Stages * kv4_stage_bytes(d), shares = rows * 256 * 4;
   m.score = m.ring + (ring > shares ? ring : shares);
   m.total = m.score + kept * kv4_score_ld(blocks);
   return m;
 }
 
 struct Kv4Plan {
-  // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, warps, blocks a warp holds, row tiles, bytes
-  int rows, kept, split, blocks, warps, stages, tiles, smem;
+  // query rows of a CTA, those with scores, CTAs of a cluster along the keys, blocks of each, warps, row tiles, bytes
+  int rows, kept, split, blocks, warps, tiles, smem;
 };
-// room[c]: clusters of c CTAs, an SM for each, that the GPU runs at the same time (c <= 16).
+// room[c]: clusters of c CTAs, an SM for each, that the GPU runs at the same time (c <= 16).  The rules were drawn by measurement (us, of the two sides; 8
+// heads of 128 unless noted):
+//   16 query rows a CTA only where tiles of 8 would not run at once: 4 heads, 14 rows: 16 sequences of 3000 keys 15.4 / 14.2 with 8, 30 sequences 19.1 / 22.7
+//   clusters from 24 blocks on, with 8 blocks a CTA at least: 2 sequences of 3000 keys 11.9 in one CTA each head / 8.9 in six, of 600 keys 7.1 / 7.6;
+//   and no larger than run at once: one of 100 003 keys 35.4 in clusters of 10 / 50.2 in clusters of 16, which wait for one another
+//   16 warps, alone on an SM, from 40 blocks a CTA on for each wave of CTAs (few of them: sequences are of uneven lengths, and the longest ends last), else
+//   8, two CTAs on an SM, which overlap one another: 37 sequences of 7000 keys 34.2 / 43.9, of 2000 18.9 / 17.0; 150 of 3000 88 / 67
 inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms, const int* room) {
   Kv4Plan p;
   const int64_t all = (max_len + kKv4Block - 1) / kKv4Block, q_rows = max_q * group;
-  for (p.rows = q_rows <= 8 ? 8 : 16;; p.rows = 8) {
+  for (p.rows = q_rows <= 8 || (q_rows + 7) / 8 * heads * seqs <= sms ? 8 : 16;; p.rows = 8) {
     p.tiles = (int)((q_rows + p.rows - 1) / p.rows);
     p.kept = (int)(q_rows < p.rows ? q_rows : p.rows);
     const int64_t ctas = (int64_t)p.tiles * heads * seqs;
     auto fits = [&]() {
       p.blocks = (int)((all + p.split - 1) / p.split);
       if (p.blocks < 1) p.blocks = 1;
-      const int64_t n = ctas * p.split;
-      // 16 warps, an SM to themselves: few CTAs, or few waves of them (sequences of uneven lengths, whose longest ends last); not many, which
-      // overlap one another, two of 8 warps on an SM.  Three blocks under way for each warp where there is room, else two.
-      const bool wide = p.rows == 8 && p.blocks >= 16 && n < 4 * sms, pairs = p.rows == 8 && p.split == 1 && n > sms;
-      for (int form = wide ? 0 : (pairs ? 1 : 2); form < 3; ++form)
-        for (p.stages = 4; p.stages >= 3; --p.stages) {
-          p.warps = form == 0 ? 16 : 8;
-          p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps, p.stages).total;
-          if (p.smem <= (form == 1 ? kKv4SmemHalf : kKv4SmemMax) && p.blocks <= kKv4Blocks) return true;
-        }
-      return false;
+      const int64_t waves = (ctas * p.split + sms - 1) / sms;
+      for (p.warps = p.rows == 8 && p.blocks >= 40 * waves ? 16 : 8;; p.warps = 8) {
+        p.smem = kv4_smem(d, p.rows, p.kept, page, p.blocks, p.split, p.warps).total;
+        if (p.smem <= kKv4SmemMax && p.blocks <= kKv4Blocks) return true;
+        if (p.warps == 8) return false;
+      }
     };
-    // the largest clusters that all run at once and leave their CTAs work enough; larger ones only where the scores need the room
+    // (larger clusters than said only where the scores need the room)
     p.split = 16;
-    while (p.split > 1 && (room[p.split] < ctas || all < (int64_t)p.split * kKv4Split)) --p.split;
+    while (p.split > 1 && (room[p.split] < ctas || all < 24 || all < 8 * p.split)) --p.split;
     bool ok = fits();
     while (!ok && p.split < 16) {
       ++p.split;

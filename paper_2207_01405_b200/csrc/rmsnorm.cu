@@ -81,9 +81,9 @@ __device__ __forceinline__ void scale_of(const ScaleDev& s, int vec, int word, i
 // passes over what the registers hold, with the sum of squares between them (kDyn: and a third behind the maximum of |z|, where
 // rows get scales of their own).  Many rows are taken eight (int32 streams: four) at a time: the constants of the channels (10 bytes
 // for each, more than an int8 row's own 4) are fetched and prepared once for all of them, and a lane has a row for the root and the division.
-// The int8 form takes about 14 instructions for a value: byte, mad.hi and shift for each of the three requantisations, half a
-// saturating pack twice, a quarter of a dp4a, multiply-add and shift for y; the three mad.hi (4 cycles of a scheduler's multiplier) are
-// what bounds it next to the memory.
+// The int8 form executes 27 instructions for a value (three requantisations of byte, mad.hi, addition and shift, two saturating packs, the
+// squares, the loads and stores), which is what bounds it: 16 383 x 2048 with the residual 41.5 us, 134 MB that the copy rate moves in 20.5; the multiplier
+// is busy 62 % of the time and the ALU 55 %.
 // XI, HI: x, res are int32 (HI = -1: no residual).  kExact: the threads' words are the row's, none is masked.
 template <int XI, int HI, int WPT, int R, bool kDyn, bool kExact>
 __global__ void __launch_bounds__(R == 1 ? 1024 : 512) rmsnorm_kernel(const RmsArgs a) {
@@ -266,8 +266,11 @@ static void launch_rows(ivit_ctx* ctx, const RmsArgs& a) {
   constexpr int R = XI || HI == 1 || kDyn ? 4 : 8;
   const int nwords = a.C >> 2;
   auto threads = [&](int wpt) { return ((nwords + wpt - 1) / wpt + 31) / 32 * 32; };
-  // R rows at a time from two groups for each SM on, up to 4096 channels (registers); below, and beyond, one row, as many threads as there are words.
-  if (a.rows >= 2 * R * ctx->sm_count && nwords <= 1024)
+  // R rows at a time where there is work for it (registers hold up to 4096 channels of them), else one row, a thread for each word (beyond 4096: for
+  // four).  us, R rows / one: int8 600 x 2048 5.3 / 5.1, 800 x 2048 5.3 / 5.8, 9000 x 2048 23 / 44; 1650 x 768 5.0 / 5.0; 3000 x 192 4.9 / 4.6, 6000 x 192 5.1 /
+  // 7.3; 450 x 4096 7.7 / 7.3; int32 250 x 2048 5.6 / 4.1, 330 x 2048 5.6 / 5.8.  Words of a thread, one / four, 64 x 4096: 3.1 / 4.4.
+  const int64_t sms = ctx->sm_count;
+  if (nwords <= 1024 && a.rows >= 3 * sms && (a.rows * nwords >= 275 * R * sms || a.rows >= 3 * R * sms))
     launch_k(nwords % 64 ? rmsnorm_kernel<XI, HI, 2, R, kDyn, false> : rmsnorm_kernel<XI, HI, 2, R, kDyn, true>, (unsigned)((a.rows + R - 1) / R),
              threads(2), 0, ctx->stream, a);
   else if (nwords <= 1024)

@@ -307,6 +307,21 @@ def test_attention_uneven_batches(B):
     assert c.poll_status() == 0
 
 
+@pytest.mark.parametrize("B,hk,G,L,tq", [(40, 4, 2, 4000, 1), (128, 2, 1, 2600, 1), (129, 2, 1, 2600, 1), (40, 2, 14, 300, 1), (40, 2, 9, 700, 1), (1, 2, 8, 13500, 76)])
+def test_attention_forms(B, hk, G, L, tq):
+    """Long uneven batches (16 warps a CTA, longest first), and CTAs of sixteen query rows: some of them never there, clusters of them."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(B + G)
+    d, page = 64, 64
+    lens = rng.integers(0, L + 1, B)
+    lens[0], lens[-1] = L, L
+    np_ = -(-L // page)
+    ref = filled(rng, 250, hk, d, page)
+    attend(c, g, ref, rand_i8(rng, (B * tq, G * hk * d)), G * hk, [tq] * B, lens, rng.integers(0, 250, (B, np_)), weights=True)
+    attend(c, g, ref, rand_i8(rng, (B * tq, G * hk * d)), G * hk, [tq] * B, lens, rng.integers(0, 250, (B, np_)))
+    assert c.poll_status() == 0
+
+
 def test_attention_longest():
     """The longest sequence that the entry point takes."""
     g, c = _g(), _g().ctx()
