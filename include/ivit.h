@@ -498,7 +498,8 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv
  *   kept[b, h, i]   = index of the i-th key that stays, -1 from new_lens[b] on             (int32 [seqs, heads, keep])
  *   row i of dst_table's pages = that key's codes and steps;  weights_out[b, h, i] = its weight, 0 from new_lens[b] to ldw_out
  * In place: dst_table == table and weights_out == weights (with the same leading dimensions).  Else the pages of dst_table hold no
- * source row, and weights_out does not overlap weights.  new_lens may be lens.  sinks + recent <= keep; ldw >= max_len, ldw_out >= keep, ldtable >=
+ * source row, and weights_out does not overlap weights.  No page that rows are moved to is named twice, for two sequences or for one (in place: sequences
+ * share no page).  new_lens may be lens.  sinks + recent <= keep; ldw >= max_len, ldw_out >= keep, ldtable >=
  * ceil(max_len / page), ld_dst >= ceil(min(keep, max_len) / page); max_len and keep <= 2^30.
  * lens above max_len and pages outside the pool are reported as above (such rows are not moved). */
 typedef struct {
