@@ -41,12 +41,16 @@ __device__ __forceinline__ unsigned two_bytes(uint32_t w, int from) {   // bytes
   asm("prmt.b32 %0, %1, %1, %2;" : "=r"(d) : "r"(w), "r"(from ? 0xb3a2 : 0x9180));
   return d;
 }
-// Largest magnitude of eight int8, two 16-bit values at a time: the larger of the maximum and of the minimum turned round.
-__device__ __forceinline__ int top_of(uint2 w) {
-  const unsigned a = two_bytes(w.x, 0), b = two_bytes(w.x, 2), c = two_bytes(w.y, 0), d = two_bytes(w.y, 2);
-  const unsigned hi = max_s16x2(max_s16x2(a, b), max_s16x2(c, d)), lo = min_s16x2(min_s16x2(a, b), min_s16x2(c, d));
-  const int h = max((int)(short)hi, (int)hi >> 16), l = min((int)(short)lo, (int)lo >> 16);
-  return max(h, -l);
+// Largest magnitude of sixteen int8, two 16-bit values at a time: the larger of the maximum and of the minimum turned round.
+__device__ __forceinline__ int top_of(const uint32_t (&w)[4]) {
+  unsigned hi = two_bytes(w[0], 0), lo = hi;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    const unsigned v = two_bytes(w[i >> 1], 2 * (i & 1));
+    hi = max_s16x2(hi, v);
+    lo = min_s16x2(lo, v);
+  }
+  return max(max((int)(short)hi, (int)hi >> 16), -min((int)(short)lo, (int)lo >> 16));
 }
 // ceil(8 top / 7), top <= 128.
 __device__ __forceinline__ int step_of(int top) { return (8 * top + 6) / 7; }
@@ -62,63 +66,58 @@ __device__ __forceinline__ uint32_t codes_of(uint32_t w, int step, unsigned r) {
   return step ? c : 0x08080808u;
 }
 
-// D / 8 lanes take a row of one token and head: eight channels each of K and of V, so that loads and stores of codes are runs of double
-// words; the lanes with a word's low and high halves are 2 apart in K, D / 16 apart in V.  U rows at a time keep loads in flight.  What
-// bounds it is the issue of instructions (20 011 tokens x 8 heads of 64 12.5 us, with four rows at a time 13.0, of those 11.6 without the stores; 31 MB would
-// take 4.8); with four channels a lane, and a division for each step and for the head, it took twice the time.
-template <int D, int U>
+// Codes of sixteen values of this lane and of the lane `other` away, low and high halves of the same bytes: words 0 and 1 of the four go to the
+// lane with the low halves, 2 and 3 to the one with the high ones.
+__device__ __forceinline__ uint2 join(const uint32_t (&c)[4], bool high, int other) {
+  const uint32_t x = __shfl_xor_sync(~0u, high ? c[0] : c[2], other), y = __shfl_xor_sync(~0u, high ? c[1] : c[3], other);
+  return high ? make_uint2(x | c[2] << 4, y | c[3] << 4) : make_uint2(c[0] | x << 4, c[1] | y << 4);
+}
+
+// D / 16 lanes take a row of one token and head: sixteen channels each of K and of V.  The lanes with a byte's low and high halves are
+// neighbours in K, D / 32 apart in V.  What bounds it is the issue of instructions: 20 011 tokens x 8 heads of 64 9.7 us (31 MB would take 4.8), of 128 17.6;
+// with eight channels a lane, and so twice the reductions, steps and addresses, 12.5 and 22.9.  Two rows for each lane were no gain (9.7 and 16.6, a call of
+// 48 tokens 1.9 -> 2.5).
+template <int D>
 __global__ void __launch_bounds__(256) kv4_append_kernel(const Cache c, const int8_t* __restrict__ K, int64_t ldk, const int8_t* __restrict__ V,
                                                          int64_t ldv, const int64_t* __restrict__ slots, unsigned rows, Kv4Div by_heads, int* status) {
-  constexpr int L = D / 8, kPer = 256 / L;       // lanes of a row, rows of a CTA
+  constexpr int L = D / 16;                      // lanes of a row
   __shared__ unsigned recip[256];
   if (threadIdx.x < 148) recip[threadIdx.x] = threadIdx.x ? (1u << 23) / threadIdx.x + 1u : 0u;
   pdl_wait();
   pdl_trigger();
   const int l = threadIdx.x & (L - 1);
-  const unsigned r0 = blockIdx.x * (kPer * U) + threadIdx.x / L;
-  uint2 k[U], v[U];
-  long long slot[U];
-  int h[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const unsigned r = min(r0 + u * kPer, rows - 1), t = (unsigned)by_heads.div((int)r);
-    h[u] = (int)(r - t * by_heads.d);
-    k[u] = *reinterpret_cast<const uint2*>(K + t * ldk + (h[u] * D + 8 * l));
-    v[u] = *reinterpret_cast<const uint2*>(V + t * ldv + (h[u] * D + 8 * l));
-    slot[u] = r0 + u * kPer < rows ? slots[t] : -1;
-  }
+  const unsigned mine = blockIdx.x * (256 / L) + threadIdx.x / L, r = min(mine, rows - 1), t = (unsigned)by_heads.div((int)r);
+  const int h = (int)(r - t * by_heads.d);
+  const uint4 k = *reinterpret_cast<const uint4*>(K + t * ldk + (h * D + 16 * l)), v = *reinterpret_cast<const uint4*>(V + t * ldv + (h * D + 16 * l));
+  const long long slot = mine < rows ? slots[t] : -1;
   __syncthreads();
-  const int kstep = kv4_kstep(D, c.page, 0), vcode = kv4_vcode(D, c.page, 0), vstep = kv4_vstep(D, c.page, 0);
+  uint32_t kw[4] = {k.x, k.y, k.z, k.w}, vw[4] = {v.x, v.y, v.z, v.w};
+  int kt = top_of(kw), vt = top_of(vw);
+  kt = max(kt, __shfl_xor_sync(~0u, kt, 1));
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    int kt = top_of(k[u]), vt = top_of(v[u]);
+  for (int o = 1; o < L; o <<= 1) vt = max(vt, __shfl_xor_sync(~0u, vt, o));
+  const int ks = step_of(kt), vs = step_of(vt);
+  const unsigned kr = recip[ks], vr = recip[vs];
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) kt = max(kt, __shfl_xor_sync(~0u, kt, o));
-#pragma unroll
-    for (int o = 1; o < L; o <<= 1) vt = max(vt, __shfl_xor_sync(~0u, vt, o));
-    const int ks = step_of(kt), vs = step_of(vt);
-    const unsigned kr = recip[ks], vr = recip[vs];
-    uint32_t k0 = codes_of(k[u].x, ks, kr), k1 = codes_of(k[u].y, ks, kr), v0 = codes_of(v[u].x, vs, vr), v1 = codes_of(v[u].y, vs, vr);
-    k0 |= __shfl_down_sync(~0u, k0, 2) << 4;
-    k1 |= __shfl_down_sync(~0u, k1, 2) << 4;
-    v0 |= __shfl_down_sync(~0u, v0, L / 2) << 4;
-    v1 |= __shfl_down_sync(~0u, v1, L / 2) << 4;
-    if (slot[u] < 0) continue;
-    if (slot[u] >> c.page_log >= c.pages) {
-      if (l == 0) report(status, IVIT_ERR_RANGE);
-      continue;
-    }
-    uint8_t* p = c.block((int)(slot[u] >> c.page_log), h[u]);
-    const int o = (int)slot[u] & (c.page - 1), g = l >> 2;
-    if ((l & 2) == 0) {                          // words 2 (l & 1) and the next one of group g
-      uint32_t* dst = reinterpret_cast<uint32_t*>(p + o * (D / 2)) + D / 32 * (2 * (l & 1)) + g;
-      dst[0] = k0;
-      dst[D / 32] = k1;
-    }
-    if (l < L / 2) *reinterpret_cast<uint2*>(p + vcode + o * (D / 2) + 8 * l) = make_uint2(v0, v1);
-    if ((l & 3) == 0) p[kstep + o * (D / 32) + g] = (uint8_t)ks;
-    if (l == 1) p[vstep + o] = (uint8_t)vs;
+  for (int i = 0; i < 4; ++i) {
+    kw[i] = codes_of(kw[i], ks, kr);
+    vw[i] = codes_of(vw[i], vs, vr);
   }
+  const bool k_high = l & 1, v_high = l >= L / 2;
+  const uint2 kc = join(kw, k_high, 1), vc = join(vw, v_high, L / 2);
+  if (slot < 0) return;
+  if (slot >> c.page_log >= c.pages) {
+    if (l == 0) report(status, IVIT_ERR_RANGE);
+    return;
+  }
+  uint8_t* p = c.block((int)(slot >> c.page_log), h);
+  const int o = (int)slot & (c.page - 1), g = l >> 1;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(p + kv4_kcode(D, c.page, o)) + D / 32 * (k_high ? 2 : 0) + g;   // words 0 and 1, or 2 and 3, of group g
+  dst[0] = kc.x;
+  dst[D / 32] = kc.y;
+  *reinterpret_cast<uint2*>(p + kv4_vcode(D, c.page, o) + 16 * (l & (L / 2 - 1)) + (v_high ? 8 : 0)) = vc;
+  if (!k_high) p[kv4_kstep(D, c.page, o) + g] = (uint8_t)ks;
+  if (l == 1) p[kv4_vstep(D, c.page, o)] = (uint8_t)vs;
 }
 
 int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
@@ -126,14 +125,11 @@ int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* 
   if (tokens == 0) return IVIT_OK;
   LaunchScope ls(ctx, KIND_MOVE, (double)tokens * cache->heads * (3 * cache->d + cache->d / 32 + 1));
   const unsigned rows = (unsigned)(tokens * cache->heads);
-  // One row at a time up to 400 for each SM, then several, whose loads are all under way (us, one / several): 5000 tokens x 8 heads of 64 4.4 / 5.8, of 128
-  // 7.4 / 7.8; 20011 tokens 13.2 / 12.5 and 24.9 / 22.9 (of 64 with four 13.0, of 128 with two 24.0).
-  const bool many = rows >= 400u * (unsigned)ctx->sm_count;
   auto go = [&](auto k, unsigned per) {
     launch_k(k, (rows + per - 1) / per, 256, 0, ctx->stream, to_dev(cache), K, ldk, V, ldv, slots, rows, kv4_div((unsigned)cache->heads), ctx->status_dev);
   };
-  if (cache->d == 128) many ? go(kv4_append_kernel<128, 4>, 64) : go(kv4_append_kernel<128, 1>, 16);
-  else many ? go(kv4_append_kernel<64, 2>, 64) : go(kv4_append_kernel<64, 1>, 32);
+  if (cache->d == 128) go(kv4_append_kernel<128>, 32);
+  else go(kv4_append_kernel<64>, 64);
   return ls.done();
 }
 
