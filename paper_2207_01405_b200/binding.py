@@ -430,14 +430,23 @@ class Context:
                                      out.data_ptr(), _ld(out), rows, Cc), "ivit_layernorm")
         return out
 
-    def _want(self, what: str, dtype, dim: int, t: torch.Tensor):
-        """Refuses a tensor that the C side would read as something else; returns its shape and leading dimension."""
+    def _want(self, what: str, dtype, t: torch.Tensor):
+        """Refuses a tensor of rows that the C side would read as something else; returns its shape and leading dimension."""
         shape, strides = t.shape, t.stride()
-        if t.dtype is not dtype or len(shape) != dim or t.get_device() != self.index or (strides[-1] != 1 and shape[-1] > 1):
-            raise ValueError(f"{what}: want a {dim}-d {dtype} tensor on {self.device} with contiguous rows, got {tuple(shape)} "
+        if t.dtype is not dtype or t.get_device() != self.index or len(shape) != 2 or (strides[1] != 1 and shape[1] > 1):
+            raise ValueError(f"{what}: want a 2-d {dtype} tensor on {self.device} with contiguous rows, got {tuple(shape)} "
                              f"{t.dtype} on {t.device}, strides {strides}")
-        # (one row, or none, has no use for a leading dimension, and its stride may be anything)
-        return shape, strides[0] if shape[0] > 1 else (shape[-1] + 15) // 16 * 16
+        if shape[0] > 1:
+            return shape, strides[0]
+        return shape, (shape[1] + 15) & -16   # (one row, or none, has no use for a leading dimension, and its stride may be anything)
+
+    def _whole(self, what: str, dtype, dim: int, t: torch.Tensor):
+        """The same for a tensor without gaps (any of one dimension that has no stride); returns its shape."""
+        shape = t.shape
+        if t.dtype is not dtype or len(shape) != dim or t.get_device() != self.index or not t.is_contiguous():
+            raise ValueError(f"{what}: want a contiguous {dim}-d {dtype} tensor on {self.device}, got {tuple(shape)} {t.dtype} on {t.device}, "
+                             f"strides {t.stride()}")
+        return shape
 
     def _fields(self, scale: DevScale, channels: int):
         """A scale as the call descriptions hold it; its arrays have an entry for each channel, on the context's device."""
@@ -450,23 +459,23 @@ class Context:
         """ivit_rmsnorm: x (int8 or int32) [rows, C], with res added first (its sum goes to sum_out, which may be res); returns int8 rows.
         row_max (int32 [rows]): every row gets a scale of its own, written there."""
         x8 = x.dtype is torch.int8
-        shape, ldx = self._want("x", torch.int8 if x8 else torch.int32, 2, x)
+        shape, ldx = self._want("x", torch.int8 if x8 else torch.int32, x)
         rows, Cc = shape
         if out is None:
             out = torch.empty((rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
-        o_shape, ldo = self._want("out", torch.int8, 2, out)
+        o_shape, ldo = self._want("out", torch.int8, out)
         if o_shape != shape:
             raise ValueError("out has the shape of x")
         r8, ldr, lds, p_res, p_sum, p_max, xs, rs = False, 0, 0, 0, 0, 0, _UNIT, _UNIT
         if res is not None:
             r8 = res.dtype is torch.int8
             dt = torch.int8 if r8 else torch.int32
-            r_shape, ldr = self._want("res", dt, 2, res)
+            r_shape, ldr = self._want("res", dt, res)
             if x_scale is None or res_scale is None or r_shape != shape:
                 raise ValueError("res has the shape of x, and comes with x_scale and res_scale")
             xs, rs, p_res = self._fields(x_scale, Cc), res_scale.fields, res.data_ptr()
             if sum_out is not None:
-                s_shape, lds = self._want("sum_out", dt, 2, sum_out)
+                s_shape, lds = self._want("sum_out", dt, sum_out)
                 if s_shape != shape:
                     raise ValueError("sum_out has the shape of x")
                 p_sum = sum_out.data_ptr()
@@ -474,7 +483,7 @@ class Context:
             raise ValueError("sum_out comes with res")
         gs = self._fields(gamma_scale, Cc)
         if row_max is not None:
-            if self._want("row_max", torch.int32, 1, row_max)[0][0] != rows:
+            if self._whole("row_max", torch.int32, 1, row_max)[0] != rows:
                 raise ValueError("row_max has an entry for each row")
             p_max = row_max.data_ptr()
         rc = self.lib.ivit_rmsnorm(self.h, _RMSNORM.pack(x.data_ptr(), ldx, p_res, ldr, p_sum, lds, out.data_ptr(), ldo, p_max, rows, Cc, *xs, *rs,
@@ -487,10 +496,10 @@ class Context:
 
     def kv4_append(self, cache: Kv4Cache, k, v, slots):
         """ivit_kv4_append: int8 rows [tokens, heads d] into the rows of the pool that slots (int64) names; negative: left out."""
-        shape, ldk = self._want("k", torch.int8, 2, k)
-        v_shape, ldv = self._want("v", torch.int8, 2, v)
+        shape, ldk = self._want("k", torch.int8, k)
+        v_shape, ldv = self._want("v", torch.int8, v)
         n, width = shape
-        if v_shape != shape or self._want("slots", torch.int64, 1, slots)[0][0] != n or width != cache.width or cache.index != self.index:
+        if v_shape != shape or self._whole("slots", torch.int64, 1, slots)[0] != n or width != cache.width or cache.index != self.index:
             raise ValueError("k and v are [tokens, heads d], slots [tokens], the pool is on the context's device")
         rc = self.lib.ivit_kv4_append(self.h, cache.ref, k.data_ptr(), ldk, v.data_ptr(), ldv, slots.data_ptr(), n)
         if rc:
@@ -500,21 +509,21 @@ class Context:
                       out=None, weights=None):
         """ivit_kv4_attention: query rows [tokens, query heads d] of len(lens) sequences over the cache; returns int8 rows of the same
         shape (a new one starts as zeros, rows of no sequence keep what out held).  weights (int64 [seqs, heads, >= max_len]) is added to."""
-        shape, ldq = self._want("q", torch.int8, 2, q)
+        shape, ldq = self._want("q", torch.int8, q)
         n, width = shape
         if out is None:
             out = torch.zeros((n, width), dtype=torch.int8, device=q.device)
-        o_shape, ldo = self._want("out", torch.int8, 2, out)
-        (seqs,), _ = self._want("lens", torch.int32, 1, lens)
-        (t_rows, t_cols), ldt = self._want("table", torch.int32, 2, table)
-        if (o_shape != shape or self._want("q_start", torch.int32, 1, q_start)[0][0] != seqs + 1 or t_rows != seqs or width % cache.d or
+        o_shape, ldo = self._want("out", torch.int8, out)
+        seqs = self._whole("lens", torch.int32, 1, lens)[0]
+        (t_rows, t_cols), ldt = self._want("table", torch.int32, table)
+        if (o_shape != shape or self._whole("q_start", torch.int32, 1, q_start)[0] != seqs + 1 or t_rows != seqs or width % cache.d or
                 t_cols * cache.page < max_len or cache.index != self.index):
             raise ValueError("q and out are [tokens, query heads d], q_start [seqs + 1], table [seqs, pages for max_len keys], the pool is on the "
                              "context's device")
         p_w, ldw = 0, 0
         if weights is not None:
-            (w_seqs, w_heads, ldw), _ = self._want("weights", torch.int64, 3, weights)
-            if w_seqs != seqs or w_heads != cache.heads or not weights.is_contiguous():
+            w_seqs, w_heads, ldw = self._whole("weights", torch.int64, 3, weights)
+            if w_seqs != seqs or w_heads != cache.heads:
                 raise ValueError("weights is a contiguous [seqs, heads, keys]")
             p_w = weights.data_ptr()
         rc = self.lib.ivit_kv4_attention(self.h, cache.ref, _ATTENTION.pack(
@@ -528,18 +537,18 @@ class Context:
                   weights_out=None, kept=None, new_lens=None):
         """ivit_kv4_evict: at most `keep` keys of each sequence and head stay; in place unless dst_table and weights_out are given.
         Returns (kept [seqs, heads, keep], new_lens [seqs])."""
-        (seqs,), _ = self._want("lens", torch.int32, 1, lens)
+        seqs = self._whole("lens", torch.int32, 1, lens)[0]
         dst_table = table if dst_table is None else dst_table
         weights_out = weights if weights_out is None else weights_out
         kept = torch.empty((seqs, cache.heads, keep), dtype=torch.int32, device=self.device) if kept is None else kept
         new_lens = torch.empty_like(lens) if new_lens is None else new_lens
-        (ws, wh, ldw), _ = self._want("weights", torch.int64, 3, weights)
-        (os_, oh, ldo), _ = self._want("weights_out", torch.int64, 3, weights_out)
-        (ks, kh, kk), _ = self._want("kept", torch.int32, 3, kept)
-        (ts, tc), ldt = self._want("table", torch.int32, 2, table)
-        (ds, dc), ldd = self._want("dst_table", torch.int32, 2, dst_table)
-        if not (ws == os_ == ks == ts == ds == seqs == self._want("new_lens", torch.int32, 1, new_lens)[0][0] and wh == oh == kh == cache.heads and
-                weights.is_contiguous() and weights_out.is_contiguous() and kept.is_contiguous() and kk == keep and cache.index == self.index):
+        ws, wh, ldw = self._whole("weights", torch.int64, 3, weights)
+        os_, oh, ldo = (ws, wh, ldw) if weights_out is weights else self._whole("weights_out", torch.int64, 3, weights_out)
+        ks, kh, kk = self._whole("kept", torch.int32, 3, kept)
+        (ts, tc), ldt = self._want("table", torch.int32, table)
+        (ds, dc), ldd = ((ts, tc), ldt) if dst_table is table else self._want("dst_table", torch.int32, dst_table)
+        if not (ws == os_ == ks == ts == ds == seqs == self._whole("new_lens", torch.int32, 1, new_lens)[0] and wh == oh == kh == cache.heads and
+                kk == keep and cache.index == self.index):
             raise ValueError("lens and new_lens are [seqs], weights and weights_out contiguous [seqs, heads, keys], kept contiguous "
                              "[seqs, heads, keep], the tables [seqs, pages], the pool is on the context's device")
         if tc * cache.page < max_len or dc * cache.page < min(keep, max_len):
