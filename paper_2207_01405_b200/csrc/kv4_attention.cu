@@ -102,7 +102,7 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
 // cluster's CTAs meet in distributed shared memory: one launch, no workspace, and integer sums, so that the order changes nothing.
 //
 // What bounds it, decoding: 37 sequences of up to 7000 keys, 32 / 8 heads of 128, 139 MB, 33 us (4.2 TB/s, 0.64 of the copy rate): about
-// 160 clocks of an SM for 32 keys, in which no unit is busy half of the time (issue 48 % of all cycles, shared memory 37 %, ALU 35 %), and 8000 clocks
+// 160 clocks of an SM for 32 keys, in which no unit is busy half of the time (issue 46 % of all cycles, shared memory 38 %, ALU 33 %), and 8000 clocks
 // around a CTA's keys (set-up, exponentials, exchange, sums, quotients).  Many query rows (16 a CTA): registers hold the sums, two warps
 // for a scheduler do not cover one another's latencies: issue 42 %.
 template <int D, int RN, int W, bool kWeights>
