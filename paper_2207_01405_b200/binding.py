@@ -338,7 +338,7 @@ class Context:
 
     def isqrt_range(self, n0: int, count: int) -> torch.Tensor:
         """ivit_isqrt_range: the I-LayerNorm kernels' integer square root of n0 .. n0 + count - 1 (uint16 on device)."""
-        out = torch.empty(count, dtype=torch.uint16, device=self.device)
+        out = self._own(torch.empty, count, dtype=torch.uint16, device=self.device)
         _chk(self.lib.ivit_isqrt_range(self.h, n0, count, out.data_ptr()), "ivit_isqrt_range")
         return out
 
@@ -360,14 +360,25 @@ class Context:
             out.append((self.lib.ivit_kernel_kind_name(kind.value).decode(), ms.value, work.value))
         return out
 
-    # ---- operators (device tensors in, device tensors out) ----
+    # ---- operators (device tensors in, device tensors out; a tensor that a call makes itself belongs to the context's stream) ----
+
+    def _own(self, make, *args, **kw):
+        """make(...), a new tensor, in memory of the context's stream: a block that another stream gave back may still be read there, and what fills the
+        tensor has to come before the call that writes it.  The current stream, where the caller may use it, is told to the allocator: its work counts
+        before the memory is given out again.  (torch.cuda.current_stream() would take 2.2 us, the first line takes 0.07.)"""
+        if torch._C._cuda_getCurrentRawStream(self.index) == self.stream.cuda_stream:
+            return make(*args, **kw)
+        with torch.cuda.stream(self.stream):
+            t = make(*args, **kw)
+        t.record_stream(torch.cuda.current_stream(self.device))
+        return t
 
     def linear(self, A, W, bias, scale: DevScale, res=None, res_scale: DevScale = None, out=None, out_dtype=I8,
                res_rows=None, out_group_rows=0, out_group_stride=0):
         M, K = A.shape
         N = W.shape[0]
         if out is None:
-            out = torch.empty((M, N), dtype=torch.int8 if out_dtype == I8 else torch.int32, device=A.device)
+            out = self._own(torch.empty, (M, N), dtype=torch.int8 if out_dtype == I8 else torch.int32, device=A.device)
         rs = res_scale.c if res_scale is not None else CScale(None, None, 1, 1)
         _chk(self.lib.ivit_linear(self.h, A.data_ptr(), _ld(A), W.data_ptr(), _ld(W), _ptr(bias), scale.c,
                                   _ptr(res), _ld(res) if res is not None else 0,
@@ -381,7 +392,7 @@ class Context:
         Nb = B.shape[1] if transB else B.shape[2]
         if out is None:
             ldc = (Nb + 15) // 16 * 16
-            out = torch.zeros((nb, Ma, ldc), dtype=torch.int8, device=A.device)[:, :, :Nb]
+            out = self._own(torch.zeros, (nb, Ma, ldc), dtype=torch.int8, device=A.device)[:, :, :Nb]
         _chk(self.lib.ivit_matmul(self.h, A.data_ptr(), A.stride(1), 0, A.stride(0), B.data_ptr(), B.stride(1), 0,
                                   B.stride(0), 1 if transB else 0, _ptr(bias32),
                                   bias32.stride(1) if bias32 is not None else 0,
@@ -393,7 +404,7 @@ class Context:
         rows, d = x.shape
         if out is None:
             ldo = (d + 15) // 16 * 16
-            out = torch.empty((rows, ldo), dtype=torch.int8, device=x.device)[:, :d]
+            out = self._own(torch.empty, (rows, ldo), dtype=torch.int8, device=x.device)[:, :d]
         pre_c = pre.c if pre is not None else CScale(None, None, 1, 1)
         _chk(self.lib.ivit_shiftmax(self.h, x.data_ptr(), I8 if x.dtype == torch.int8 else I32, _ld(x), _ptr(bias32),
                                     _ld(bias32) if bias32 is not None else 0,
@@ -406,7 +417,7 @@ class Context:
         rows, d = x.shape
         if out is None:
             ldo = (d + 15) // 16 * 16
-            out = torch.empty((rows, ldo), dtype=torch.int8, device=x.device)[:, :d]
+            out = self._own(torch.empty, (rows, ldo), dtype=torch.int8, device=x.device)[:, :d]
         _chk(self.lib.ivit_shiftmax_direct(self.h, x.data_ptr(), _ld(x), _cexp(p), out.data_ptr(), _ld(out), rows, d),
              "ivit_shiftmax_direct")
         return out
@@ -415,7 +426,7 @@ class Context:
         """static_max=True: ivit_shiftgelu_static (I_max fixed at I_p(127), element-wise; not the paper's function)."""
         rows, cols = x.shape
         if out is None:
-            out = torch.empty_like(x)
+            out = self._own(torch.empty_like, x)
         fn = self.lib.ivit_shiftgelu_static if static_max else self.lib.ivit_shiftgelu
         _chk(fn(self.h, x.data_ptr(), _ld(x), _cexp(p), post.c, out.data_ptr(), _ld(out), rows, cols), "ivit_shiftgelu")
         return out
@@ -424,7 +435,7 @@ class Context:
         r, Cc = x.shape
         rows = r if rows is None else rows
         if out is None:
-            out = torch.empty((rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
+            out = self._own(torch.empty, (rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
         _chk(self.lib.ivit_layernorm(self.h, x.data_ptr(), I8 if x.dtype == torch.int8 else I32,
                                      _ld(x) if ldin is None else ldin, gamma_scale.c, _ptr(beta), M_ln,
                                      out.data_ptr(), _ld(out), rows, Cc), "ivit_layernorm")
@@ -462,7 +473,7 @@ class Context:
         shape, ldx = self._want("x", torch.int8 if x8 else torch.int32, x)
         rows, Cc = shape
         if out is None:
-            out = torch.empty((rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
+            out = self._own(torch.empty, (rows, (Cc + 15) // 16 * 16), dtype=torch.int8, device=x.device)[:, :Cc]
         o_shape, ldo = self._want("out", torch.int8, out)
         if o_shape != shape:
             raise ValueError("out has the shape of x")
@@ -512,7 +523,7 @@ class Context:
         shape, ldq = self._want("q", torch.int8, q)
         n, width = shape
         if out is None:
-            out = torch.zeros((n, width), dtype=torch.int8, device=q.device)
+            out = self._own(torch.zeros, (n, width), dtype=torch.int8, device=q.device)
         o_shape, ldo = self._want("out", torch.int8, out)
         seqs = self._whole("lens", torch.int32, 1, lens)[0]
         (t_rows, t_cols), ldt = self._want("table", torch.int32, table)
@@ -540,8 +551,8 @@ class Context:
         seqs = self._whole("lens", torch.int32, 1, lens)[0]
         dst_table = table if dst_table is None else dst_table
         weights_out = weights if weights_out is None else weights_out
-        kept = torch.empty((seqs, cache.heads, keep), dtype=torch.int32, device=self.device) if kept is None else kept
-        new_lens = torch.empty_like(lens) if new_lens is None else new_lens
+        kept = self._own(torch.empty, (seqs, cache.heads, keep), dtype=torch.int32, device=self.device) if kept is None else kept
+        new_lens = self._own(torch.empty_like, lens) if new_lens is None else new_lens
         ws, wh, ldw = self._whole("weights", torch.int64, 3, weights)
         os_, oh, ldo = (ws, wh, ldw) if weights_out is weights else self._whole("weights_out", torch.int64, 3, weights_out)
         ks, kh, kk = self._whole("kept", torch.int32, 3, kept)
@@ -562,14 +573,14 @@ class Context:
 
     def patchify(self, img, P, window=0):
         B, Cc, Hi, Wi = img.shape
-        out = torch.empty((B * (Hi // P) * (Wi // P), Cc * P * P), dtype=torch.int8, device=img.device)
+        out = self._own(torch.empty, (B * (Hi // P) * (Wi // P), Cc * P * P), dtype=torch.int8, device=img.device)
         _chk(self.lib.ivit_patchify(self.h, img.data_ptr(), B, Cc, Hi, Wi, P, window, out.data_ptr(), _ld(out)),
              "ivit_patchify")
         return out
 
     def gather_rows(self, src, index, width=None):
         width = width or src.shape[1]
-        dst = torch.empty((index.numel(), width), dtype=torch.int8, device=src.device)
+        dst = self._own(torch.empty, (index.numel(), width), dtype=torch.int8, device=src.device)
         _chk(self.lib.ivit_gather_rows(self.h, src.data_ptr(), _ld(src), index.data_ptr(), index.numel(), width,
                                        dst.data_ptr(), _ld(dst)), "ivit_gather_rows")
         return dst
@@ -581,7 +592,7 @@ class Context:
 
     def token_mean(self, x, T, scale: DevScale):
         groups, Cc = x.shape[0] // T, x.shape[1]
-        out = torch.empty((groups, Cc), dtype=torch.int8, device=x.device)
+        out = self._own(torch.empty, (groups, Cc), dtype=torch.int8, device=x.device)
         _chk(self.lib.ivit_token_mean(self.h, x.data_ptr(), _ld(x), groups, T, Cc, scale.c, out.data_ptr(), _ld(out)),
              "ivit_token_mean")
         return out
@@ -590,8 +601,8 @@ class Context:
 
     def block_forward(self, blk: "DeviceBlock", X, Y=None, workspace=None):
         if Y is None:
-            Y = torch.empty_like(X)
-        ws = workspace if workspace is not None else blk.workspace()
+            Y = self._own(torch.empty_like, X)
+        ws = workspace if workspace is not None else self._own(blk.workspace)
         _chk(self.lib.ivit_block_forward(self.h, C.byref(blk.c), X.data_ptr(), Y.data_ptr(), ws.data_ptr(), ws.numel()),
              "ivit_block_forward")
         return Y
@@ -599,15 +610,15 @@ class Context:
     def block_forward_static(self, blk: "DeviceBlock", X, Y=None):
         """ivit_block_forward_static: same block, scratch taken from the library's fixed device array."""
         if Y is None:
-            Y = torch.empty_like(X)
+            Y = self._own(torch.empty_like, X)
         _chk(self.lib.ivit_block_forward_static(self.h, C.byref(blk.c), X.data_ptr(), Y.data_ptr()),
              "ivit_block_forward_static")
         return Y
 
     def attention(self, blk: "DeviceBlock", QKV, O=None, workspace=None):
         if O is None:
-            O = torch.empty((QKV.shape[0], blk.c.D), dtype=torch.int8, device=QKV.device)
-        ws = workspace if workspace is not None else blk.workspace()
+            O = self._own(torch.empty, (QKV.shape[0], blk.c.D), dtype=torch.int8, device=QKV.device)
+        ws = workspace if workspace is not None else self._own(blk.workspace)
         _chk(self.lib.ivit_attention(self.h, C.byref(blk.c), QKV.data_ptr(), O.data_ptr(), ws.data_ptr(), ws.numel()),
              "ivit_attention")
         return O
@@ -616,8 +627,8 @@ class Context:
         """ivit_vit_forward; with `tokens` ([B*T, D] int8) ivit_vit_forward_tokens, which also hands back the
         output of the last encoder block."""
         if logits is None:
-            logits = torch.empty((model.c.B, model.c.classes), dtype=torch.int32, device=image.device)
-        ws = workspace if workspace is not None else model.workspace()
+            logits = self._own(torch.empty, (model.c.B, model.c.classes), dtype=torch.int32, device=image.device)
+        ws = workspace if workspace is not None else self._own(model.workspace)
         if tokens is None:
             _chk(self.lib.ivit_vit_forward(self.h, C.byref(model.c), image.data_ptr(), logits.data_ptr(), ws.data_ptr(),
                                            ws.numel()), "ivit_vit_forward")
@@ -789,9 +800,9 @@ def swin_forward(ctx: Context, m: DeviceSwin, image: torch.Tensor, return_tokens
     """ivit_swin_forward: image [B,3,img,img] int8 on the device -> int32 logits [B, classes]; with return_tokens
     also the output of the last block ([B * tokens, C] int8, window-major rows)."""
     if logits is None:
-        logits = torch.empty((m.c.B, m.c.classes), dtype=torch.int32, device=image.device)
-    tokens = torch.empty(m.tokens_shape, dtype=torch.int8, device=image.device) if return_tokens else None
-    ws = workspace if workspace is not None else m.workspace()
+        logits = ctx._own(torch.empty, (m.c.B, m.c.classes), dtype=torch.int32, device=image.device)
+    tokens = ctx._own(torch.empty, m.tokens_shape, dtype=torch.int8, device=image.device) if return_tokens else None
+    ws = workspace if workspace is not None else ctx._own(m.workspace)
     _chk(ctx.lib.ivit_swin_forward(ctx.h, C.byref(m.c), image.data_ptr(), logits.data_ptr(), _ptr(tokens), ws.data_ptr(),
                                    ws.numel()), "ivit_swin_forward")
     return (logits, tokens) if return_tokens else logits

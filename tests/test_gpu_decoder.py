@@ -703,3 +703,76 @@ def test_the_binding_refuses_what_the_library_would_misread():
     assert c.launch_count() == before
     torch.cuda.synchronize()
     assert c.poll_status() == 0
+
+
+def _calls_that_make_their_outputs(c, g):
+    """name -> (a call that is given no output, its first output's bytes), on inputs that stay as they are."""
+    rng = np.random.default_rng(41)
+    B, one = g.binding, g.binding.DevScale.of(*dyadic(0.01))
+    rows, d, page, hk, L = 1500, 64, 32, 2, 300
+    x, w = cuda(rand_i8(rng, (rows, 1024))), cuda(rand_i8(rng, (1024, 1024)))
+    ref = filled(rng, 20, hk, d, page)
+    cache = B.Kv4Cache(cuda(ref.to_bytes()), d, page)
+    q, qs, lens = cuda(rand_i8(rng, (rows, 4 * d))), cuda(np.array([0, 100], np.int32)), cuda(np.array([L], np.int32))
+    table, dst = cuda(np.arange(10, dtype=np.int32)[None]), cuda(np.arange(10, 20, dtype=np.int32)[None])
+    weights, wo = cuda(rng.integers(0, 10 ** 6, (1, hk, L))), torch.zeros((1, hk, 320), dtype=torch.int64, device="cuda")
+    qk, pv, gelu = B.DevScale.of(*dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40))), B.DevScale.of(*dyadic(1 / 128)), ExpParams(17, 15)
+    nb = cuda(rand_i8(rng, (9, 90, 64)))
+    index = cuda(rng.integers(0, rows, 700).astype(np.int32))
+    return {
+        "rmsnorm": (lambda: c.rmsnorm(x, one), rows * 1024),
+        "kv4_attention": (lambda: c.kv4_attention(cache, q, qs, lens, table, qk, gelu, pv, 100, L), rows * 4 * d),
+        "kv4_evict": (lambda: c.kv4_evict(cache, weights, lens, table, 200, 4, 16, L, dst_table=dst, weights_out=wo)[0], 4 * hk * 200),
+        "linear": (lambda: c.linear(x, w, None, one), rows * 1024),
+        "matmul": (lambda: c.matmul(nb, nb, True, one), 9 * 90 * 96),
+        "layernorm": (lambda: c.layernorm(x, one, None), rows * 1024),
+        "gather_rows": (lambda: c.gather_rows(x, index), 700 * 1024),
+        "token_mean": (lambda: c.token_mean(x, 3, one), 500 * 1024),
+    }
+
+
+@pytest.mark.parametrize("name", ["rmsnorm", "kv4_attention", "kv4_evict", "linear", "matmul", "layernorm", "gather_rows", "token_mean"])
+def test_outputs_that_a_call_makes_belong_to_the_context_s_stream(name):
+    """A context with a stream of its own, while another one is current and busy: what the call does to a new output may not wait there (zeros that
+    land behind the kernel), and its memory may not be a block that the current stream has still to read."""
+    g = _g()
+    side = torch.cuda.Stream()
+    c = g.binding.Context(0, side)
+    call, nbytes = _calls_that_make_their_outputs(c, g)[name]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        want = [g.host(call()) for _ in range(2)][1]
+    torch.cuda.synchronize()
+    torch.cuda._sleep(40_000_000)                                   # (20 ms)
+    got = call()
+    torch.cuda.synchronize()
+    g.assert_equal(g.host(got), want, "behind a busy stream")
+    del got
+    for _ in range(3):
+        old = torch.full((nbytes,), 77, dtype=torch.int8, device="cuda")
+        copy = torch.empty_like(old)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(40_000_000)
+        copy.copy_(old)
+        del old
+        got = call()
+        torch.cuda.synchronize()
+        assert (copy == 77).all()
+        g.assert_equal(g.host(got), want, "beside a busy stream")
+        del got
+    # what the current stream still reads of an output that the caller has dropped is not the next call's output
+    side.synchronize()
+    for _ in range(3):
+        got = call()
+        torch.cuda.current_stream().wait_stream(side)
+        copy = torch.empty_like(got)
+        torch.cuda._sleep(40_000_000)
+        copy.copy_(got)
+        got = None
+        with torch.cuda.stream(side):
+            junk = [torch.full((nbytes,), 77, dtype=torch.int8, device="cuda") for _ in range(2)]
+        torch.cuda.synchronize()
+        g.assert_equal(g.host(copy), want, "read by a busy stream")
+        del junk
+    assert c.poll_status() == 0
+    c.close()
