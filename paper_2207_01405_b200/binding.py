@@ -558,6 +558,8 @@ class Context:
         ks, kh, kk = self._whole("kept", torch.int32, 3, kept)
         (ts, tc), ldt = self._want("table", torch.int32, table)
         (ds, dc), ldd = ((ts, tc), ldt) if dst_table is table else self._want("dst_table", torch.int32, dst_table)
+        if seqs == 1 and dst_table.data_ptr() == table.data_ptr():
+            ldt = ldd = max(ldt, ldd)   # (columns of one table: a single row of it has no leading dimension of its own, in place wants the same for both)
         if not (ws == os_ == ks == ts == ds == seqs == self._whole("new_lens", torch.int32, 1, new_lens)[0] and wh == oh == kh == cache.heads and
                 kk == keep and cache.index == self.index):
             raise ValueError("lens and new_lens are [seqs], weights and weights_out contiguous [seqs, heads, keys], kept contiguous "

@@ -776,3 +776,23 @@ def test_outputs_that_a_call_makes_belong_to_the_context_s_stream(name):
         del junk
     assert c.poll_status() == 0
     c.close()
+
+
+@pytest.mark.parametrize("B", [1, 2])
+@pytest.mark.parametrize("cols,dst_cols", [(40, 5), (5, 40), (40, 40)])
+def test_evict_in_place_by_columns_of_one_table(B, cols, dst_cols):
+    """The table's first columns name where the rows go: in place, whatever the columns and however few the sequences."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(43)
+    L, keep, page, hk = 150, 70, 32, 2
+    ref = filled(rng, B * 5 + 1, hk, 64, page)
+    table = np.full((B, 40), -1, np.int32)
+    table[:, :5] = rng.permutation(B * 5).reshape(B, 5)
+    w, lens = rng.integers(0, 10 ** 6, (B, hk, L)), [L, 90][:B]
+    cache, dw, dt = g.binding.Kv4Cache(cuda(ref.to_bytes()), 64, page), cuda(w), cuda(table)
+    kept, _ = c.kv4_evict(cache, dw, cuda(np.array(lens, np.int32)), dt[:, :cols], keep, 3, 7, L, dst_table=dt[:, :dst_cols])
+    wk, _, ww, pool = D.evict(ref, w, lens, table, table, L, keep, 3, 7)
+    g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+    g.assert_equal(g.host(dw), ww, "weights")
+    g.assert_equal(g.host(cache.pool), pool, "pool")
+    assert c.poll_status() == 0
