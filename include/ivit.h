@@ -30,7 +30,8 @@
  *    enqueued on the stream before it, an earlier library call included.
  *  - A context belongs to one device; the caller keeps that device current
  *    (cudaSetDevice) while calling into the library with that context.
- *    Kernel attributes are set per device by ivit_ctx_create, so several
+ *    Kernel attributes are set per device by ivit_ctx_create (those of
+ *    ivit_kv4_attention by its first call), so several
  *    contexts on several devices may live in one process.
  *  - Matrices are row-major; leading dimensions (ld*) and strides are in
  *    elements.  int8 tensors: pointer 16-byte aligned and ld a multiple of 16.

@@ -45,6 +45,7 @@ struct ivit_ctx {
   int64_t pair_launches;   // Dense launches that ran on CTA pairs (ivit_ctx_pair_launch_count)
   int gemm_engine;
   int sm_count;
+  bool kv4_ready;         // kv4_prepare_device has run (by the first ivit_kv4_attention)
   int cluster_room[17];   // clusters of 1 ... 16 CTAs, an SM for each, that the device runs at once (kv4_prepare_device)
   void* tmap_encode;  // cuTensorMapEncodeTiled, resolved at context creation
   int gemm_pairs;     // CTA pairs (cta_group::2) for Dense layers: 0 never, 1 wherever possible, 2 by size (ivit_ctx_set_gemm_pairs)
@@ -282,8 +283,8 @@ int launch_shiftgelu_static(ivit_ctx* ctx, const int8_t* in, int64_t ldin, ivit_
 int launch_shiftgelu(ivit_ctx* ctx, const int8_t* in, int64_t ldin, ivit_exp_params p, ivit_scale post,
                      int8_t* out, int64_t ldout, int64_t rows, int64_t cols);
 int launch_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params& p);
-// The cache in 4 bits (kv4.cu, kv4_attention.cu); kv4_prepare_device: shared-memory limits of its kernels, and the
-// clusters that the current device runs at once.
+// The cache in 4 bits (kv4.cu, kv4_attention.cu); kv4_prepare_device, once for a context: shared-memory limits of the attention's
+// kernels, and the clusters that the current device runs at once.
 int kv4_prepare_device(ivit_ctx* ctx);
 int launch_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K, int64_t ldk, const int8_t* V, int64_t ldv,
                       const int64_t* slots, int64_t tokens);

@@ -462,8 +462,7 @@ int ivit_ctx_create(ivit_ctx** out, int device, void* cuda_stream) {
       qres != cudaDriverEntryPointSuccess)
     fn = nullptr;
   c->tmap_encode = fn;
-  if (gemm_tc_prepare_device() != IVIT_OK || gemm_small_prepare_device() != IVIT_OK || attention_prepare_device() != IVIT_OK ||
-      kv4_prepare_device(c) != IVIT_OK) {
+  if (gemm_tc_prepare_device() != IVIT_OK || gemm_small_prepare_device() != IVIT_OK || attention_prepare_device() != IVIT_OK) {
     cudaGetLastError();
     cudaFree(c->gelu_tables);
     cudaFreeHost(c->status_host);
@@ -1153,6 +1152,13 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv
   if (!any) return IVIT_OK;
   DeviceGuard guard(ctx);
   if (!guard.ok) return IVIT_ERR_CUDA;
+  if (!ctx->kv4_ready) {   // (contexts that never come here, an encoder's, do not pay for it, and do not fail by it)
+    if (kv4_prepare_device(ctx) != IVIT_OK) {
+      cudaGetLastError();
+      return IVIT_ERR_CUDA;
+    }
+    ctx->kv4_ready = true;
+  }
   return launch_kv4_attention(ctx, *cache, *p);
 }
 

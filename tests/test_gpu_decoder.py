@@ -796,3 +796,39 @@ def test_evict_in_place_by_columns_of_one_table(B, cols, dst_cols):
     g.assert_equal(g.host(dw), ww, "weights")
     g.assert_equal(g.host(cache.pool), pool, "pool")
     assert c.poll_status() == 0
+
+
+def test_the_first_attention_of_a_context_is_captured():
+    """A context that has made no call: its first attention, by a cluster, goes into a graph; a second context's runs at once."""
+    g = _g()
+    rng = np.random.default_rng(47)
+    d, page, hk, hq, L = 64, 64, 2, 4, 5000
+    np_ = -(-L // page)
+    ref = filled(rng, np_, hk, d, page)
+    table, q = rng.permutation(np_)[None], rand_i8(rng, (1, hq * d))
+    qk, pv = dyadic(25.0 / (8 * np.sqrt(d) * 32 * 40)), dyadic(1 / 128)
+    want, _ = D.attention(ref, q, hq, [0, 1], [L], table, qk, 17, 15, pv, np.zeros((1, hq * d)))
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        cache = g.binding.Kv4Cache(cuda(ref.to_bytes()), d, page)
+        args = (cache, cuda(q), cuda(np.array([0, 1], np.int32)), cuda(np.array([L], np.int32)), cuda(table.astype(np.int32)), g.binding.DevScale.of(*qk),
+                ExpParams(17, 15), g.binding.DevScale.of(*pv), 1, L)
+        out = torch.full((1, hq * d), 55, dtype=torch.int8, device="cuda")
+        c = g.binding.Context(0, stream)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            c.kv4_attention(*args, out=out)
+        stream.synchronize()
+        assert (out == 55).all()
+        graph.replay()
+        stream.synchronize()
+        g.assert_equal(g.host(out), want.astype(np.int8), "replayed")
+        other = g.binding.Context(0, stream)
+        out.fill_(55)
+        other.kv4_attention(*args, out=out)
+        stream.synchronize()
+        g.assert_equal(g.host(out), want.astype(np.int8), "launched")
+        for x in (c, other):
+            assert x.poll_status() == 0
+            x.close()
