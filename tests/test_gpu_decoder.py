@@ -832,3 +832,64 @@ def test_the_first_attention_of_a_context_is_captured():
         for x in (c, other):
             assert x.poll_status() == 0
             x.close()
+
+
+# rows that are taken several at a time (GROUPED: 8, with an int32 tensor or row scales 4), at widths whose threads' words are all there (C / 4 a
+# multiple of 64) and at others, the last group not full
+GROUPED = [(3601, 132), (1999, 1000), (1999, 2048), (901, 4092)]
+
+
+@pytest.mark.parametrize("x32,h32", [(0, None), (1, None), (0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("rows,C", GROUPED)
+def test_rmsnorm_groups_of_rows(rows, C, x32, h32):
+    g, c = _g(), _g().ctx()
+    sms, R = torch.cuda.get_device_properties(0).multi_processor_count, 8
+    assert rows >= 3 * sms and (rows * (C // 4) >= 275 * R * sms or rows >= 3 * R * sms) and rows % 4   # (the rule, at its largest R)
+    rng = np.random.default_rng(rows + C + 7 * x32 + 3 * (h32 or 0))
+    for kind in ("ordinary", "extreme"):
+        x, res = norm_case(rng, rows, C, x32, h32 or 0, kind)
+        x[-1], res[-2] = x[-1][::-1], 0
+        xs = scale_channels(rng.uniform(0.5, 1.5, C) * ((500.0 if h32 else 10.0) / (20000.0 if x32 else 1100.0)))
+        rs = Scale(*dyadic(0.96875))
+        for dynamic, M_ln, ratio in ((False, 20, 32.0 * np.sqrt(C) / 2 ** 20), (True, 22, 0.4)):
+            gs = scale_channels(rng.uniform(0.8, 1.1, C) * min(ratio, 0.9))
+            want, top, total = D.rmsnorm(x, (gs.mult, gs.shift), M_ln, (xs.mult, xs.shift), None if h32 is None else res, (rs.mult, rs.shift), h32 == 1,
+                                         dynamic)
+            sums = None if h32 is None else g.dev(np.zeros_like(res))
+            rm = torch.full((rows,), -1, dtype=torch.int32, device="cuda") if dynamic else None
+            got = c.rmsnorm(g.dev(x), g.binding.DevScale(gs, "cuda"), x_scale=g.binding.DevScale(xs, "cuda"), res=None if h32 is None else g.dev(res),
+                            res_scale=None if h32 is None else g.binding.DevScale(rs, "cuda"), M_ln=M_ln, sum_out=sums, row_max=rm)
+            what = f"{kind}, dynamic {dynamic}"
+            g.assert_equal(g.host(got), want.astype(np.int8), what)
+            if dynamic:
+                g.assert_equal(g.host(rm), top.astype(np.int32), what + " row_max")
+            if h32 is not None:
+                g.assert_equal(g.host(sums), total.astype(res.dtype), what + " sum")
+    assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("h32", [0, 1])
+@pytest.mark.parametrize("rows,C", GROUPED)
+def test_rmsnorm_groups_leave_the_rest_alone(rows, C, h32):
+    """The stream in place: columns past C and rows past the last keep what they held, the others get their sums once."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(rows + h32)
+    x, res = norm_case(rng, rows, C, 0, h32, "ordinary")
+    ld = (C + 15) // 16 * 16 + 16
+    dt = torch.int32 if h32 else torch.int8
+    scale = Scale(*dyadic(0.01))
+    s = g.binding.DevScale(scale, "cuda")
+    for dynamic in (False, True):
+        bx = torch.full((rows + 9, ld), 77, dtype=torch.int8, device="cuda")
+        br, bo, rm = bx.clone().to(dt), bx.clone(), torch.full((rows + 9,), 77, dtype=torch.int32, device="cuda")
+        bx[:rows, :C], br[:rows, :C] = cuda(x), cuda(res)
+        c.rmsnorm(bx[:rows, :C], s, x_scale=s, res=br[:rows, :C], res_scale=s, sum_out=br[:rows, :C], out=bo[:rows, :C], row_max=rm[:rows] if dynamic else None)
+        want, top, total = D.rmsnorm(x, (scale.mult, scale.shift), 20, (scale.mult, scale.shift), res, (scale.mult, scale.shift), h32 == 1, dynamic)
+        g.assert_equal(g.host(bo[:rows, :C]), want.astype(np.int8), "out")
+        g.assert_equal(g.host(br[:rows, :C]), total.astype(res.dtype), "stream")
+        g.assert_equal(g.host(bx[:rows, :C]), x, "x")
+        for t in (bx, br, bo):
+            assert (t[rows:] == 77).all() and (t[:, C:] == 77).all()
+        assert (rm[rows if dynamic else 0:] == 77).all()
+        if dynamic:
+            g.assert_equal(g.host(rm[:rows]), top.astype(np.int32), "row_max")
