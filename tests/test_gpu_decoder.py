@@ -893,3 +893,102 @@ def test_rmsnorm_groups_leave_the_rest_alone(rows, C, h32):
         assert (rm[rows if dynamic else 0:] == 77).all()
         if dynamic:
             g.assert_equal(g.host(rm[:rows]), top.astype(np.int32), "row_max")
+
+
+def weights_of(kind, rng, L):
+    """Weights whose threshold falls where the kernel's first digit (bit length and five bits) does not tell it."""
+    if kind == "equal":                # one value, far above the small ones
+        return np.full(L, 3 << 40)
+    if kind == "equal_and_others":     # as many as are wanted and more of one value, a few above and below in other digits
+        w = np.full(L, (1 << 50) + 12345)
+        w[rng.permutation(L)[:L // 20]] = rng.integers(0, 1 << 62, L // 20)
+        return w
+    if kind == "one_digit":            # all of one digit, most of them different, some equal ones
+        return (1 << 40) + rng.integers(0, 1 << 34, L) // 3 * 3
+    if kind == "one_digit_ties":       # few values, of one digit: ties at the threshold
+        return (1 << 40) + rng.integers(0, 3, L) * 65537
+    if kind == "low_bytes":            # equal but for the last byte
+        return (1 << 55) + rng.integers(0, 200, L)
+    if kind == "negative":             # nearly all below zero: the threshold too
+        w = -rng.integers(1, 1 << 62, L)
+        w[rng.permutation(L)[:40]] = rng.integers(0, 1 << 40, 40)
+        return w
+    if kind == "negative_equal":       # all of them the least value
+        return np.full(L, -2 ** 63)
+    if kind == "negative_and_zero":    # zeros and negative ones share the first digit
+        return np.where(rng.random(L) < 0.1, 0, -rng.integers(1, 5, L))
+    # few_negative: at most 1024 below one, the threshold among them
+    w = rng.integers(1 << 20, 1 << 60, L)
+    w[rng.permutation(L)[:700]] = -rng.integers(0, 9, 700)
+    return w
+
+
+KINDS = ["equal", "equal_and_others", "one_digit", "one_digit_ties", "low_bytes", "negative", "negative_equal", "negative_and_zero", "few_negative"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("L", [2900, 16384, 16385, 20003])      # (keys in registers up to 16384, else read again)
+def test_evict_selects_within_one_digit(L, kind):
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(L + len(kind))
+    page, hk, sinks, recent = 256, 2, 3, 50
+    keep = L - 300 if kind == "few_negative" else L // 2
+    np_ = -(-L // page)
+    w = np.stack([weights_of(kind, rng, L) for _ in range(2 * hk)]).reshape(2, hk, L).astype(np.int64)
+    w[:, :, :sinks], w[:, :, L - 500:] = 2 ** 63 - 1, np.where(rng.random(500) < 0.5, -2 ** 63, w[:, :, L - 500:])   # (not candidates; another length's are)
+    lens = [L, L - 400]
+    for in_place in (True, False):
+        ref = filled(rng, 4 * np_, hk, 64, page)
+        table, dst = np.arange(2 * np_, dtype=np.int32).reshape(2, np_), np.arange(2 * np_, 4 * np_, dtype=np.int32).reshape(2, np_)
+        cache, dw = g.binding.Kv4Cache(cuda(ref.to_bytes()), 64, page), cuda(w)
+        wo = dw if in_place else torch.empty_like(dw)
+        kept, new = c.kv4_evict(cache, dw, cuda(np.array(lens, np.int32)), cuda(table), keep, sinks, recent, L,
+                                dst_table=None if in_place else cuda(dst), weights_out=wo)
+        wk, wn, ww, pool = D.evict(ref, w, lens, table, table if in_place else dst, L, keep, sinks, recent)
+        g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+        g.assert_equal(g.host(new), wn.astype(np.int32), "new lens")
+        g.assert_equal(g.host(wo), ww, "weights")
+        g.assert_equal(g.host(cache.pool), pool, "pool")
+    assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("in_place", [True, False])
+@pytest.mark.parametrize("d", [64, 128])
+def test_evict_moves_nothing_from_or_to_pages_that_are_not_there(d, in_place):
+    """Rows of source or destination pages outside the pool: no byte of them is written, all others move; kept, weights and lengths as ever."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(d)
+    page, hk, keep, sinks, recent, L = 32, 2, 100, 2, 9, 200
+    lens = [200, 200, 77, 260, -4]                      # (the last two: past max_len, and none)
+    B, ps, pd = len(lens), 7, 4
+    before = rng.integers(0, 256, (B * (ps + pd), hk, page * (d + d // 32 + 1))).astype(np.uint8)
+    order = rng.permutation(B * (ps + pd)).astype(np.int32)
+    table, dst = order[:B * ps].reshape(B, ps).copy(), order[B * ps:].reshape(B, pd).copy()
+    table[0, 1], table[0, 4], table[1, 0], table[2, 2], table[2, 6] = len(before), -1, 2 ** 31 - 1, -2 ** 31, 12345   # (the last one holds no key)
+    dst[1, 2], dst[2, 0], dst[3, 3] = -1, len(before), 2 ** 31 - 1
+    w = rng.integers(0, 10 ** 6, (B, hk, L))
+    cache, dw, dt = g.binding.Kv4Cache(cuda(before), d, page), cuda(w), cuda(table)
+    wo = dw if in_place else torch.full((B, hk, pd * page), -5, dtype=torch.int64, device="cuda")
+    kept, new = c.kv4_evict(cache, dw, cuda(np.array(lens, np.int32)), dt, keep, sinks, recent, L, dst_table=dt if in_place else cuda(dst), weights_out=wo)
+    torch.cuda.synchronize()
+    assert c.poll_status() == -3 and c.poll_status() == 0
+    to = table if in_place else dst
+    at = dict(kc=(0, d // 2), ks=(page * d // 2, d // 32), vc=(page * (d // 2 + d // 32), d // 2), vs=(page * (d + d // 32), 1))
+    pool, wk, ww = before.copy(), np.full((B, hk, keep), -1), np.zeros((B, hk, wo.shape[2]), np.int64)
+    for b in range(B):
+        n = min(max(lens[b], 0), L)
+        for h in range(hk):
+            stay = list(range(n))
+            if n > keep:
+                best = sorted(range(sinks, n - recent), key=lambda j: (-w[b, h, j], j))[:keep - sinks - recent]
+                stay = sorted(list(range(sinks)) + best + list(range(n - recent, n)))
+            wk[b, h, :len(stay)], ww[b, h, :len(stay)] = stay, w[b, h, stay]
+            for i, j in enumerate(stay):
+                s, t = table[b, j // page], to[b, i // page]
+                if 0 <= s < len(before) and 0 <= t < len(before):
+                    for first, step in at.values():
+                        pool[t, h, first + i % page * step:first + (i % page + 1) * step] = before[s, h, first + j % page * step:first + (j % page + 1) * step]
+    g.assert_equal(g.host(kept), wk.astype(np.int32), "kept")
+    g.assert_equal(g.host(new), np.array([min(keep, max(0, min(n, L))) for n in lens], np.int32), "new lens")
+    g.assert_equal(g.host(wo), ww, "weights")
+    g.assert_equal(g.host(cache.pool), pool, "pool")
