@@ -992,3 +992,22 @@ def test_evict_moves_nothing_from_or_to_pages_that_are_not_there(d, in_place):
     g.assert_equal(g.host(new), np.array([min(keep, max(0, min(n, L))) for n in lens], np.int32), "new lens")
     g.assert_equal(g.host(wo), ww, "weights")
     g.assert_equal(g.host(cache.pool), pool, "pool")
+
+
+@pytest.mark.parametrize("B,hk,G,L", [(40, 4, 2, 2700), (38, 8, 4, 4000), (128, 2, 3, 2600)])
+def test_attention_longest_first(B, hk, G, L):
+    """Heads of 128 in CTAs of sixteen warps that take the sequences longest first (40 blocks of 32 keys or more for each wave of CTAs): equal lengths, empty ones,
+    bad ones, the longest at the end."""
+    g, c = _g(), _g().ctx()
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert B <= 128 and B * hk > sms and -(-L // 32) >= 40 * -(-B * hk // sms)
+    rng = np.random.default_rng(B)
+    d, page = 128, 64
+    lens = rng.integers(0, L + 1, B)
+    lens[::4], lens[1], lens[-1] = L // 3, 0, L
+    np_ = -(-L // page)
+    ref = filled(rng, 60, hk, d, page)
+    q, table = rand_i8(rng, (B, G * hk * d)), rng.integers(0, 60, (B, np_))
+    for w in (False, True):
+        attend(c, g, ref, q, G * hk, [1] * B, lens, table, weights=w, max_len=L)
+    assert c.poll_status() == 0
