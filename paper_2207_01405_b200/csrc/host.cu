@@ -1173,7 +1173,8 @@ int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_ev
   if (p->ldw < p->max_len || p->ldw_out < p->keep || p->ldtable < (p->max_len + cache->page - 1) / cache->page ||
       p->ld_dst < (rows + cache->page - 1) / cache->page)
     return IVIT_ERR_INVALID_ARG;
-  if ((p->dst_table == p->table && p->ld_dst != p->ldtable) || (p->weights_out == p->weights && p->ldw_out != p->ldw)) return IVIT_ERR_INVALID_ARG;
+  if (p->seqs > 0 && ((p->dst_table == p->table && p->ld_dst != p->ldtable) || (p->weights_out == p->weights && p->ldw_out != p->ldw)))
+    return IVIT_ERR_INVALID_ARG;   // (no sequences: nothing is moved, and all of the pointers may be null)
   const uintptr_t al8 = reinterpret_cast<uintptr_t>(p->weights) | reinterpret_cast<uintptr_t>(p->weights_out);
   if ((al8 & 7) || !aligned4(p->lens) || !aligned4(p->table) || !aligned4(p->dst_table) || !aligned4(p->kept) || !aligned4(p->new_lens))
     return IVIT_ERR_ALIGNMENT;

@@ -417,3 +417,11 @@ def test_scales_that_are_not_on_the_device_are_refused(lib):
     c.index = -1
     assert c._fields(scale, 64) == scale.fields and c._fields(lib.DevScale.of(2 ** 30, 35), 7) == (0, 0, 2 ** 30, 35)
     c.h = None
+
+
+def test_evict_of_no_sequences_to_other_pages(lib):
+    """Tensors without elements have no address: that both are null does not make the call one in place."""
+    none = dict(seqs=0, w=None, wo=None, lens=None, table=None, dst=None, kept=None, new=None)
+    assert evict(lib, **none) == 0
+    assert evict(lib, **none, ldt=100, ldd=2, ldw=100, ldwo=50) == 0
+    assert evict(lib, **none, keep=0) == -1

@@ -1011,3 +1011,23 @@ def test_attention_longest_first(B, hk, G, L):
     for w in (False, True):
         attend(c, g, ref, q, G * hk, [1] * B, lens, table, weights=w, max_len=L)
     assert c.poll_status() == 0
+
+
+def test_calls_without_rows_or_sequences():
+    """Nothing to do: every operator takes it, launches nothing, and hands back tensors of the right shapes."""
+    g, c = _g(), _g().ctx()
+    B = g.binding
+    z = lambda *s, t=torch.int8: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    one, cache, i32, i64 = B.DevScale.of(2 ** 30, 40), B.Kv4Cache.empty(4, 2, 64, 32, "cuda"), torch.int32, torch.int64
+    before = c.launch_count()
+    assert c.rmsnorm(z(0, 64), one).shape == (0, 64)
+    assert c.rmsnorm(z(0, 64), one, x_scale=one, res=z(0, 64), res_scale=one, sum_out=z(0, 64), row_max=z(0, t=i32)).shape == (0, 64)
+    c.kv4_append(cache, z(0, 128), z(0, 128), z(0, t=i64))
+    att = lambda n, b: c.kv4_attention(cache, z(n, 256), z(b + 1, t=i32), z(b, t=i32), z(b, 2, t=i32), one, ExpParams(17, 15), one, 1, 64, weights=z(b, 2, 64, t=i64))  # noqa: E731
+    assert att(0, 0).shape == (0, 256) and att(0, 3).shape == (0, 256) and att(3, 0).shape == (3, 256)
+    for k in (dict(), dict(dst_table=z(0, 5, t=i32)), dict(dst_table=z(0, 5, t=i32), weights_out=z(0, 2, 40, t=i64))):
+        kept, new = c.kv4_evict(cache, z(0, 2, 64, t=i64), z(0, t=i32), z(0, 2, t=i32), 40, 1, 1, 64, **k)
+        assert kept.shape == (0, 2, 40) and new.shape == (0,)
+    assert c.launch_count() == before
+    torch.cuda.synchronize()
+    assert c.poll_status() == 0
