@@ -1164,7 +1164,8 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv
 
 int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_evict_params* p) {
   if (!ctx || !p || p->seqs < 0 || p->max_len < 0) return IVIT_ERR_INVALID_ARG;
-  if (p->seqs > 0 && (!p->weights || !p->lens || !p->table || !p->dst_table || !p->weights_out || !p->kept || !p->new_lens)) return IVIT_ERR_INVALID_ARG;
+  if (p->seqs > 0 && (!p->lens || !p->weights_out || !p->kept || !p->new_lens || (p->max_len > 0 && (!p->weights || !p->table || !p->dst_table))))
+    return IVIT_ERR_INVALID_ARG;
   const int rc = check_kv4(cache, true);
   if (rc) return rc;
   if (p->keep < 1 || p->sinks < 0 || p->recent < 0 || p->sinks > p->keep || p->recent > p->keep - p->sinks) return IVIT_ERR_INVALID_ARG;
@@ -1173,8 +1174,8 @@ int ivit_kv4_evict(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv4_ev
   if (p->ldw < p->max_len || p->ldw_out < p->keep || p->ldtable < (p->max_len + cache->page - 1) / cache->page ||
       p->ld_dst < (rows + cache->page - 1) / cache->page)
     return IVIT_ERR_INVALID_ARG;
-  if (p->seqs > 0 && ((p->dst_table == p->table && p->ld_dst != p->ldtable) || (p->weights_out == p->weights && p->ldw_out != p->ldw)))
-    return IVIT_ERR_INVALID_ARG;   // (no sequences: nothing is moved, and all of the pointers may be null)
+  if (p->seqs > 0 && p->max_len > 0 && ((p->dst_table == p->table && p->ld_dst != p->ldtable) || (p->weights_out == p->weights && p->ldw_out != p->ldw)))
+    return IVIT_ERR_INVALID_ARG;   // (no sequences, or no keys: nothing is moved, and these pointers may be null)
   const uintptr_t al8 = reinterpret_cast<uintptr_t>(p->weights) | reinterpret_cast<uintptr_t>(p->weights_out);
   if ((al8 & 7) || !aligned4(p->lens) || !aligned4(p->table) || !aligned4(p->dst_table) || !aligned4(p->kept) || !aligned4(p->new_lens))
     return IVIT_ERR_ALIGNMENT;

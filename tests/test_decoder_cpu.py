@@ -425,3 +425,13 @@ def test_evict_of_no_sequences_to_other_pages(lib):
     assert evict(lib, **none) == 0
     assert evict(lib, **none, ldt=100, ldd=2, ldw=100, ldwo=50) == 0
     assert evict(lib, **none, keep=0) == -1
+
+
+def test_evict_without_keys_needs_no_tables(lib):
+    """max_len = 0: there is nothing to read or to move, and tables and weights without columns have no address.  What is written has to be there."""
+    none = dict(seqs=0, ml=0, w=None, table=None, dst=None)
+    assert evict(lib, **none) == 0
+    for n in ("lens", "wo", "kept", "new"):
+        assert evict(lib, **{**none, "seqs": 3, n: None}) == -1, n
+    for n in ("w", "table", "dst"):
+        assert evict(lib, **{n: None}) == -1, n

@@ -1031,3 +1031,18 @@ def test_calls_without_rows_or_sequences():
     assert c.launch_count() == before
     torch.cuda.synchronize()
     assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_without_keys(in_place):
+    """Sequences that have no keys yet, in a call that is sized for none: tables and weights without columns."""
+    g, c = _g(), _g().ctx()
+    z = lambda *s, t=torch.int32: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    pool = torch.full((4, 2, 32 * 67), 99, dtype=torch.uint8, device="cuda")
+    cache, keep = g.binding.Kv4Cache(pool, 64, 32), 40
+    table = z(3, 0)
+    wo = torch.full((3, 2, 45), -5, dtype=torch.int64, device="cuda")
+    kept, new = c.kv4_evict(cache, z(3, 2, 0, t=torch.int64), z(3), table, keep, 4, 16, 0, dst_table=None if in_place else z(3, 2), weights_out=wo)
+    assert (kept == -1).all() and (new == 0).all() and (wo == 0).all() and (pool == 99).all()
+    torch.cuda.synchronize()
+    assert c.poll_status() == 0
