@@ -427,8 +427,8 @@ int ivit_isqrt_range(ivit_ctx* ctx, uint32_t n0, uint32_t count, uint16_t* out);
  *                     out = floor((z R + 2^(22+a)) / 2^(23+a)),  row_max[r] = A:  the row stands for out A / 127
  * x int8 or int32 (the output, or the accumulators, of a Dense layer); res (the stream) int8, saturated like int8, or int32,
  * saturated to [-2^20, 2^20]; without res x is clipped to [-2^20, 2^20], x_scale and res_scale are not used and sum must be NULL.
- * sum has the type of res, may be res itself (with its leading dimension), or NULL (not wanted).  x_scale and gamma_scale per-channel or per-tensor, res_scale
- * per-tensor.  8 <= M_ln <= 22, C % 4 == 0, C <= 16384; pointers 16-byte aligned, leading dimensions multiples of 16 bytes (row_max and
+ * sum has the type of res, may be res or x itself (with its leading dimension; x only if it has that type), or NULL (not wanted).  x_scale and
+ * gamma_scale per-channel or per-tensor, res_scale per-tensor.  8 <= M_ln <= 22, C % 4 == 0, C <= 16384; pointers 16-byte aligned, leading dimensions multiples of 16 bytes (row_max and
  * the scales' arrays of their own size).  out may not overlap the other tensors. */
 typedef struct {
   const void* x; int64_t ldx;              /* [rows, C] */

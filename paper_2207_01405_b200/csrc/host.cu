@@ -1096,6 +1096,7 @@ int ivit_rmsnorm(ivit_ctx* ctx, const ivit_rmsnorm_params* p) {
   if (misaligned(p->x, p->ldx, p->x_dtype) || misaligned(p->out, p->ldout, IVIT_I8) || !aligned4(p->row_max)) return IVIT_ERR_ALIGNMENT;
   if ((p->res && misaligned(p->res, p->ldres, p->res_dtype)) || (p->sum && misaligned(p->sum, p->ldsum, p->res_dtype))) return IVIT_ERR_ALIGNMENT;
   if (p->sum && p->sum == p->res && p->ldsum != p->ldres) return IVIT_ERR_INVALID_ARG;
+  if (p->rows > 0 && p->sum && p->sum == p->x && (p->ldsum != p->ldx || p->res_dtype != p->x_dtype)) return IVIT_ERR_INVALID_ARG;
   if (!scale_ok(p->gamma_scale) || (p->res && (!scale_ok(p->x_scale) || !scale_ok(p->res_scale) || p->res_scale.mult_c))) return IVIT_ERR_RANGE;
   if (!aligned4(p->gamma_scale.mult_c) || (p->res && !aligned4(p->x_scale.mult_c))) return IVIT_ERR_ALIGNMENT;
   if (p->rows == 0) return IVIT_OK;

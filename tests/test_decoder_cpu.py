@@ -435,3 +435,11 @@ def test_evict_without_keys_needs_no_tables(lib):
         assert evict(lib, **{**none, "seqs": 3, n: None}) == -1, n
     for n in ("w", "table", "dst"):
         assert evict(lib, **{n: None}) == -1, n
+
+
+def test_rmsnorm_refuses_a_sum_that_runs_over_x(lib):
+    """sum == x with another leading dimension or type: words of it would lie on values of x that other threads have still to read."""
+    for k in (dict(lds=80, ldx=64), dict(lds=64, ldx=80), dict(xd=1, lds=64), dict(rd=1, lds=64)):
+        assert rms(lib, **{**dict(res=2 * AT, ldr=80, sum=AT, rows=4), **k}) == -1, k
+    for k in (dict(xd=0, rd=0), dict(xd=1, rd=1), dict(xd=1, lds=80)):       # (the same place, or no rows)
+        assert rms(lib, **{**dict(res=2 * AT, ldr=80, sum=AT, lds=64, rows=0), **k}) == 0, k

@@ -1046,3 +1046,27 @@ def test_evict_without_keys(in_place):
     assert (kept == -1).all() and (new == 0).all() and (wo == 0).all() and (pool == 99).all()
     torch.cuda.synchronize()
     assert c.poll_status() == 0
+
+
+@pytest.mark.parametrize("wide", [0, 1])
+@pytest.mark.parametrize("rows,C", [(1, 768), (197, 1000), (1999, 1000), (1999, 2048)])
+def test_rmsnorm_sum_over_x(rows, C, wide):
+    """The sum takes the place of x, and x may be the stream too; scales that lie anywhere, 16-byte aligned or not."""
+    g, c = _g(), _g().ctx()
+    rng = np.random.default_rng(rows + wide)
+    x, res = norm_case(rng, rows, C, wide, wide, "ordinary")
+    xs, gs = scale_channels(rng.uniform(0.3, 0.9, C)), scale_channels(rng.uniform(0.8, 1.1, C) * 32 * np.sqrt(C) / 2 ** 20)
+    rs = Scale(*dyadic(0.96875))
+    off = lambda a: torch.cat([torch.zeros(1, dtype=torch.from_numpy(a).dtype), torch.from_numpy(a)]).cuda()[1:]  # noqa: E731
+    dx_scale, dgamma = (g.binding.DevScale.of(off(s.mult.astype(np.int32)), off(s.shift.astype(np.uint8))) for s in (xs, gs))
+    assert dx_scale.mult_t.data_ptr() % 16 == 4
+    drs = g.binding.DevScale(rs, "cuda")
+    for same in (False, True):
+        want, _, total = D.rmsnorm(x, (gs.mult, gs.shift), 20, (xs.mult, xs.shift), x if same else res, (rs.mult, rs.shift), wide == 1)
+        dx = g.dev(x)
+        dr = dx if same else g.dev(res)
+        got = c.rmsnorm(dx, dgamma, x_scale=dx_scale, res=dr, res_scale=drs, sum_out=dx)
+        g.assert_equal(g.host(got), want.astype(np.int8), f"out, {same}")
+        g.assert_equal(g.host(dx), total.astype(x.dtype), f"sum, {same}")
+        if not same:
+            g.assert_equal(g.host(dr), res, "res")
