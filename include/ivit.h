@@ -57,7 +57,7 @@ enum {
   IVIT_OK = 0,
   IVIT_ERR_INVALID_ARG = -1,    /* null pointer, negative size, bad enum */
   IVIT_ERR_ALIGNMENT = -2,      /* pointer or leading dimension not aligned as stated above */
-  IVIT_ERR_RANGE = -3,          /* a quantisation constant violates a stated bound */
+  IVIT_ERR_RANGE = -3,          /* a quantisation constant violates a stated bound; from ivit_ctx_poll_status: an index or a length on the device does */
   IVIT_ERR_UNSUPPORTED = -4,    /* shape / dtype combination not built */
   IVIT_ERR_WORKSPACE = -5,      /* workspace missing, misaligned or too small */
   IVIT_ERR_CUDA = -6,           /* a CUDA runtime / driver call failed */
@@ -415,7 +415,7 @@ int ivit_probe_int8_mma(ivit_ctx* ctx, int32_t iters, float* ms, double* ops);
 int ivit_isqrt_range(ivit_ctx* ctx, uint32_t n0, uint32_t count, uint16_t* out);
 
 /* ---- decoder operators: root-mean-square norm, a key/value cache held in 4 bits ----
- * The paper describes encoders; these are the operators that a decoder needs beside ivit_linear, in the same integer arithmetic. */
+ * The paper describes encoders; these are operators of a decoder, to go with ivit_linear, in the same integer arithmetic. */
 
 /* Root-mean-square norm over each row, with the residual's addition in front:
  *   h   = res ? sat( rq(x; x_scale[c]) + rq(res; res_scale) ) : clip(x)        (sum = h)
@@ -425,6 +425,8 @@ int ivit_isqrt_range(ivit_ctx* ctx, uint32_t n0, uint32_t count, uint16_t* out);
  *   row_max == NULL:  out = sat8(z)                                            (one static scale)
  *   row_max != NULL:  A = max_c |z|, a = bit length of A, R = floor(127 2^(23+a) / A) (0 when A = 0),
  *                     out = floor((z R + 2^(22+a)) / 2^(23+a)),  row_max[r] = A:  the row stands for out A / 127
+ * The mean's sqrt(C) and 2^-M_ln belong into gamma_scale: its ratio is gamma sqrt(C) / 2^M_ln over the output's unit.  No epsilon: a row of zeros stays zeros.
+ * The root is a whole number, so that y is too large by up to one part in sd: 2 % at sd = 50, and 73 % in a row with V = 3.
  * x int8 or int32 (the output, or the accumulators, of a Dense layer); res (the stream) int8, saturated like int8, or int32,
  * saturated to [-2^20, 2^20]; without res x is clipped to [-2^20, 2^20], x_scale and res_scale are not used and sum must be NULL.
  * sum has the type of res, may be res or x itself (with its leading dimension; x only if it has that type), or NULL (not wanted).  x_scale and
@@ -475,10 +477,15 @@ int ivit_kv4_append(ivit_ctx* ctx, const ivit_kv4_cache* cache, const int8_t* K,
  *   u_j  = floor((e_j vstep_j + 2^(z-1)) / 2^z), z = bit length of top - 8     (weights in 16 bits)
  *   num_c = sum_j u_j vcode[j,c];  den = sum_j e_j;  t_c = floor(num_c 2^(z+5) / den)        (1/256 of a value's unit)
  *   O_c  = sat8(rq(t_c; pv_scale))
- * The division comes behind the product, in one piece: probabilities of 8 bits would turn nearly every key of a long row into zero.  A
- * row that sees no key gets zeros.  weights (NULL: not wanted) int64 [seqs, heads, ldw]:
+ * The division comes behind the product, in one piece: probabilities of 8 bits would turn nearly every key of a long row into zero.  The 16
+ * bits of u_j have an end of the same kind, farther down: a key more than ln(256 vstep_j) to ln(512 vstep_j) nats below the row's largest (10 to 11 at
+ * a step of 100) adds nothing to num_c, but counts in den.  Over L keys t_c is within 7 L 2^z / (16 den) of a value's unit of the quotient with
+ * weights that are not rounded (less than L / 292, as den >= 2^(z+7)): below one unit for rows of up to 292 keys, and for longer ones whose weight is
+ * spread, but tens of units where few keys hold it against tens of thousands far below them (one key, and 30 000 keys of code 7 and step 100
+ * that are 11 nats lower: 0 where it should be 31).
+ * A row that sees no key gets zeros.  weights (NULL: not wanted) int64 [seqs, heads, ldw]:
  *   weights[b, h, j] += sum over the rows that see j, of all query heads that read h, of floor(e_j 2^24 / den)
- * Q, O int8 [tokens, q_heads d], not overlapping, 16-byte aligned; rows of no sequence are left as they are.  max_q and max_len: no sequence has more query
+ * Q, O int8 [tokens, q_heads d], not overlapping, 16-byte aligned; rows of no sequence are left as they are.  With tokens, seqs or max_q 0 nothing is looked at.  max_q and max_len: no sequence has more query
  * tokens or keys (the launch is sized by them; ldtable >= ceil(max_len / page), ldw >= max_len); max_len <= IVIT_KV4_MAX_LEN.  A sequence
  * that breaks them, a q_start outside 0 .. tokens, or a page outside the pool is reported by ivit_ctx_poll_status (IVIT_ERR_RANGE) and read only as
  * far as it is valid: keys of such a page are not seen, query rows past max_q or tokens are not written, keys past max_len do not exist. */
@@ -499,7 +506,7 @@ int ivit_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache* cache, const ivit_kv
  *   kept[b, h, i]   = index of the i-th key that stays, -1 from new_lens[b] on             (int32 [seqs, heads, keep])
  *   row i of dst_table's pages = that key's codes and steps;  weights_out[b, h, i] = its weight, 0 from new_lens[b] to ldw_out
  * In place: dst_table == table and weights_out == weights (with the same leading dimensions).  Else the pages of dst_table hold no
- * source row, and weights_out does not overlap weights.  No page that rows are moved to is named twice, for two sequences or for one (in place: sequences
+ * source row, and weights_out does not overlap weights.  With max_len 0 weights and the tables may be NULL.  No page that rows are moved to is named twice, for two sequences or for one (in place: sequences
  * share no page).  new_lens may be lens.  sinks + recent <= keep; ldw >= max_len, ldw_out >= keep, ldtable >=
  * ceil(max_len / page), ld_dst >= ceil(min(keep, max_len) / page); max_len and keep <= 2^30.
  * lens above max_len and pages outside the pool are reported as above (such rows are not moved). */

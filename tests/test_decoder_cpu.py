@@ -443,3 +443,30 @@ def test_rmsnorm_refuses_a_sum_that_runs_over_x(lib):
         assert rms(lib, **{**dict(res=2 * AT, ldr=80, sum=AT, rows=4), **k}) == -1, k
     for k in (dict(xd=0, rd=0), dict(xd=1, rd=1), dict(xd=1, lds=80)):       # (the same place, or no rows)
         assert rms(lib, **{**dict(res=2 * AT, ldr=80, sum=AT, lds=64, rows=0), **k}) == 0, k
+
+
+@pytest.mark.parametrize("L,far", [(300, 187), (3000, 187), (30000, 187), (30000, 120), (30000, 0)])
+def test_what_the_weights_16_bits_cost(L, far):
+    """A key's weight u is off by half a unit of 2^z at most, so by 7 2^z / 16 in the numerator's units of a value: over all keys that are seen the output is within
+    7 L 2^z / (16 den) of a value's unit of the one with weights that are not rounded (t: and its floor, 1/256).  Where one key holds the weight, the others
+    far below it, nearly all of that comes about: den is top, more than 2^(z+7), and the tail of a long row is rounded away from the numerator alone."""
+    rng = np.random.default_rng(L + far)
+    I0, N, d = 17, 15, 64
+    z = (I0 << N).bit_length() - 8
+    vs, vc = np.full(L, 100), np.full((L, d), 7)
+    vc[:, d // 2:] = rng.integers(-7, 8, (L, d // 2))
+    diff = np.full(L, far)
+    diff[0] = 0
+    vs[0], vc[0] = 100, 0
+    e = D.shiftexp(diff, I0, N)
+    den = int(e.sum())
+    u = (e * vs + (1 << (z - 1))) >> z
+    t = np.array([(int(v) << (z + 5)) // den for v in u @ vc]) / 256
+    exact = (e * vs) @ vc / (8 * den)
+    bound = 7 * L * 2 ** z / (16 * den)
+    assert (np.abs(t - exact) <= bound + 1 / 256 + 1e-9).all()
+    assert bound <= L / 292                                          # (den >= top >= 2^(z+7))
+    if far == 187:                                                   # 100 e < 2^(z-1): the whole tail is gone, and it would have counted
+        assert (u[1:] == 0).all() and (t == 0).all() and exact[0] > 0.45 * bound
+    if far == 0:
+        assert np.abs(t - exact).max() <= 7 / 2048 + 1 / 256
