@@ -74,7 +74,7 @@ __device__ __forceinline__ uint2 join(const uint32_t (&c)[4], bool high, int oth
 }
 
 // D / 16 lanes take a row of one token and head: sixteen channels each of K and of V.  The lanes with a byte's low and high halves are
-// neighbours in K, D / 32 apart in V.  What bounds it is the issue of instructions: 20 011 tokens x 8 heads of 64 9.7 us (31 MB would take 4.8), of 128 17.6;
+// neighbours in K, D / 32 apart in V.  What bounds it is the issue of instructions: 20 011 tokens x 8 heads of 64 9.7 us (31 MB would take 4.8), of 128 17.4;
 // with eight channels a lane, and so twice the reductions, steps and addresses, 12.5 and 22.9.  Two rows for each lane were no gain (9.7 and 16.6, a call of
 // 48 tokens 1.9 -> 2.5).
 template <int D>
@@ -170,8 +170,8 @@ __device__ __forceinline__ int first_digit(unsigned long long k) {
 //   1. counts of the first digits, and the digit in which `need` of the largest are reached;
 //   2. the keys of that digit: one value (small weights; all equal) needs no more, up to 1024 are ranked against one another, more are told apart byte by byte;
 //   3. each warp counts what stays of its run, and writes it behind what stays of the runs in front.
-// 12 sequences x 8 heads of 16 001 keys: 19 us, of which the weights' 12.3 MB would be 2; with 96 CTAs it is their passes, one behind the other, that
-// count.  Reading the keys again in each pass takes 19 us more (41.3 / 60.0 for the whole call); for 4000 keys it is all the same (11.8 / 11.3).
+// 12 sequences x 8 heads of 16 001 keys: 20 us, of which the weights' 12.3 MB would be 2; with 96 CTAs it is their passes, one behind the other, that
+// count.  Reading the keys again in each pass takes 19 us more (41.2 / 60.1 for the whole call), for 4000 keys 3 us (13.6 / 16.8).
 template <bool kRegs>
 __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
   constexpr int kKeys = 16;
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(1024) kv4_select_kernel(const EvictArgs a) {
 // Moves the rows that stay, 16 bytes of K and of V to a thread.  kOrdered (in place): one CTA for each (sequence, head), group of rows behind
 // group of rows, each loaded before any of it is stored; rows that are read later lie behind those that are written.  Else the groups of rows are
 // shared out.  Bound by the latency of three dependent loads (index, page, row), hence the rows that a thread has
-// under way: 12 sequences x 8 heads, 4001 rows of 16 001, 102 MB in 25 us, 0.48 of the DRAM's peak.
+// under way: 12 sequences x 8 heads, 4001 rows of 16 001, 27 us alone, 0.45 of the DRAM's peak.
 template <int D, bool kOrdered>
 __global__ void __launch_bounds__(kOrdered ? 512 : 256) kv4_compact_kernel(const EvictArgs a) {
   constexpr int kParts = D / 32, U = 4;                            // threads of a row; rows of a thread

@@ -104,7 +104,7 @@ __device__ __forceinline__ unsigned exp_of(uint32_t w, uint32_t sel, uint32_t t)
 // What bounds it, decoding: 37 sequences of up to 7000 keys, 32 / 8 heads of 128, 139 MB, 33 us (4.2 TB/s, 0.64 of the copy rate): about
 // 160 clocks of an SM for 32 keys, in which no unit is busy half of the time (issue 46 % of all cycles, shared memory 38 %, ALU 33 %), and 8000 clocks
 // around a CTA's keys (set-up, exponentials, exchange, sums, quotients).  Many query rows (16 a CTA): registers hold the sums, two warps
-// for a scheduler do not cover one another's latencies: issue 42 %.
+// for a scheduler do not cover one another's latencies: issue 43 % (5 sequences of up to 300 tokens over up to 2500 keys, 63 us).
 template <int D, int RN, int W, bool kWeights>
 __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attention_kernel(const AttendArgs a) {
   constexpr int kG = D / 32;               // groups of a key
@@ -662,8 +662,8 @@ int launch_kv4_attention(ivit_ctx* ctx, const ivit_kv4_cache& cache, const ivit_
   while (top >> (a.z + 8)) ++a.z;
   a.O = c.O; a.ldo = c.ldo; a.weights = c.weights; a.ldw = c.ldw;
   a.max_q = (int)c.max_q; a.max_len = (int)c.max_len; a.split = p.split; a.blocks = p.blocks; a.kept = p.kept;
-  // Few waves of long CTAs go longest first: 37 sequences of up to 7000 keys 33.6 us / 41.3 in their order; it takes 0.2 us to find a CTA's sequence (the
-  // lengths wait where the scores will be).
+  // Few waves of long CTAs go longest first, 8 heads, us / in their order: sequences of up to 7000 keys 20 of them 24.1 / 26.0, 25 24.5 / 34.1, 37 32.5 / 40.0,
+  // 55 49 / 55; of up to 3000 37 20.8 / 24.0; of up to 12 000 100 130 / 134.  It takes 0.2 us to find a CTA's sequence (the lengths wait where the scores will be).
   const int64_t ctas = cache.heads * c.seqs;
   a.sorted = p.warps == 16 && p.split == 1 && p.tiles == 1 && ctas > ctx->sm_count && c.seqs <= 128 ? (int)c.seqs : 0;
   a.status = ctx->status_dev;

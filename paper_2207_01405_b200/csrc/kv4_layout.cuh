@@ -105,8 +105,8 @@ inline Kv4Div kv4_div(unsigned d) {
 constexpr int kKv4Block = 32;      // keys that a warp takes at a time
 constexpr int kKv4Copies = 8;      // copies of the exponentials
 constexpr int kKv4Blocks = 1024;   // most blocks of a CTA: a byte of codes times a byte of a weight, over 32768 keys, stays below 2^31
-constexpr int kKv4Stages = 3;      // blocks that a warp holds: one that it works on, two on their way (with a fourth 0 to 3 % slower: 34.2 / 33.3 us for
-                                   // 37 sequences of up to 7000 keys, 65.6 / 64.5 for pieces of prompts)
+constexpr int kKv4Stages = 3;      // blocks that a warp holds: one that it works on, two on their way (us / with a fourth: 37 sequences of up to 7000 keys 32.5 /
+                                   // 32.8, 2 of 20 000 16.0 / 16.6, pieces of prompts 63.1 / 63.2; 150 of 5000 89.2 / 87.8)
 constexpr int kKv4Small = 3968;    // bytes of the rows' numbers
 constexpr int kKv4SmemMax = 227 * 1024;
 
@@ -142,11 +142,11 @@ struct Kv4Plan {
 };
 // room[c]: clusters of c CTAs, an SM for each, that the GPU runs at the same time (c <= 16).  The rules were drawn by measurement (us, of the two sides; 8
 // heads of 128 unless noted):
-//   16 query rows a CTA only where tiles of 8 would not run at once: 4 heads, 14 rows: 16 sequences of 3000 keys 15.4 / 14.2 with 8, 30 sequences 19.1 / 22.7
-//   clusters from 24 blocks on, with 8 blocks a CTA at least: 2 sequences of 3000 keys 11.9 in one CTA each head / 8.9 in six, of 600 keys 7.1 / 7.6;
-//   and no larger than run at once: one of 100 003 keys 35.4 in clusters of 10 / 50.2 in clusters of 16, which wait for one another
+//   16 query rows a CTA only where tiles of 8 would not run at once: 4 heads, 14 rows: 16 sequences of 3000 keys 15.0 / 13.5 with 8, 30 sequences 18.7 / 21.5
+//   clusters from 24 blocks on, with 8 blocks a CTA at least: 2 sequences of 3000 keys 13.3 in one CTA each head / 8.1 in clusters, of 600 keys 6.9 / 7.5;
+//   and no larger than run at once: one of 100 003 keys 33.0 in clusters of 10 / 46.8 in clusters of 16, which wait for one another
 //   16 warps, alone on an SM, from 40 blocks a CTA on for each wave of CTAs (few of them: sequences are of uneven lengths, and the longest ends last), else
-//   8, two CTAs on an SM, which overlap one another: 37 sequences of 7000 keys 34.2 / 43.9, of 2000 18.9 / 17.0; 150 of 3000 88 / 67
+//   8, two CTAs on an SM, which overlap one another: 37 sequences of 7000 keys 32.5 / 42.9, of 2000 18.1 / 16.6; 150 of 3000 83 / 64
 inline Kv4Plan kv4_plan(int d, int page, int64_t group, int64_t heads, int64_t seqs, int64_t max_q, int64_t max_len, int sms, const int* room) {
   Kv4Plan p;
   const int64_t all = (max_len + kKv4Block - 1) / kKv4Block, q_rows = max_q * group;

@@ -267,8 +267,8 @@ static void launch_rows(ivit_ctx* ctx, const RmsArgs& a) {
   const int nwords = a.C >> 2;
   auto threads = [&](int wpt) { return ((nwords + wpt - 1) / wpt + 31) / 32 * 32; };
   // R rows at a time where there is work for it (registers hold up to 4096 channels of them), else one row, a thread for each word (beyond 4096: for
-  // four).  us, R rows / one: int8 600 x 2048 5.3 / 5.1, 800 x 2048 5.3 / 5.8, 9000 x 2048 23 / 44; 1650 x 768 5.0 / 5.0; 3000 x 192 4.9 / 4.6, 6000 x 192 5.1 /
-  // 7.3; 450 x 4096 7.7 / 7.3; int32 250 x 2048 5.6 / 4.1, 330 x 2048 5.6 / 5.8.  Words of a thread, one / four, 64 x 4096: 3.1 / 4.4.
+  // four).  us, R rows / one: int8 600 x 2048 5.3 / 5.1, 800 x 2048 5.3 / 5.8, 9000 x 2048 23 / 44; 1650 x 768 5.0 / 5.0; 3000 x 192 4.9 / 4.5, 6000 x 192 5.0 /
+  // 7.3; 450 x 4096 7.7 / 7.3; int32 250 x 2048 5.6 / 4.1, 330 x 2048 5.6 / 5.8.  Words of a thread, one / four, 64 x 4096: 3.1 / 4.5.
   const int64_t sms = ctx->sm_count;
   if (nwords <= 1024 && a.rows >= 3 * sms && (a.rows * nwords >= 275 * R * sms || a.rows >= 3 * R * sms))
     launch_k(nwords % 64 ? rmsnorm_kernel<XI, HI, 2, R, kDyn, false> : rmsnorm_kernel<XI, HI, 2, R, kDyn, true>, (unsigned)((a.rows + R - 1) / R),
