@@ -371,8 +371,8 @@ __global__ void __launch_bounds__(32 * W, RN == 1 && W == 8 ? 2 : 1) kv4_attenti
       send_i32(peer_addr(smem_u32(top_in + rank * kRows + pr), pk), v, peer_addr(bar0, pk));
     }
     if (split > 1) {
-      mbar_wait(bar0, 0, a.status);
-      v = pk < split ? top_in[pk * kRows + pr] : -128;
+      const bool arrived = mbar_wait(bar0, 0, a.status);
+      v = pk < split ? kv4_peer_top(arrived, top_in[pk * kRows + pr]) : -128;
 #pragma unroll
       for (int o = 1; o < 16; o <<= 1) v = max(v, __shfl_xor_sync(~0u, v, o));
       if (pk == 0) top[pr] = v;

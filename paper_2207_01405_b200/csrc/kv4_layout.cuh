@@ -47,6 +47,10 @@ IVIT_KV4_FN int kv4_seen(const Kv4Seq& s, int t) {
   return v < 0 ? 0 : (v > s.len ? s.len : v);
 }
 
+// A peer's maximum of a row, or 127 where the wait for it ran out and the place holds anything: the exponentials are looked up at maximum - score, and with
+// a maximum that is no score's upper bound that would leave the table, and shared memory.  (The outputs are meaningless then, and the status says so.)
+IVIT_KV4_FN int kv4_peer_top(bool arrived, int v) { return arrived ? v : 127; }
+
 // ---- quotients of the attention ----
 
 IVIT_KV4_FN int kv4_clz(unsigned long long n) {

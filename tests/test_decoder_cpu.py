@@ -470,3 +470,19 @@ def test_what_the_weights_16_bits_cost(L, far):
         assert (u[1:] == 0).all() and (t == 0).all() and exact[0] > 0.45 * bound
     if far == 0:
         assert np.abs(t - exact).max() <= 7 / 2048 + 1 / 256
+
+
+def test_a_maximum_that_did_not_arrive_stays_inside_the_table(tmp_path):
+    """Behind a wait that ran out a peer's maximum is whatever shared memory held.  The row's maximum over sixteen of them, some of them there, looks every
+    score up inside the 256 exponentials all the same."""
+    src = tmp_path / "t.cpp"
+    src.write_text('#include <climits>\n#include "kv4_layout.cuh"\nusing namespace ivit;\nint main() {\n'
+                   '  const int junk[] = {INT_MIN, -100000, -129, -128, 0, 127, 128, 65536, INT_MAX};\n'
+                   '  for (int v : junk)\n    for (int there = -128; there < 128; ++there)\n      for (int n = 0; n < 16; ++n) {\n'
+                   '        int top = -128;\n        for (int k = 0; k < 16; ++k) {\n          const int t = k < n ? kv4_peer_top(true, there) : kv4_peer_top(false, v);\n'
+                   '          top = t > top ? t : top;\n        }\n'
+                   '        for (int score = -128; score < 128; ++score)\n          if (top - score < 0 || top - score > 255) return 1;\n      }\n'
+                   '  for (int v = -128; v < 128; ++v)\n    if (kv4_peer_top(true, v) != v) return 2;\n  return 0;\n}\n')
+    exe = tmp_path / "t"
+    subprocess.run(["g++", "-O2", "-I", os.path.join(ROOT, "paper_2207_01405_b200", "csrc"), "-o", str(exe), str(src)], check=True)
+    assert subprocess.run([str(exe)]).returncode == 0
